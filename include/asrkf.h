@@ -140,6 +140,15 @@ typedef struct {
                                 Eq. 2; token scope: its mean over layers) is counted in
                                 asrkf_stats.margin_hits -- decisions that rounding can flip;
                                 a run whose scores keep that margin reports 0 */
+    int32_t kv_bits;         /* 0: the cache holds K and V rows in dtype.  4: in 4 bits (bf16
+                                contexts, resident mode): groups of 32 values share a power
+                                of two X in 2^-100 .. 2^125, the smallest with max|x| < 7 X,
+                                and a value is held as the nearest of 0, 0.5, 1, 1.5, 2, 3, 4,
+                                6 times X with its sign (ties to the even one of the eight, 6 X
+                                for what lies above); a group with an infinity or a NaN reads
+                                as NaN.  Rows are rounded when they enter the cache, and every
+                                step attends to what the codes stand for, the new token's own
+                                row too.  A row of D values takes D / 2 + D / 32 bytes */
 } asrkf_config;
 
 typedef struct {
@@ -175,12 +184,53 @@ asrkf_status asrkf_init(const asrkf_config* cfg, asrkf_ctx** out);
  * pairs (K_j, V_j) of every previous token).  k, v: device,
  * [n_tokens][n_kv_heads][head_dim] of cfg.dtype (EINVAL where that reaches
  * past the end of an allocation; memory that a kernel on this device cannot
- * read, such as host memory, goes through the runtime's copies).  Every layer
+ * read, such as host memory, goes through the runtime's copies; with 4-bit rows
+ * such memory, and pointers off 16-byte alignment, are EINVAL).  Every layer
  * of a sequence must be given the same n_tokens (1 .. max_ctx-1); a sequence
  * never prefilled starts empty.  Only before the first decode step (else
  * ESTATE).  Asynchronous. */
 asrkf_status asrkf_prefill(asrkf_ctx* ctx, int32_t layer, int32_t seq,
                            const void* k, const void* v, int32_t n_tokens, void* stream);
+
+/* Prompts of several sequences in one call, with their attention: the rows of
+ * one layer into the cache as asrkf_prefill does it, and, where q and out are
+ * given, causal attention over each prompt (Eq. 1 with the active set of token
+ * i being the prompt's tokens 0 .. i), which the model around the path needs
+ * before the first decode step.  The prompts stand one after another ("packed",
+ * T tokens in all), in the order of seqs.
+ *   seqs:     host, [n_seqs] sequences, each at most once
+ *   n_tokens: host, [n_seqs] prompt lengths, 0 .. max_ctx-1; 0 gives the
+ *             sequence no prompt.  Every layer of a sequence must be given the
+ *             same length, here or by asrkf_prefill.
+ *   q:        device, [T][n_q_heads][head_dim] of cfg.dtype, or NULL with out:
+ *             the rows are stored only
+ *   k, v:     device, [T][n_kv_heads][head_dim] of cfg.dtype
+ *   q_stride, k_stride, v_stride: elements from one token to the next, 0 for
+ *             dense rows; else at least a token's row, a multiple of 16 bytes
+ *             and at most 16 MiB (rows of a fused projection)
+ *   out:      device, [T][n_q_heads][head_dim] of cfg.dtype, dense (written):
+ *             a prompt's outputs go into the next product in that type.  Sums
+ *             and softmax statistics are held in fp32; bf16 contexts round the
+ *             softmax weights to bf16 for the product with v.
+ * The attention is over k and v as given, also where the cache holds 4 bits.  A
+ * value of v that is not finite reaches the tokens from its own on.  All
+ * pointers 16-byte aligned, in memory of the context's device (EINVAL
+ * otherwise, or where they reach past the end of an allocation).  Only before
+ * the first decode step (else ESTATE).  Asynchronous; the host arrays may be
+ * reused on return. */
+asrkf_status asrkf_prefill_packed(asrkf_ctx* ctx, int32_t layer, int32_t n_seqs,
+                                  const int32_t* seqs, const int32_t* n_tokens,
+                                  const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                                  const void* v, int64_t v_stride, void* out, void* stream);
+
+/* Rows of one (layer, sequence) as the cache holds them, copied out (test
+ * export; also a prompt's rows to keep elsewhere): positions first .. first +
+ * n - 1 of the n_t that the host knows of.  With 4-bit rows the values that
+ * the codes stand for, which enter such a cache again unchanged.
+ *   k, v: device, [n][n_kv_heads][head_dim] of cfg.dtype, 16-byte aligned (written)
+ * ESTATE in spill mode.  Asynchronous. */
+asrkf_status asrkf_get_rows(asrkf_ctx* ctx, int32_t layer, int32_t seq, int32_t first, int32_t n,
+                            void* k, void* v, void* stream);
 
 /* Algorithm 1 up to the end of the freeze loop, for one layer of every
  * sequence: append the new token, attend over the active cache (Eq. 1),

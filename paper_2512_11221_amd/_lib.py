@@ -36,6 +36,7 @@ class asrkf_config(ctypes.Structure):
         ("device_rows", ctypes.c_int32), ("history_W", ctypes.c_int32),
         ("relevance", ctypes.c_int32), ("scope", ctypes.c_int32),
         ("candidates", ctypes.c_int32), ("debug_margin", ctypes.c_float),
+        ("kv_bits", ctypes.c_int32),
     ]
 
 
@@ -79,10 +80,12 @@ def load():
     import torch
     torch.cuda.is_available()
     lib = ctypes.CDLL(LIB_PATH)
-    P, I32, F = ctypes.c_void_p, ctypes.c_int32, ctypes.c_float
+    P, I32, I64, F = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
     sig = {
         "asrkf_init": ([ctypes.POINTER(asrkf_config), ctypes.POINTER(P)], I32),
         "asrkf_prefill": ([P, I32, I32, P, P, I32, P], I32),
+        "asrkf_prefill_packed": ([P, I32, I32, P, P, P, I64, P, I64, P, I64, P, P], I32),
+        "asrkf_get_rows": ([P, I32, I32, I32, I32, P, P, P], I32),
         "asrkf_decode_step": ([P, I32, P, P, P, P, P], I32),
         "asrkf_decode_step_static": ([P, I32, P, P, P, P, P], I32),
         "asrkf_restore": ([P, P, I32, P], I32),
@@ -146,7 +149,7 @@ def _enum(name, value, names):
 def make_config(n_layers, batch, n_q_heads, n_kv_heads, head_dim, max_ctx, window_K, tau,
                 k_soft, vocab, entropy_spike=math.inf, conf_drop=0.0, wr_last_N=0,
                 dtype="bf16", spill_min_D=0, device_rows=0, history_W=0, relevance="abs",
-                scope="layer", candidates="outside", debug_margin=0.0):
+                scope="layer", candidates="outside", debug_margin=0.0, kv_bits=0):
     return asrkf_config(n_layers, batch, n_q_heads, n_kv_heads, head_dim, max_ctx, window_K,
                         tau, k_soft, vocab, entropy_spike, conf_drop, wr_last_N,
                         _enum("dtype", dtype, {"bf16": BF16, "f32": F32}),
@@ -154,7 +157,8 @@ def make_config(n_layers, batch, n_q_heads, n_kv_heads, head_dim, max_ctx, windo
                         _enum("relevance", relevance, {"abs": REL_ABS, "softmax": REL_SOFTMAX}),
                         _enum("scope", scope, {"layer": SCOPE_LAYER, "token": SCOPE_TOKEN}),
                         _enum("candidates", candidates,
-                              {"outside": CAND_OUTSIDE, "inside": CAND_INSIDE}), debug_margin)
+                              {"outside": CAND_OUTSIDE, "inside": CAND_INSIDE}), debug_margin,
+                        kv_bits)
 
 
 def asrkf_init(cfg):
@@ -165,6 +169,43 @@ def asrkf_init(cfg):
 
 def asrkf_prefill(ctx, layer, seq, k, v, n_tokens, stream=None):
     _check(load().asrkf_prefill(ctx, layer, seq, _ptr(k), _ptr(v), n_tokens, _stream(stream)))
+
+
+def _token_stride(name, x):
+    """Elements from one token to the next of packed rows [T][heads][dim]: a tensor's
+    own stride where it has three dimensions (a slice of a fused projection), else 0
+    (dense).  The rows of a token must be dense."""
+    if x is None or not hasattr(x, "stride"):
+        return 0
+    if x.dim() == 3 and x.shape[0] > 1 and x.stride(2) == 1 and x.stride(1) == x.shape[2]:
+        return x.stride(0)
+    if not x.is_contiguous():
+        raise ValueError(f"{name}: the heads of a token must be dense rows")
+    return 0
+
+
+def _dense(name, x):
+    if hasattr(x, "is_contiguous") and not x.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+
+
+def asrkf_prefill_packed(ctx, layer, seqs, n_tokens, q, k, v, out, stream=None):
+    """seqs, n_tokens: Python sequences of ints of the same length."""
+    n = len(seqs)
+    if len(n_tokens) != n:
+        raise ValueError(f"{n} sequences, {len(n_tokens)} lengths")
+    _dense("out", out)
+    a = (ctypes.c_int32 * n)(*seqs)
+    b = (ctypes.c_int32 * n)(*n_tokens)
+    _check(load().asrkf_prefill_packed(ctx, layer, n, a, b, _ptr(q), _token_stride("q", q), _ptr(k),
+                                       _token_stride("k", k), _ptr(v), _token_stride("v", v), _ptr(out),
+                                       _stream(stream)))
+
+
+def asrkf_get_rows(ctx, layer, seq, first, n, k, v, stream=None):
+    _dense("k", k)
+    _dense("v", v)
+    _check(load().asrkf_get_rows(ctx, layer, seq, first, n, _ptr(k), _ptr(v), _stream(stream)))
 
 
 def asrkf_decode_step(ctx, layer, q, k_new, v_new, out, stream=None):

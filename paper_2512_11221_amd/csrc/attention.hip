@@ -50,6 +50,7 @@
 
 #include "attention_split.h"
 #include "kernels.h"
+#include "rows.h"
 
 namespace asrkf {
 namespace {
@@ -238,11 +239,15 @@ __device__ __forceinline__ Plan make_plan(const PlanInput& a, int tile, int32_t*
 
 // ---- tiles ----
 
-template <bool BF16, int D>
+template <int ROWS, int D>
 struct Row {
-    static constexpr int kElem = BF16 ? 2 : 4;
-    static constexpr int kBytes = D * kElem;              // one token, one KV head
-    static constexpr int kLanes = kBytes / 16;            // lanes per row in a load
+    static constexpr bool kFour = ROWS == kRowsFour;
+    static constexpr int kElem = ROWS == kRowsF32 ? 4 : 2;
+    static constexpr int kBytes = D * kElem;              // one token, one KV head, of the arguments and in LDS
+    static constexpr int kPoolBytes = kFour ? D / 2 : kBytes;     // the same in the cache
+    static constexpr int kLanes = kPoolBytes / 16;        // lanes per row in a load
+    static constexpr int kNewLanes = kBytes / 16;         // lanes that hold the new token's row
+    static constexpr int kScales = D / kScaleGroup;       // 4-bit rows: scale bytes of a row
     // tokens per tile: 16 KB of K and V rows, in a wave's registers while they travel
     static constexpr int kTile = tile_tokens(kBytes);
     static constexpr int kBlocks = kTile / 16;            // score blocks of 16 tokens
@@ -258,7 +263,7 @@ struct Row {
     static constexpr int kRelLds = kRelRoomBytes;
     static constexpr int kWaveLds = kTileLds + kRelLds;
     static constexpr int kWaves = kAttnWaves;
-    static constexpr int kQRegs = BF16 ? D / 32 : D / 16; // 16-byte pieces of q per lane
+    static constexpr int kQRegs = kBytes / 64;            // 16-byte pieces of q per lane
 };
 
 // Rows of P: query head h of part p sits in row p * G + h.  With G = 8 the
@@ -372,15 +377,31 @@ __device__ __forceinline__ void store_state(const Acc& acc, float* st, int lane)
     }
 }
 
-template <bool BF16, int D>
-constexpr int threads_of() { return 64 * Row<BF16, D>::kWaves; }
+// A lane's eight values of a row as codes, with their group's scale byte (its four
+// lanes hold the same); x becomes the values that the codes stand for.
+__device__ __forceinline__ uint32_t round_new(intx4& x, uint32_t& byte) {
+    uint32_t top = max_magnitude(max_magnitude(x[0], x[1]), max_magnitude(x[2], x[3]));
+    top = max(top & 0xFFFFu, top >> 16);
+    top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0xB1, 0xF, 0xF, false));   // quad_perm [1,0,3,2]
+    top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0x4E, 0xF, 0xF, false));   // quad_perm [2,3,0,1]
+    byte = scale_byte(top);
+    const float f = scale_value(byte);
+    const uint32_t c = encode8(x[0], x[1], x[2], x[3], f);
+    x = intx4{(int)decode2<0>(c, f), (int)decode2<1>(c, f), (int)decode2<2>(c, f), (int)decode2<3>(c, f)};
+    return c;
+}
 
-template <bool BF16, int D, int G>
-__global__ void __launch_bounds__((threads_of<BF16, D>()), 2)
+template <int ROWS, int D>
+constexpr int threads_of() { return 64 * Row<ROWS, D>::kWaves; }
+
+template <int ROWS, int D, int G>
+__global__ void __launch_bounds__((threads_of<ROWS, D>()), 2)
 attention_kernel(AttnArgs a) {
-    using R = Row<BF16, D>;
+    using R = Row<ROWS, D>;
+    constexpr bool BF16 = ROWS != kRowsF32;
+    constexpr bool FOUR = R::kFour;
     constexpr int kWaves = R::kWaves;
-    constexpr int kThreads = threads_of<BF16, D>();
+    constexpr int kThreads = threads_of<ROWS, D>();
     constexpr int kTile = R::kTile;
     constexpr int NBLK = R::kBlocks;
     constexpr int NL = R::kLoads;
@@ -408,6 +429,7 @@ attention_kernel(AttnArgs a) {
     const int q4 = lane >> 4;
     const int piece = (lane % R::kLanes) * 16;    // the lane's 16 bytes of a row
     const int lrow = lane / R::kLanes;            // its row group in a load
+    const int new_piece = FOUR ? lane * 16 : piece;   // its 16 bytes of the new token's row
     const int wh = wave % hw;                     // the wave's KV head within the group
     const int wt = wave / hw;                     // its turn among the tiles
     const int nwt = kWaves / hw;
@@ -437,9 +459,9 @@ attention_kernel(AttnArgs a) {
         const int pair = b * groups + gi;
         const int g = gi * hw + wh;               // the wave's KV head
         const size_t pool_row0 = ((size_t)b * a.Hkv + g) * a.pool_rows;
-        const int pool_bytes = a.pool_rows * R::kBytes;
-        const auto rk = buffer((const char*)a.kpool + pool_row0 * R::kBytes, pool_bytes);
-        const auto rv = buffer((const char*)a.vpool + pool_row0 * R::kBytes, pool_bytes);
+        const int pool_bytes = a.pool_rows * R::kPoolBytes;
+        const auto rk = buffer((const char*)a.kpool + pool_row0 * R::kPoolBytes, pool_bytes);
+        const auto rv = buffer((const char*)a.vpool + pool_row0 * R::kPoolBytes, pool_bytes);
         const int32_t* list_b = (a.spill ? a.list_row : a.list) + (size_t)b * a.cap;
         const auto rl = buffer(list_b, a.cap * 4);
         const int planes = rel_abs ? groups : a.Hq;
@@ -448,30 +470,66 @@ attention_kernel(AttnArgs a) {
         // dense list one instruction reads 1 KiB in a row.  Lane i of a row of 16 lanes
         // holds the list entry that the row's lanes need in load i (a row broadcast
         // hands it out; where 16 lanes span two tokens, lanes 8 and up hold the second's).
+        // 4-bit rows take two loads a tile: every lane holds its own two entries.
         // The list's last entry is the new token: its row comes from the arguments, not
         // from the cache.
         const int n_cached = nb - 1;
         auto load_rows = [&](int t) __attribute__((always_inline)) {
-            return __builtin_amdgcn_raw_buffer_load_b32(rl, t < t1 ? (t * kTile + entry) * 4 : kNowhere, 0, 0);
+            if constexpr (FOUR) {
+                const int o = (t * kTile + lrow) * 4;
+                return intx2{(int)__builtin_amdgcn_raw_buffer_load_b32(rl, t < t1 ? o : kNowhere, 0, 0),
+                             (int)__builtin_amdgcn_raw_buffer_load_b32(rl, t < t1 ? o + kPer * 4 : kNowhere, 0, 0)};
+            } else {
+                return __builtin_amdgcn_raw_buffer_load_b32(rl, t < t1 ? (t * kTile + entry) * 4 : kNowhere, 0, 0);
+            }
         };
-        auto row_offsets = [&](int t, int rw, int (&off)[NL]) __attribute__((always_inline)) {
+        auto row_offsets = [&](int t, auto rw, int (&off)[NL]) __attribute__((always_inline)) {
             const int lim = t < t1 ? n_cached - t * kTile - lrow : 0;
             unroll<NL>([&](auto J) __attribute__((always_inline)) {
                 constexpr int j = decltype(J)::value;
-                int row = row_bcast<j>(rw);
-                if constexpr (R::kLanes == 8) row = (lane & 8) ? row_bcast<8 + j>(rw) : row;
-                off[j] = j * kPer < lim ? row * R::kBytes + piece : kNowhere;
+                int row;
+                if constexpr (FOUR) {
+                    row = rw[j];
+                } else {
+                    row = row_bcast<j>(rw);
+                    if constexpr (R::kLanes == 8) row = (lane & 8) ? row_bcast<8 + j>(rw) : row;
+                }
+                off[j] = j * kPer < lim ? row * R::kPoolBytes + piece : kNowhere;
             });
         };
         // The order of the loop's loads is fixed (the list entries of the tile after
         // next, the next tile's K rows, its V rows), and the same ahead of the loop, so
         // that every wait counts exactly what is younger.
-        auto load_tile = [&](__amdgpu_buffer_rsrc_t r, const int (&off)[NL], intx4 (&x)[NL])
-            __attribute__((always_inline)) {
+        auto load_tile = [&](__amdgpu_buffer_rsrc_t r, __amdgpu_buffer_rsrc_t rs, const int (&off)[NL], intx4 (&x)[NL],
+                             uint32_t (&sc)[NL]) __attribute__((always_inline)) {
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int j = 0; j < NL; ++j) x[j] = load16<kStreamPolicy>(r, off[j]);
+            if constexpr (FOUR) {                 // byte o / 16 of the scales belongs to the codes at o
+#pragma unroll
+                for (int j = 0; j < NL; ++j)
+                    sc[j] = __builtin_amdgcn_raw_buffer_load_b8(rs, off[j] < 0 ? kNowhere : off[j] >> 4, 0, 0);
+            }
             __builtin_amdgcn_sched_barrier(0);
+        };
+        // a tile's rows, registers -> LDS
+        auto keep_tile = [&](char* to, int stride, const intx4 (&x)[NL], const uint32_t (&sc)[NL])
+            __attribute__((always_inline)) {
+#pragma unroll
+            for (int j = 0; j < NL; ++j) {
+                char* row = to + (j * kPer + lrow) * stride;
+                if constexpr (FOUR) {
+                    const float f = scale_value(sc[j]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const uint32_t c = x[j][e];
+                        *reinterpret_cast<intx4*>(row + piece * 4 + e * 16) =
+                            intx4{(int)decode2<0>(c, f), (int)decode2<1>(c, f), (int)decode2<2>(c, f), (int)decode2<3>(c, f)};
+                    }
+                } else {
+                    *reinterpret_cast<intx4*>(row + piece) = x[j];
+                }
+            }
         };
         // The relevance values stay in LDS and are stored together, at the piece's end or
         // when the room is full, summed over the workgroup's KV heads: stored tile by
@@ -505,8 +563,11 @@ attention_kernel(AttnArgs a) {
             }
         };
 
+        auto scales_of = [&](const uint8_t* p) __attribute__((always_inline)) {
+            return buffer(FOUR ? p + pool_row0 * R::kScales : p, FOUR ? a.pool_rows * R::kScales : 0);
+        };
         int t = t0 + wt;
-        int rows = load_rows(t);
+        auto rows = load_rows(t);
         // the query heads of the wave's KV head, as columns (repeated)
         intx4 qf[NQ];
         {
@@ -522,17 +583,27 @@ attention_kernel(AttnArgs a) {
         int new_row;
         {
             const int span = a.B * a.Hkv * R::kBytes;
-            const int no = owns_new && lane < R::kLanes ? (b * a.Hkv + g) * R::kBytes + piece : kNowhere;
+            const int no = owns_new && lane < R::kNewLanes ? (b * a.Hkv + g) * R::kBytes + new_piece : kNowhere;
             k_new = load16<0>(buffer(a.knew, span), no);
             v_new = load16<0>(buffer(a.vnew, span), no);
             new_row = __builtin_amdgcn_raw_buffer_load_b32(rl, owns_new ? n_cached * 4 : kNowhere, 0, 0);
         }
         intx4 kx[NL], vx[NL];
+        uint32_t ks[NL], vs[NL];                  // 4-bit rows: the scales
+        const auto rks = scales_of(a.kscale), rvs = scales_of(a.vscale);
         int off[NL];
-        int next_rows = load_rows(t + nwt);
+        auto next_rows = load_rows(t + nwt);
         row_offsets(t, rows, off);
-        load_tile(rk, off, kx);
-        load_tile(rv, off, vx);
+        load_tile(rk, rks, off, kx, ks);
+        load_tile(rv, rvs, off, vx, vs);
+        // 4-bit rows: the new token attends as its codes read
+        uint32_t k_codes = 0, v_codes = 0, k_byte = 0, v_byte = 0;
+        if constexpr (FOUR) {
+            if (owns_new) {
+                k_codes = round_new(k_new, k_byte);
+                v_codes = round_new(v_new, v_byte);
+            }
+        }
 
         float m = -INFINITY, l = 0.f;             // of the lane's column (l: its own tokens)
         floatx4 acc[NB];
@@ -545,16 +616,18 @@ attention_kernel(AttnArgs a) {
         int kept = 0;
         for (; t < c1; t += nwt) {
             // K: registers -> LDS, then request the next tile's
+            if constexpr (FOUR) keep_tile(kt, R::kKStride, kx, ks);
+            else
 #pragma unroll
             for (int j = 0; j < NL; ++j)
                 *reinterpret_cast<intx4*>(kt + (j * kPer + lrow) * R::kKStride + piece) = kx[j];
-            if (t == t_new && lane < R::kLanes)
-                *reinterpret_cast<intx4*>(kt + (n_cached % kTile) * R::kKStride + piece) = k_new;
+            if (t == t_new && lane < R::kNewLanes)
+                *reinterpret_cast<intx4*>(kt + (n_cached % kTile) * R::kKStride + new_piece) = k_new;
             __builtin_amdgcn_wave_barrier();
             rows = next_rows;
             next_rows = load_rows(t + 2 * nwt);
             row_offsets(t + nwt, rows, off);
-            load_tile(rk, off, kx);
+            load_tile(rk, rks, off, kx, ks);
 
             // scores: rows = tokens 4 q4 + i (+ 16), column = the lane's head
             // several shorter chains, added at the end: less rounding, less latency
@@ -584,13 +657,15 @@ attention_kernel(AttnArgs a) {
             }
             // V: the same, in the same place
             __builtin_amdgcn_wave_barrier();
+            if constexpr (FOUR) keep_tile(vt, R::kVStride, vx, vs);
+            else
 #pragma unroll
             for (int j = 0; j < NL; ++j)
                 *reinterpret_cast<intx4*>(vt + (j * kPer + lrow) * R::kVStride + piece) = vx[j];
-            if (t == t_new && lane < R::kLanes)
-                *reinterpret_cast<intx4*>(vt + (n_cached % kTile) * R::kVStride + piece) = v_new;
+            if (t == t_new && lane < R::kNewLanes)
+                *reinterpret_cast<intx4*>(vt + (n_cached % kTile) * R::kVStride + new_piece) = v_new;
             __builtin_amdgcn_wave_barrier();
-            load_tile(rv, off, vx);
+            load_tile(rv, rvs, off, vx, vs);
 
             float y[NBLK][4];
             const int left = nb - t * kTile - q4 * 4;     // tokens from the lane's first one on
@@ -736,10 +811,21 @@ attention_kernel(AttnArgs a) {
         lds_barrier();
         c0 = c1;
         }
-        if (owns_new && lane < R::kLanes) {       // the append
-            const size_t dst = (pool_row0 + new_row) * R::kBytes + piece;
-            *reinterpret_cast<intx4*>((char*)a.kpool_w + dst) = k_new;
-            *reinterpret_cast<intx4*>((char*)a.vpool_w + dst) = v_new;
+        if (owns_new && lane < R::kNewLanes) {    // the append
+            const size_t row = pool_row0 + new_row;
+            if constexpr (FOUR) {
+                const size_t dst = row * R::kPoolBytes + lane * 4;
+                *reinterpret_cast<uint32_t*>((char*)a.kpool_w + dst) = k_codes;
+                *reinterpret_cast<uint32_t*>((char*)a.vpool_w + dst) = v_codes;
+                if (lane % 4 == 0) {              // four lanes of eight values are a group
+                    a.kscale_w[row * R::kScales + lane / 4] = (uint8_t)k_byte;
+                    a.vscale_w[row * R::kScales + lane / 4] = (uint8_t)v_byte;
+                }
+            } else {
+                const size_t dst = row * R::kBytes + piece;
+                *reinterpret_cast<intx4*>((char*)a.kpool_w + dst) = k_new;
+                *reinterpret_cast<intx4*>((char*)a.vpool_w + dst) = v_new;
+            }
         }
 
         // ---- merge the waves: every wave's state (its head's G x D sums) into its own tile ----
@@ -885,9 +971,9 @@ attention_kernel(AttnArgs a) {
     }
 }
 
-template <bool BF16, int D, int G>
+template <int ROWS, int D, int G>
 size_t lds_bytes(int B) {
-    using R = Row<BF16, D>;
+    using R = Row<ROWS, D>;
     return (size_t)R::kWaves * R::kWaveLds + R::kWaves * 2 * G * 4 + (B > 64 ? (size_t)(2 * B + 1) * 4 : 0);
 }
 
@@ -900,11 +986,11 @@ struct Launch {
     int* occ;                       // non-null: report occupancy instead
 };
 
-template <bool BF16, int D, int G>
+template <int ROWS, int D, int G>
 hipError_t launch_t(const AttnArgs& a, const Launch& l) {
-    const size_t lds = lds_bytes<BF16, D, G>(a.B);
-    constexpr int threads = threads_of<BF16, D>();
-    auto k = attention_kernel<BF16, D, G>;
+    const size_t lds = lds_bytes<ROWS, D, G>(a.B);
+    constexpr int threads = threads_of<ROWS, D>();
+    auto k = attention_kernel<ROWS, D, G>;
     if (l.occ) {
         return hipOccupancyMaxActiveBlocksPerMultiprocessor(l.occ, k, threads, lds);
     }
@@ -914,25 +1000,29 @@ hipError_t launch_t(const AttnArgs& a, const Launch& l) {
                               args, lds, l.stream, l.start, l.stop, 0);
 }
 
-template <bool BF16, int D>
+template <int ROWS, int D>
 hipError_t launch_g(const AttnArgs& a, int group, const Launch& l) {
     switch (group) {
-        case 1: return launch_t<BF16, D, 1>(a, l);
-        case 2: return launch_t<BF16, D, 2>(a, l);
-        case 4: return launch_t<BF16, D, 4>(a, l);
-        case 8: return launch_t<BF16, D, 8>(a, l);
+        case 1: return launch_t<ROWS, D, 1>(a, l);
+        case 2: return launch_t<ROWS, D, 2>(a, l);
+        case 4: return launch_t<ROWS, D, 4>(a, l);
+        case 8: return launch_t<ROWS, D, 8>(a, l);
     }
     return hipErrorInvalidValue;
 }
 
-hipError_t dispatch(const AttnArgs& a, int dtype_bf16, int head_dim, int group, const Launch& l) {
-    if (dtype_bf16) {
-        if (head_dim == 128) return launch_g<true, 128>(a, group, l);
-        if (head_dim == 64) return launch_g<true, 64>(a, group, l);
-        if (head_dim == 256) return launch_g<true, 256>(a, group, l);
+hipError_t dispatch(const AttnArgs& a, int rows, int head_dim, int group, const Launch& l) {
+    if (rows == kRowsBF16) {
+        if (head_dim == 128) return launch_g<kRowsBF16, 128>(a, group, l);
+        if (head_dim == 64) return launch_g<kRowsBF16, 64>(a, group, l);
+        if (head_dim == 256) return launch_g<kRowsBF16, 256>(a, group, l);
+    } else if (rows == kRowsFour) {
+        if (head_dim == 128) return launch_g<kRowsFour, 128>(a, group, l);
+        if (head_dim == 64) return launch_g<kRowsFour, 64>(a, group, l);
+        if (head_dim == 256) return launch_g<kRowsFour, 256>(a, group, l);
     } else {
-        if (head_dim == 128) return launch_g<false, 128>(a, group, l);
-        if (head_dim == 64) return launch_g<false, 64>(a, group, l);
+        if (head_dim == 128) return launch_g<kRowsF32, 128>(a, group, l);
+        if (head_dim == 64) return launch_g<kRowsF32, 64>(a, group, l);
     }
     return hipErrorInvalidValue;
 }
@@ -948,14 +1038,14 @@ bool attention_shape_supported(int dtype_bf16, int head_dim, int group, int n_kv
     return n_kv_heads * head_dim * (dtype_bf16 ? 2 : 4) <= 8192 && group * n_kv_heads <= 64;
 }
 
-hipError_t launch_attention(const AttnArgs& a, int dtype_bf16, int head_dim, int group,
+hipError_t launch_attention(const AttnArgs& a, int rows, int head_dim, int group,
                             int grid, hipStream_t s, hipEvent_t start, hipEvent_t stop) {
-    return dispatch(a, dtype_bf16, head_dim, group, Launch{grid, s, start, stop, nullptr});
+    return dispatch(a, rows, head_dim, group, Launch{grid, s, start, stop, nullptr});
 }
 
-hipError_t attention_occupancy(const AttnArgs& a, int dtype_bf16, int head_dim, int group,
+hipError_t attention_occupancy(const AttnArgs& a, int rows, int head_dim, int group,
                                int* blocks_per_cu) {
-    return dispatch(a, dtype_bf16, head_dim, group, Launch{0, nullptr, nullptr, nullptr, blocks_per_cu});
+    return dispatch(a, rows, head_dim, group, Launch{0, nullptr, nullptr, nullptr, blocks_per_cu});
 }
 
 }  // namespace asrkf

@@ -42,6 +42,10 @@ __device__ __forceinline__ bool freeze_candidate(int pos, int wedge, bool inside
     return (pos < wedge) != inside;
 }
 
+// How the rows of a cache are held: in the type of the queries, or (bf16 queries)
+// in 4 bits (rows.h).
+enum RowKind { kRowsF32 = 0, kRowsBF16 = 1, kRowsFour = 2 };
+
 // The K/V cache of a layer: [B][Hkv][pool_rows][D], head-major, so that a
 // (sequence, KV head) pair's rows are one contiguous region.
 struct AttnArgs {
@@ -52,6 +56,10 @@ struct AttnArgs {
     const void* vnew;
     void* kpool_w;            // same as kpool, writable (append)
     void* vpool_w;
+    const uint8_t* kscale;    // 4-bit rows: layer base, [B][Hkv][pool_rows][D / 32], else null
+    const uint8_t* vscale;
+    uint8_t* kscale_w;        // the same, writable (append)
+    uint8_t* vscale_w;
     const int32_t* list;      // layer base, [B][cap] ascending positions
     const int32_t* list_row;  // layer base, [B][cap] device row of each listed position
                               // (spill mode only; in resident mode the row is the position)
@@ -187,6 +195,43 @@ struct PrefillArgs {
     int32_t rows;             // rows that the kernel copies: n, or 0 (only the length is set)
 };
 
+// Packed prompts of one layer (prompt.hip).
+constexpr int kPromptSeqs = 192;           // sequences of a launch, whose table is a kernel argument
+constexpr int kPromptStoreTokens = 16;     // tokens of a workgroup that writes rows into the cache
+struct PromptBatch {
+    int32_t n;                             // sequences, none of them empty
+    int32_t start[kPromptSeqs];            // first token among the packed ones
+    int32_t len[kPromptSeqs];              // tokens
+    int32_t first[kPromptSeqs];            // first work unit (set for each launch)
+    uint16_t seq[kPromptSeqs];             // sequence of the context
+};
+struct PromptArgs {
+    const char* q;            // [T][Hq][D], tokens q_stride bytes apart (16-byte aligned, as the strides)
+    const char* k;            // [T][Hkv][D]
+    const char* v;
+    char* out;                // [T][Hq][D], dense
+    int64_t q_stride, k_stride, v_stride;
+    char* kpool;              // layer base, [B][Hkv][pool_rows][row of the cache]
+    char* vpool;
+    uint8_t* kscale;          // 4-bit rows: layer base, [B][Hkv][pool_rows][D / 32]
+    uint8_t* vscale;
+    int32_t* plen;            // [B] prompt lengths (written)
+    int32_t Hq, Hkv, pool_rows;
+    int32_t head_bytes;       // one token, one KV head, of k and v
+    float scale_log2, lazy;   // set for the launch
+};
+// Rows of a sequence's cache, read back.
+struct RowsArgs {
+    const char* kpool;        // the sequence's, [Hkv][pool_rows][row of the cache]
+    const char* vpool;
+    const uint8_t* kscale;
+    const uint8_t* vscale;
+    char* k;                  // [n][Hkv][D]
+    char* v;
+    int32_t first, n, Hkv, pool_rows;
+    int32_t head_bytes;       // one token, one KV head, of k and v
+};
+
 // Row copies between the device cache and the host store (spill mode).
 struct XferArgs {
     char* kpool;              // [L][B][Hkv][pool_rows][row_bytes / Hkv]
@@ -226,9 +271,9 @@ struct EntropyArgs {
 };
 
 // start/stop (may be null) are recorded by the kernel's own dispatch.
-hipError_t launch_attention(const AttnArgs& a, int dtype_bf16, int head_dim, int group,
+hipError_t launch_attention(const AttnArgs& a, int rows, int head_dim, int group,
                             int grid, hipStream_t s, hipEvent_t start, hipEvent_t stop);
-hipError_t attention_occupancy(const AttnArgs& a, int dtype_bf16, int head_dim, int group,
+hipError_t attention_occupancy(const AttnArgs& a, int rows, int head_dim, int group,
                                int* blocks_per_cu);
 hipError_t launch_clear(const ClearArgs& a, hipStream_t s);
 hipError_t launch_compact(const CompactArgs& a, int n_instances, hipStream_t s);
@@ -243,5 +288,10 @@ hipError_t launch_delay(int microseconds, hipStream_t s);
 hipError_t launch_monitor(const EntropyArgs* e, const VerdictArgs& v, hipStream_t s);
 // A prompt's rows into the head-major cache: k, v [n][Hkv][row] -> [Hkv][pool_rows][row].
 hipError_t launch_prefill(const PrefillArgs& a, hipStream_t s);
+// Packed prompts: their rows into the cache; their attention (launch_* fill in what
+// the comments above leave to the launch).
+hipError_t launch_prompt_store(const PromptArgs& a, const PromptBatch& b, bool four, hipStream_t s);
+hipError_t launch_prompt_attention(const PromptArgs& a, const PromptBatch& b, int bf16, int head_dim, hipStream_t s);
+hipError_t launch_get_rows(const RowsArgs& a, bool four, hipStream_t s);
 
 }  // namespace asrkf

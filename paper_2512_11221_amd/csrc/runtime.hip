@@ -2,7 +2,8 @@
 //
 // HBM layout of a context (cap = max_ctx + 1 rounded up to 64 positions;
 // pool_rows = cap in resident mode, the configured device rows in spill mode):
-//   K, V cache      [L][B][Hkv][pool_rows][D]   dtype   head-major rows
+//   K, V cache      [L][B][Hkv][pool_rows][D]   dtype   head-major rows (or 4-bit codes, rows.h)
+//   K, V scales     [L][B][Hkv][pool_rows][D/32] uint8  4-bit rows only
 //   unfreeze U      [L][B][cap]           int32   token attends at step t iff U <= t
 //   count c         [L][B][cap]           int32   low-relevance detections (Eq. 3)
 //   score flag      [L][B][cap]           uint8   s_j < tau at the current step (Eq. 2)
@@ -106,7 +107,9 @@ struct asrkf_ctx {
     int cap = 0;                 // positions per (layer, seq) array
     int group = 0;
     size_t esz = 0;
-    size_t row_bytes = 0;        // one token, all KV heads
+    size_t row_bytes = 0;        // one token, all KV heads, in the cache
+    size_t scale_bytes = 0;      // the same, scale bytes of 4-bit rows (else 0)
+    bool four = false;           // rows held in 4 bits
     int grid = 0;                // attention grid (resident workgroups)
     int heads_per_group = 1;     // KV heads a workgroup takes together (set for each step)
     int launch = 0;              // workgroups of the step's attention launches
@@ -115,6 +118,8 @@ struct asrkf_ctx {
     // device memory
     void* kpool = nullptr;
     void* vpool = nullptr;
+    uint8_t* kscale = nullptr;      // 4-bit rows
+    uint8_t* vscale = nullptr;
     int32_t* unfreeze = nullptr;
     int32_t* count = nullptr;
     uint8_t* flag = nullptr;
@@ -241,7 +246,7 @@ asrkf_status dev_alloc(asrkf_ctx* ctx, T** p, size_t bytes) {
 }
 
 void free_all(asrkf_ctx* ctx) {
-    void* ptrs[] = {ctx->kpool, ctx->vpool, ctx->unfreeze, ctx->count, ctx->flag, ctx->list, ctx->small,
+    void* ptrs[] = {ctx->kpool, ctx->vpool, ctx->kscale, ctx->vscale, ctx->unfreeze, ctx->count, ctx->flag, ctx->list, ctx->small,
                     ctx->part_acc, ctx->rel, ctx->rel_sum, ctx->row_of, ctx->on_host, ctx->list_row, ctx->last_row,
                     ctx->row_owner, ctx->pop_buf, ctx->out_pos, ctx->out_row, ctx->in_pos, ctx->in_row,
                     ctx->hmask, ctx->hlast, ctx->seg_count};
@@ -284,6 +289,9 @@ asrkf_status validate(const asrkf_config* c) {
     if (!(c->debug_margin >= 0.f) || isinf(c->debug_margin))
         return fail(ASRKF_EINVAL, "debug_margin must be finite and >= 0");
     if (c->dtype != ASRKF_BF16 && c->dtype != ASRKF_F32) return fail(ASRKF_EINVAL, "unknown dtype");
+    if (c->kv_bits != 0 && c->kv_bits != 4) return fail(ASRKF_EINVAL, "kv_bits must be 0 or 4");
+    if (c->kv_bits == 4 && c->dtype != ASRKF_BF16) return fail(ASRKF_EINVAL, "4-bit rows need bf16 contexts");
+    if (c->kv_bits == 4 && c->spill_min_D != 0) return fail(ASRKF_EINVAL, "4-bit rows are not combined with spill mode");
     if (c->spill_min_D < 0) return fail(ASRKF_EINVAL, "spill_min_D must be >= 0");
     if (c->history_W < 0 || c->history_W > 64) return fail(ASRKF_EINVAL, "history_W must be in 0..64");
     if (c->relevance != ASRKF_REL_ABS && c->relevance != ASRKF_REL_SOFTMAX)
@@ -323,6 +331,10 @@ hipError_t follow_last_stream(asrkf_ctx* ctx, hipStream_t s) {
     hipError_t e = hipEventRecord(ctx->ev_switch, ctx->last_stream);
     if (e == hipSuccess) e = hipStreamWaitEvent(s, ctx->ev_switch, 0);
     return e;
+}
+
+int row_kind(const asrkf_ctx* ctx) {
+    return ctx->four ? kRowsFour : ctx->cfg.dtype == ASRKF_BF16 ? kRowsBF16 : kRowsF32;
 }
 
 // Split partials, in query heads: one slot per workgroup and pair, each for the
@@ -382,6 +394,36 @@ void mark_queued(asrkf_ctx* ctx, hipStream_t s, bool capture) {
     if (capture) ctx->captured = true;
 }
 
+// Bytes from one token to the next of packed rows, at most: offsets within a tile of
+// 64 tokens stay below 2 GiB.
+constexpr int64_t kMaxTokenStride = (int64_t)16 << 20;
+
+asrkf_status on_device(const asrkf_ctx* ctx) {
+    int d = -1;
+    if (hipGetDevice(&d) != hipSuccess || d != ctx->device)
+        return fail(ASRKF_EINVAL, "the context's device %d is not the current one", ctx->device);
+    return ASRKF_OK;
+}
+
+// What a launch over packed prompts of a layer takes from the context.
+PromptArgs prompt_args(const asrkf_ctx* ctx, int layer) {
+    const asrkf_config& c = ctx->cfg;
+    PromptArgs p{};
+    const size_t rows = (size_t)layer * c.batch * ctx->pool_rows;
+    p.kpool = static_cast<char*>(ctx->kpool) + rows * ctx->row_bytes;
+    p.vpool = static_cast<char*>(ctx->vpool) + rows * ctx->row_bytes;
+    if (ctx->four) {
+        p.kscale = ctx->kscale + rows * ctx->scale_bytes;
+        p.vscale = ctx->vscale + rows * ctx->scale_bytes;
+    }
+    p.plen = ctx->plen;
+    p.Hq = c.n_q_heads;
+    p.Hkv = c.n_kv_heads;
+    p.pool_rows = ctx->pool_rows;
+    p.head_bytes = (int32_t)(c.head_dim * ctx->esz);
+    return p;
+}
+
 }  // namespace
 
 extern "C" {
@@ -408,7 +450,9 @@ asrkf_status asrkf_init(const asrkf_config* cfg, asrkf_ctx** out) {
     ctx->cap = (c.max_ctx + 1 + 63) / 64 * 64;
     ctx->group = c.n_q_heads / c.n_kv_heads;
     ctx->esz = c.dtype == ASRKF_BF16 ? 2 : 4;
-    ctx->row_bytes = (size_t)c.n_kv_heads * c.head_dim * ctx->esz;
+    ctx->four = c.kv_bits == 4;
+    ctx->row_bytes = (size_t)c.n_kv_heads * (ctx->four ? c.head_dim / 2 : c.head_dim * ctx->esz);
+    ctx->scale_bytes = ctx->four ? (size_t)c.n_kv_heads * c.head_dim / 32 : 0;
     ctx->plen_host.assign(c.batch, 0);
     ctx->prefilled.assign(c.batch, 0);
 
@@ -434,7 +478,7 @@ asrkf_status asrkf_init(const asrkf_config* cfg, asrkf_ctx** out) {
         probe.B = c.batch;
         probe.Hkv = c.n_kv_heads;
         int per_cu = 0;
-        e = attention_occupancy(probe, c.dtype == ASRKF_BF16, c.head_dim, ctx->group, &per_cu);
+        e = attention_occupancy(probe, row_kind(ctx), c.head_dim, ctx->group, &per_cu);
         if (e != hipSuccess) { delete ctx; return hip_fail(nullptr, e, "hipOccupancyMaxActiveBlocksPerMultiprocessor"); }
         if (per_cu < 1) {
             delete ctx;
@@ -461,6 +505,10 @@ asrkf_status asrkf_init(const asrkf_config* cfg, asrkf_ctx** out) {
     const size_t pool_bytes = inst * ctx->pool_rows * ctx->row_bytes;
     ALLOC(kpool, pool_bytes);
     ALLOC(vpool, pool_bytes);
+    if (ctx->four) {
+        ALLOC(kscale, inst * ctx->pool_rows * ctx->scale_bytes);
+        ALLOC(vscale, inst * ctx->pool_rows * ctx->scale_bytes);
+    }
     ALLOC(unfreeze, st_pos * 4);
     ALLOC(count, st_pos * 4);
     ALLOC(flag, st_pos);
@@ -609,11 +657,29 @@ asrkf_status asrkf_prefill(asrkf_ctx* ctx, int32_t layer, int32_t seq, const voi
                     seq, ctx->plen_host[seq]);
     hipStream_t s = static_cast<hipStream_t>(stream);
     bool inside_k, inside_v;
-    const size_t bytes = (size_t)n_tokens * ctx->row_bytes;
+    const size_t token_bytes = (size_t)c.n_kv_heads * c.head_dim * ctx->esz;
+    const size_t bytes = (size_t)n_tokens * token_bytes;
     const bool direct_k = kernel_readable(ctx, k, bytes, &inside_k), direct_v = kernel_readable(ctx, v, bytes, &inside_v);
     if (!inside_k || !inside_v)
         return fail(ASRKF_EINVAL, "%s is smaller than %d tokens (%zu bytes)", inside_k ? "v" : "k", n_tokens, bytes);
+    if (ctx->four && (!direct_k || !direct_v || !aligned16(k) || !aligned16(v)))
+        return fail(ASRKF_EINVAL, "4-bit rows are made from 16-byte aligned memory of the context's device");
     HIP_OK(ctx, follow_last_stream(ctx, s));
+    if (ctx->four) {
+        PromptArgs p = prompt_args(ctx, layer);
+        p.k = static_cast<const char*>(k);
+        p.v = static_cast<const char*>(v);
+        p.k_stride = p.v_stride = (int64_t)token_bytes;
+        PromptBatch one{};
+        one.n = 1;
+        one.len[0] = n_tokens;
+        one.seq[0] = (uint16_t)seq;
+        HIP_OK(ctx, launch_prompt_store(p, one, true, s));
+        ctx->prefilled[seq] = 1;
+        ctx->plen_host[seq] = n_tokens;
+        mark_queued(ctx, s, capturing(s));
+        return ASRKF_OK;
+    }
     const size_t off = ((size_t)layer * c.batch + seq) * ctx->pool_rows * ctx->row_bytes;
     PrefillArgs p{};
     p.k = static_cast<const char*>(k);
@@ -641,6 +707,138 @@ asrkf_status asrkf_prefill(asrkf_ctx* ctx, int32_t layer, int32_t seq, const voi
     HIP_OK(ctx, launch_prefill(p, s));
     ctx->prefilled[seq] = 1;
     ctx->plen_host[seq] = n_tokens;
+    mark_queued(ctx, s, capturing(s));
+    return ASRKF_OK;
+}
+
+asrkf_status asrkf_prefill_packed(asrkf_ctx* ctx, int32_t layer, int32_t n_seqs, const int32_t* seqs,
+                                  const int32_t* n_tokens, const void* q, int64_t q_stride, const void* k,
+                                  int64_t k_stride, const void* v, int64_t v_stride, void* out, void* stream) {
+    TraceRange range("asrkf_prefill_packed");
+    asrkf_status st = check_ctx(ctx);
+    if (st != ASRKF_OK) return st;
+    const asrkf_config& c = ctx->cfg;
+    if (ctx->t > 0 || ctx->next_layer != 0 || ctx->lists_ready)
+        return fail(ASRKF_ESTATE, "prefill after the first decode step");
+    if (layer < 0 || layer >= c.n_layers) return fail(ASRKF_EINVAL, "layer out of range");
+    if (n_seqs < 1 || n_seqs > c.batch) return fail(ASRKF_EINVAL, "n_seqs must be in 1..%d", c.batch);
+    if (!seqs || !n_tokens || !k || !v) return fail(ASRKF_EINVAL, "null argument");
+    if (!q != !out) return fail(ASRKF_EINVAL, "q and out go together");
+    st = on_device(ctx);
+    if (st != ASRKF_OK) return st;
+    int64_t total = 0;
+    std::vector<char> seen(c.batch, 0);
+    for (int i = 0; i < n_seqs; ++i) {
+        const int seq = seqs[i], n = n_tokens[i];
+        if (seq < 0 || seq >= c.batch) return fail(ASRKF_EINVAL, "sequence %d out of range", seq);
+        if (seen[seq]) return fail(ASRKF_EINVAL, "sequence %d is named twice", seq);
+        seen[seq] = 1;
+        if (n < 0 || n > c.max_ctx - 1) return fail(ASRKF_EINVAL, "n_tokens must be in 0..max_ctx-1");
+        if (n > ctx->pool_rows - 1)
+            return fail(ASRKF_EINVAL, "n_tokens must leave one device row free (device_rows = %d)", ctx->pool_rows);
+        if (ctx->prefilled[seq] && ctx->plen_host[seq] != n)
+            return fail(ASRKF_EINVAL, "sequence %d was prefilled with %d tokens in another layer", seq,
+                        ctx->plen_host[seq]);
+        total += n;
+    }
+    if (total >= ((int64_t)1 << 31)) return fail(ASRKF_EINVAL, "%lld packed tokens", (long long)total);
+    PromptArgs p = prompt_args(ctx, layer);
+    struct Packed { const char* name; const void* p; int64_t stride; int heads; int64_t* bytes; };
+    const Packed all[] = {{"q", q, q_stride, c.n_q_heads, &p.q_stride},
+                          {"k", k, k_stride, c.n_kv_heads, &p.k_stride},
+                          {"v", v, v_stride, c.n_kv_heads, &p.v_stride},
+                          {"out", out, 0, c.n_q_heads, nullptr}};
+    for (const Packed& x : all) {
+        const int64_t row = (int64_t)x.heads * p.head_bytes;
+        if (x.stride < 0 || x.stride > kMaxTokenStride)
+            return fail(ASRKF_EINVAL, "%s: token stride out of range", x.name);
+        const int64_t stride = x.stride ? x.stride * (int64_t)ctx->esz : row;
+        if (stride < row || stride % 16 || stride > kMaxTokenStride)
+            return fail(ASRKF_EINVAL, "%s: the token stride must be a multiple of 16 bytes from a token's row up to 16 MiB",
+                        x.name);
+        if (x.bytes) *x.bytes = stride;
+        if (!x.p || total == 0) continue;
+        if (!aligned16(x.p)) return fail(ASRKF_EINVAL, "%s must be 16-byte aligned", x.name);
+        bool inside;
+        const size_t bytes = (size_t)(total - 1) * stride + row;
+        if (!kernel_readable(ctx, x.p, bytes, &inside))
+            return fail(ASRKF_EINVAL, "%s must be in memory of the context's device", x.name);
+        if (!inside) return fail(ASRKF_EINVAL, "%s is smaller than %lld tokens", x.name, (long long)total);
+    }
+    p.q = static_cast<const char*>(q);
+    p.k = static_cast<const char*>(k);
+    p.v = static_cast<const char*>(v);
+    p.out = static_cast<char*>(out);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    HIP_OK(ctx, follow_last_stream(ctx, s));
+    // the longest prompts first, so that the launch does not end on one of them
+    std::vector<int32_t> start(n_seqs), order;
+    int32_t at = 0;
+    for (int i = 0; i < n_seqs; ++i) {
+        start[i] = at;
+        at += n_tokens[i];
+        if (n_tokens[i] > 0) order.push_back(i);
+    }
+    std::stable_sort(order.begin(), order.end(), [&](int x, int y) { return n_tokens[x] > n_tokens[y]; });
+    for (size_t i0 = 0; i0 < order.size(); i0 += kPromptSeqs) {
+        PromptBatch b{};
+        for (size_t i = i0; i < order.size() && b.n < kPromptSeqs; ++i, ++b.n) {
+            b.start[b.n] = start[order[i]];
+            b.len[b.n] = n_tokens[order[i]];
+            b.seq[b.n] = (uint16_t)seqs[order[i]];
+        }
+        HIP_OK(ctx, launch_prompt_store(p, b, ctx->four, s));
+        if (q) HIP_OK(ctx, launch_prompt_attention(p, b, c.dtype == ASRKF_BF16, c.head_dim, s));
+    }
+    for (int i = 0; i < n_seqs; ++i) {
+        ctx->prefilled[seqs[i]] = 1;
+        ctx->plen_host[seqs[i]] = n_tokens[i];
+    }
+    mark_queued(ctx, s, capturing(s));
+    return ASRKF_OK;
+}
+
+asrkf_status asrkf_get_rows(asrkf_ctx* ctx, int32_t layer, int32_t seq, int32_t first, int32_t n, void* k, void* v,
+                            void* stream) {
+    asrkf_status st = check_ctx(ctx);
+    if (st != ASRKF_OK) return st;
+    const asrkf_config& c = ctx->cfg;
+    if (ctx->spill) return fail(ASRKF_ESTATE, "rows are not read back in spill mode");
+    if (layer < 0 || layer >= c.n_layers || seq < 0 || seq >= c.batch)
+        return fail(ASRKF_EINVAL, "layer or sequence out of range");
+    const int64_t have = (int64_t)ctx->plen_host[seq] + ctx->t;
+    if (first < 0 || n < 1 || (int64_t)first + n > have)
+        return fail(ASRKF_EINVAL, "positions %d .. %lld of %lld", first, (long long)first + n - 1, (long long)have);
+    if (!k || !v) return fail(ASRKF_EINVAL, "null k or v");
+    if (!aligned16(k) || !aligned16(v)) return fail(ASRKF_EINVAL, "k and v must be 16-byte aligned");
+    st = on_device(ctx);
+    if (st != ASRKF_OK) return st;
+    const size_t bytes = (size_t)n * c.n_kv_heads * c.head_dim * ctx->esz;
+    for (const void* x : {(const void*)k, (const void*)v}) {
+        bool inside;
+        if (!kernel_readable(ctx, x, bytes, &inside))
+            return fail(ASRKF_EINVAL, "k and v must be in memory of the context's device");
+        if (!inside) return fail(ASRKF_EINVAL, "k or v is smaller than %d rows", n);
+    }
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    HIP_OK(ctx, follow_last_stream(ctx, s));
+    const PromptArgs p = prompt_args(ctx, layer);
+    const size_t rows = (size_t)seq * ctx->pool_rows;
+    RowsArgs r{};
+    r.kpool = p.kpool + rows * ctx->row_bytes;
+    r.vpool = p.vpool + rows * ctx->row_bytes;
+    if (ctx->four) {
+        r.kscale = p.kscale + rows * ctx->scale_bytes;
+        r.vscale = p.vscale + rows * ctx->scale_bytes;
+    }
+    r.k = static_cast<char*>(k);
+    r.v = static_cast<char*>(v);
+    r.first = first;
+    r.n = n;
+    r.Hkv = c.n_kv_heads;
+    r.pool_rows = ctx->pool_rows;
+    r.head_bytes = p.head_bytes;
+    HIP_OK(ctx, launch_get_rows(r, ctx->four, s));
     mark_queued(ctx, s, capturing(s));
     return ASRKF_OK;
 }
@@ -868,6 +1066,11 @@ asrkf_status decode_step_impl(asrkf_ctx* ctx, int32_t layer, const void* q, cons
     a.vpool = (const char*)ctx->vpool + pool_off;
     a.kpool_w = (char*)ctx->kpool + pool_off;
     a.vpool_w = (char*)ctx->vpool + pool_off;
+    if (ctx->four) {
+        const size_t scale_off = inst0 * ctx->pool_rows * ctx->scale_bytes;
+        a.kscale = a.kscale_w = ctx->kscale + scale_off;
+        a.vscale = a.vscale_w = ctx->vscale + scale_off;
+    }
     a.q = q;
     a.knew = k_new;
     a.vnew = v_new;
@@ -911,7 +1114,7 @@ asrkf_status decode_step_impl(asrkf_ctx* ctx, int32_t layer, const void* q, cons
             HIP_OK(ctx, hipEventCreateWithFlags(&ev.second, hipEventDisableSystemFence));
         }
     }
-    HIP_OK(ctx, launch_attention(a, c.dtype == ASRKF_BF16, c.head_dim, ctx->group, ctx->launch, s,
+    HIP_OK(ctx, launch_attention(a, row_kind(ctx), c.head_dim, ctx->group, ctx->launch, s,
                                  ev.first, ev.second));
     if (ev.first) ctx->ev_used.push_back(ev);
     // the next layer overwrites the planes kept so far

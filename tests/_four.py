@@ -1,0 +1,27 @@
+"""The 4-bit format of a cache by its definition, in 64 bits (NumPy)."""
+import numpy as np
+
+VALUES = np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])
+
+
+def rounded(x):
+    """The values that the codes of x stand for; groups of 32 along the last axis."""
+    x = np.asarray(x, dtype=np.float64)
+    g = x.reshape(-1, 32)
+    out = np.empty_like(g)
+    bad = ~np.isfinite(g).all(axis=1)
+    out[bad] = np.nan
+    y = g[~bad]
+    top = np.abs(y).max(axis=1, keepdims=True)
+    # X: the smallest power of two with top < 7 X
+    m, e = np.frexp(top / 7)                       # top / 7 = m 2^e, m in [0.5, 1)
+    X = np.exp2(e.astype(np.float64))              # > top / 7
+    X = np.where(top < 7 * (X / 2), X / 2, X)
+    X = np.clip(np.where(top == 0, 2.0 ** -100, X), 2.0 ** -100, 2.0 ** 125)
+    a = np.abs(y) / X
+    code = np.zeros(a.shape, dtype=np.int64)
+    for i in range(1, 8):
+        mid = (VALUES[i - 1] + VALUES[i]) / 2
+        code += (a >= mid) if i % 2 == 0 else (a > mid)      # ties to the even one
+    out[~bad] = np.copysign(VALUES[code] * X, y)
+    return out.reshape(x.shape)
