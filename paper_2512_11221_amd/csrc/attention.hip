@@ -245,25 +245,42 @@ struct Row {
     static constexpr int kElem = ROWS == kRowsF32 ? 4 : 2;
     static constexpr int kBytes = D * kElem;              // one token, one KV head, of the arguments and in LDS
     static constexpr int kPoolBytes = kFour ? D / 2 : kBytes;     // the same in the cache
-    static constexpr int kLanes = kPoolBytes / 16;        // lanes per row in a load
-    static constexpr int kNewLanes = kBytes / 16;         // lanes that hold the new token's row
-    static constexpr int kScales = D / kScaleGroup;       // 4-bit rows: scale bytes of a row
+    static constexpr int kLanes = kBytes / 16;            // lanes per row in a load
     // tokens per tile: 16 KB of K and V rows, in a wave's registers while they travel
-    static constexpr int kTile = tile_tokens(kBytes);
+    // (4-bit rows: the 64 tokens of a wave's score products)
+    static constexpr int kTile = kFour ? kFourTile : tile_tokens(kBytes);
     static constexpr int kBlocks = kTile / 16;            // score blocks of 16 tokens
     static constexpr int kLoads = kTile * kLanes / 64;    // load instructions per tile (K or V)
+    // 4-bit rows: a lane loads 16 bytes of codes, a group of 32 values with one scale
+    static constexpr int kScales = D / kScaleGroup;       // scale bytes (and lanes in a load) of a row
+    static constexpr int kFourRows = 64 / kScales;        // rows per load
+    static constexpr int kFourLoads = kTile / kFourRows;  // loads per tile
+    static constexpr int kSpan = D == 256 ? 16 : 32;      // tokens of V that LDS holds at a time
     // LDS row strides: the padding shifts consecutive rows by 4 (K) and 8 (V)
     // banks, so the 16-byte reads of K rows and the transposed reads of V rows
     // meet no bank twice.  A wave's K tile is read before its V tile is written,
-    // in the same place.
+    // in the same place (4-bit rows: K's codes, then V's values).
     static constexpr int kKStride = kBytes + 16;
     static constexpr int kVStride = kBytes + 32;
-    static constexpr int kTileLds = kTile * kVStride;
+    static constexpr int kTileLds = (kFour ? kSpan : kTile) * kVStride;
     // room for the relevance values a wave keeps before they are stored
-    static constexpr int kRelLds = kRelRoomBytes;
-    static constexpr int kWaveLds = kTileLds + kRelLds;
+    static constexpr int kRelLds = kFour ? four_room(D) : kRelRoomBytes;
+    // 4-bit rows: the scales of a tile's K and V rows, and the query heads with a row of zeros
+    static constexpr int kScaleLds = kFour ? 2 * kTile * kScales : 0;
+    static constexpr int kQStride = kBytes + 16;
+    static constexpr int q_lds(int group) { return kFour ? (group + 1) * kQStride : 0; }
+    static constexpr int wave_lds(int group) { return kTileLds + kRelLds + kScaleLds + q_lds(group); }
     static constexpr int kWaves = kAttnWaves;
     static constexpr int kQRegs = kBytes / 64;            // 16-byte pieces of q per lane
+};
+
+// A tile's codes (of K or V) in a wave's registers: load j takes the rows
+// kFourRows j + lane / kScales; and the scales of one row, the lane's list entry's.
+template <int D>
+struct FourTile {
+    using R = Row<kRowsFour, D>;
+    intx4 codes[R::kFourLoads];
+    uint32_t scale[D == 256 ? 2 : 1];
 };
 
 // Rows of P: query head h of part p sits in row p * G + h.  With G = 8 the
@@ -377,20 +394,7 @@ __device__ __forceinline__ void store_state(const Acc& acc, float* st, int lane)
     }
 }
 
-// A lane's eight values of a row as codes, with their group's scale byte (its four
-// lanes hold the same); x becomes the values that the codes stand for.
-__device__ __forceinline__ uint32_t round_new(intx4& x, uint32_t& byte) {
-    uint32_t top = max_magnitude(max_magnitude(x[0], x[1]), max_magnitude(x[2], x[3]));
-    top = max(top & 0xFFFFu, top >> 16);
-    top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0xB1, 0xF, 0xF, false));   // quad_perm [1,0,3,2]
-    top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0x4E, 0xF, 0xF, false));   // quad_perm [2,3,0,1]
-    byte = scale_byte(top);
-    const float f = scale_value(byte);
-    const uint32_t c = encode8(x[0], x[1], x[2], x[3], f);
-    x = intx4{(int)decode2<0>(c, f), (int)decode2<1>(c, f), (int)decode2<2>(c, f), (int)decode2<3>(c, f)};
-    return c;
-}
-
+#include "attention_four.h"
 template <int ROWS, int D>
 constexpr int threads_of() { return 64 * Row<ROWS, D>::kWaves; }
 
@@ -407,13 +411,15 @@ attention_kernel(AttnArgs a) {
     constexpr int NL = R::kLoads;
     constexpr int NQ = R::kQRegs;
     constexpr int NB = D / 16;                    // column blocks of the accumulators
+    constexpr int kWaveLds = R::wave_lds(G);
     constexpr bool kTwice = two_passes<BF16, G>();
     static_assert(G * (D + 4) * 4 <= R::kTileLds, "wave state fits its tile");
     static_assert(64 * 24 <= R::kTileLds, "a wave's folded states fit its tile");
+    static_assert(!FOUR || kTile * R::kPoolBytes <= R::kTileLds, "K's codes fit the tile");
 
     extern __shared__ __align__(16) char lds[];
     char* tiles = lds;                                            // [kWaves][kWaveLds]
-    float* ml_lds = reinterpret_cast<float*>(lds + kWaves * R::kWaveLds);   // [kWaves][2][G]
+    float* ml_lds = reinterpret_cast<float*>(lds + kWaves * kWaveLds);   // [kWaves][2][G]
     int32_t* plan_lds = reinterpret_cast<int32_t*>(ml_lds + kWaves * 2 * G);
     __shared__ int last_arrival;
 
@@ -429,11 +435,10 @@ attention_kernel(AttnArgs a) {
     const int q4 = lane >> 4;
     const int piece = (lane % R::kLanes) * 16;    // the lane's 16 bytes of a row
     const int lrow = lane / R::kLanes;            // its row group in a load
-    const int new_piece = FOUR ? lane * 16 : piece;   // its 16 bytes of the new token's row
     const int wh = wave % hw;                     // the wave's KV head within the group
     const int wt = wave / hw;                     // its turn among the tiles
     const int nwt = kWaves / hw;
-    char* kt = tiles + wave * R::kWaveLds;        // the wave's K tile, then its V tile
+    char* kt = tiles + wave * kWaveLds;        // the wave's K tile, then its V tile
     char* vt = kt;
     float* rel_kept = reinterpret_cast<float*>(kt + R::kTileLds);  // [tile][wide][kTile]
     // which 8 bits of p the lane's rows of P carry: leading (0), middle (1), trailing (2 and up)
@@ -470,66 +475,30 @@ attention_kernel(AttnArgs a) {
         // dense list one instruction reads 1 KiB in a row.  Lane i of a row of 16 lanes
         // holds the list entry that the row's lanes need in load i (a row broadcast
         // hands it out; where 16 lanes span two tokens, lanes 8 and up hold the second's).
-        // 4-bit rows take two loads a tile: every lane holds its own two entries.
         // The list's last entry is the new token: its row comes from the arguments, not
         // from the cache.
         const int n_cached = nb - 1;
         auto load_rows = [&](int t) __attribute__((always_inline)) {
-            if constexpr (FOUR) {
-                const int o = (t * kTile + lrow) * 4;
-                return intx2{(int)__builtin_amdgcn_raw_buffer_load_b32(rl, t < t1 ? o : kNowhere, 0, 0),
-                             (int)__builtin_amdgcn_raw_buffer_load_b32(rl, t < t1 ? o + kPer * 4 : kNowhere, 0, 0)};
-            } else {
-                return __builtin_amdgcn_raw_buffer_load_b32(rl, t < t1 ? (t * kTile + entry) * 4 : kNowhere, 0, 0);
-            }
+            return __builtin_amdgcn_raw_buffer_load_b32(rl, t < t1 ? (t * kTile + entry) * 4 : kNowhere, 0, 0);
         };
-        auto row_offsets = [&](int t, auto rw, int (&off)[NL]) __attribute__((always_inline)) {
+        auto row_offsets = [&](int t, int rw, int (&off)[NL]) __attribute__((always_inline)) {
             const int lim = t < t1 ? n_cached - t * kTile - lrow : 0;
             unroll<NL>([&](auto J) __attribute__((always_inline)) {
                 constexpr int j = decltype(J)::value;
-                int row;
-                if constexpr (FOUR) {
-                    row = rw[j];
-                } else {
-                    row = row_bcast<j>(rw);
-                    if constexpr (R::kLanes == 8) row = (lane & 8) ? row_bcast<8 + j>(rw) : row;
-                }
-                off[j] = j * kPer < lim ? row * R::kPoolBytes + piece : kNowhere;
+                int row = row_bcast<j>(rw);
+                if constexpr (R::kLanes == 8) row = (lane & 8) ? row_bcast<8 + j>(rw) : row;
+                off[j] = j * kPer < lim ? row * R::kBytes + piece : kNowhere;
             });
         };
         // The order of the loop's loads is fixed (the list entries of the tile after
         // next, the next tile's K rows, its V rows), and the same ahead of the loop, so
         // that every wait counts exactly what is younger.
-        auto load_tile = [&](__amdgpu_buffer_rsrc_t r, __amdgpu_buffer_rsrc_t rs, const int (&off)[NL], intx4 (&x)[NL],
-                             uint32_t (&sc)[NL]) __attribute__((always_inline)) {
+        auto load_tile = [&](__amdgpu_buffer_rsrc_t r, const int (&off)[NL], intx4 (&x)[NL])
+            __attribute__((always_inline)) {
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int j = 0; j < NL; ++j) x[j] = load16<kStreamPolicy>(r, off[j]);
-            if constexpr (FOUR) {                 // byte o / 16 of the scales belongs to the codes at o
-#pragma unroll
-                for (int j = 0; j < NL; ++j)
-                    sc[j] = __builtin_amdgcn_raw_buffer_load_b8(rs, off[j] < 0 ? kNowhere : off[j] >> 4, 0, 0);
-            }
             __builtin_amdgcn_sched_barrier(0);
-        };
-        // a tile's rows, registers -> LDS
-        auto keep_tile = [&](char* to, int stride, const intx4 (&x)[NL], const uint32_t (&sc)[NL])
-            __attribute__((always_inline)) {
-#pragma unroll
-            for (int j = 0; j < NL; ++j) {
-                char* row = to + (j * kPer + lrow) * stride;
-                if constexpr (FOUR) {
-                    const float f = scale_value(sc[j]);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const uint32_t c = x[j][e];
-                        *reinterpret_cast<intx4*>(row + piece * 4 + e * 16) =
-                            intx4{(int)decode2<0>(c, f), (int)decode2<1>(c, f), (int)decode2<2>(c, f), (int)decode2<3>(c, f)};
-                    }
-                } else {
-                    *reinterpret_cast<intx4*>(row + piece) = x[j];
-                }
-            }
         };
         // The relevance values stay in LDS and are stored together, at the piece's end or
         // when the room is full, summed over the workgroup's KV heads: stored tile by
@@ -549,12 +518,12 @@ attention_kernel(AttnArgs a) {
                     const int turn = row % nwt, idx = row / nwt;
                     for (int h = 0; h < hw; ++h)
                         v += *reinterpret_cast<const floatx4*>(
-                            tiles + (h + hw * turn) * R::kWaveLds + R::kTileLds + (idx * kTile + o * 4) * 4);
+                            tiles + (h + hw * turn) * kWaveLds + R::kTileLds + (idx * kTile + o * 4) * 4);
                     at = gi * a.rel_cap + (c0 + row) * kTile + o * 4;
                 } else {
                     const int c = row % wide, idx = row / wide % per_wave, wv = row / wide / per_wave;
                     const int tile = c0 + wv / hw + idx * nwt;
-                    v = *reinterpret_cast<const floatx4*>(tiles + wv * R::kWaveLds + R::kTileLds +
+                    v = *reinterpret_cast<const floatx4*>(tiles + wv * kWaveLds + R::kTileLds +
                                                           ((idx * wide + c) * kTile + o * 4) * 4);
                     at = ((gi * hw + wv % hw) * G + c) * a.rel_cap + tile * kTile + o * 4;
                     if (tile >= c1) at = kNowhere / 4;
@@ -563,11 +532,41 @@ attention_kernel(AttnArgs a) {
             }
         };
 
-        auto scales_of = [&](const uint8_t* p) __attribute__((always_inline)) {
-            return buffer(FOUR ? p + pool_row0 * R::kScales : p, FOUR ? a.pool_rows * R::kScales : 0);
-        };
+        float m = -INFINITY, l = 0.f;             // of the lane's column (l: its own tokens)
+        floatx4 acc[NB];
+#pragma unroll
+        for (int k = 0; k < NB; ++k) acc[k] = floatx4{0.f, 0.f, 0.f, 0.f};
+        int first = t0;                           // first tile of the last chunk
+        if constexpr (FOUR) {
+            FourStream<D, G> f;
+            f.lane = lane;
+            f.lds = kt;
+            f.rel_kept = rel_kept;
+            f.t1 = t1;
+            f.n = nb;
+            f.step = nwt;
+            f.scale_log2 = a.scale_log2;
+            f.rel_abs = rel_abs;
+            f.list = rl;
+            f.k = rk;
+            f.v = rv;
+            f.ks = buffer(a.kscale + pool_row0 * R::kScales, a.pool_rows * R::kScales);
+            f.vs = buffer(a.vscale + pool_row0 * R::kScales, a.pool_rows * R::kScales);
+            const int row = b * a.Hkv + g;        // of the new token's rows, and of the queries' heads
+            f.begin(a, t0 + wt, t0, row, pool_row0);
+            for (int c0 = t0, kept = 0;; kept = 0) {
+                const int c1 = min(t1, c0 + chunk);
+                for (; f.t < c1; f.t += nwt) f.tile(kept++, m, l, acc);
+                first = c0;
+                if (c1 == t1) break;
+                lds_barrier();
+                store_kept(c0, c1);
+                lds_barrier();
+                c0 = c1;
+            }
+        } else {
         int t = t0 + wt;
-        auto rows = load_rows(t);
+        int rows = load_rows(t);
         // the query heads of the wave's KV head, as columns (repeated)
         intx4 qf[NQ];
         {
@@ -583,32 +582,17 @@ attention_kernel(AttnArgs a) {
         int new_row;
         {
             const int span = a.B * a.Hkv * R::kBytes;
-            const int no = owns_new && lane < R::kNewLanes ? (b * a.Hkv + g) * R::kBytes + new_piece : kNowhere;
+            const int no = owns_new && lane < R::kLanes ? (b * a.Hkv + g) * R::kBytes + piece : kNowhere;
             k_new = load16<0>(buffer(a.knew, span), no);
             v_new = load16<0>(buffer(a.vnew, span), no);
             new_row = __builtin_amdgcn_raw_buffer_load_b32(rl, owns_new ? n_cached * 4 : kNowhere, 0, 0);
         }
         intx4 kx[NL], vx[NL];
-        uint32_t ks[NL], vs[NL];                  // 4-bit rows: the scales
-        const auto rks = scales_of(a.kscale), rvs = scales_of(a.vscale);
         int off[NL];
-        auto next_rows = load_rows(t + nwt);
+        int next_rows = load_rows(t + nwt);
         row_offsets(t, rows, off);
-        load_tile(rk, rks, off, kx, ks);
-        load_tile(rv, rvs, off, vx, vs);
-        // 4-bit rows: the new token attends as its codes read
-        uint32_t k_codes = 0, v_codes = 0, k_byte = 0, v_byte = 0;
-        if constexpr (FOUR) {
-            if (owns_new) {
-                k_codes = round_new(k_new, k_byte);
-                v_codes = round_new(v_new, v_byte);
-            }
-        }
-
-        float m = -INFINITY, l = 0.f;             // of the lane's column (l: its own tokens)
-        floatx4 acc[NB];
-#pragma unroll
-        for (int k = 0; k < NB; ++k) acc[k] = floatx4{0.f, 0.f, 0.f, 0.f};
+        load_tile(rk, off, kx);
+        load_tile(rv, off, vx);
 
         int c0 = t0;                              // first tile of the chunk
         for (;;) {
@@ -616,18 +600,16 @@ attention_kernel(AttnArgs a) {
         int kept = 0;
         for (; t < c1; t += nwt) {
             // K: registers -> LDS, then request the next tile's
-            if constexpr (FOUR) keep_tile(kt, R::kKStride, kx, ks);
-            else
 #pragma unroll
             for (int j = 0; j < NL; ++j)
                 *reinterpret_cast<intx4*>(kt + (j * kPer + lrow) * R::kKStride + piece) = kx[j];
-            if (t == t_new && lane < R::kNewLanes)
-                *reinterpret_cast<intx4*>(kt + (n_cached % kTile) * R::kKStride + new_piece) = k_new;
+            if (t == t_new && lane < R::kLanes)
+                *reinterpret_cast<intx4*>(kt + (n_cached % kTile) * R::kKStride + piece) = k_new;
             __builtin_amdgcn_wave_barrier();
             rows = next_rows;
             next_rows = load_rows(t + 2 * nwt);
             row_offsets(t + nwt, rows, off);
-            load_tile(rk, rks, off, kx, ks);
+            load_tile(rk, off, kx);
 
             // scores: rows = tokens 4 q4 + i (+ 16), column = the lane's head
             // several shorter chains, added at the end: less rounding, less latency
@@ -657,15 +639,13 @@ attention_kernel(AttnArgs a) {
             }
             // V: the same, in the same place
             __builtin_amdgcn_wave_barrier();
-            if constexpr (FOUR) keep_tile(vt, R::kVStride, vx, vs);
-            else
 #pragma unroll
             for (int j = 0; j < NL; ++j)
                 *reinterpret_cast<intx4*>(vt + (j * kPer + lrow) * R::kVStride + piece) = vx[j];
-            if (t == t_new && lane < R::kNewLanes)
-                *reinterpret_cast<intx4*>(vt + (n_cached % kTile) * R::kVStride + new_piece) = v_new;
+            if (t == t_new && lane < R::kLanes)
+                *reinterpret_cast<intx4*>(vt + (n_cached % kTile) * R::kVStride + piece) = v_new;
             __builtin_amdgcn_wave_barrier();
-            load_tile(rv, rvs, off, vx, vs);
+            load_tile(rv, off, vx);
 
             float y[NBLK][4];
             const int left = nb - t * kTile - q4 * 4;     // tokens from the lane's first one on
@@ -811,31 +791,27 @@ attention_kernel(AttnArgs a) {
         lds_barrier();
         c0 = c1;
         }
-        if (owns_new && lane < R::kNewLanes) {    // the append
-            const size_t row = pool_row0 + new_row;
-            if constexpr (FOUR) {
-                const size_t dst = row * R::kPoolBytes + lane * 4;
-                *reinterpret_cast<uint32_t*>((char*)a.kpool_w + dst) = k_codes;
-                *reinterpret_cast<uint32_t*>((char*)a.vpool_w + dst) = v_codes;
-                if (lane % 4 == 0) {              // four lanes of eight values are a group
-                    a.kscale_w[row * R::kScales + lane / 4] = (uint8_t)k_byte;
-                    a.vscale_w[row * R::kScales + lane / 4] = (uint8_t)v_byte;
-                }
-            } else {
-                const size_t dst = row * R::kBytes + piece;
-                *reinterpret_cast<intx4*>((char*)a.kpool_w + dst) = k_new;
-                *reinterpret_cast<intx4*>((char*)a.vpool_w + dst) = v_new;
-            }
+        if (owns_new && lane < R::kLanes) {       // the append
+            const size_t dst = (pool_row0 + new_row) * R::kBytes + piece;
+            *reinterpret_cast<intx4*>((char*)a.kpool_w + dst) = k_new;
+            *reinterpret_cast<intx4*>((char*)a.vpool_w + dst) = v_new;
+        }
+        first = c0;
         }
 
         // ---- merge the waves: every wave's state (its head's G x D sums) into its own tile ----
+        if constexpr (FOUR) {                     // the lane's own tokens: of one part of its column
+            if constexpr (G < 8) l += __shfl_xor(l, 4);
+            l += __shfl_xor(l, 8);
+        }
         l += __shfl_xor(l, 16);
         l += __shfl_xor(l, 32);
         if (lane < G) {
             ml_lds[(wave * 2) * G + lane] = m;
             ml_lds[(wave * 2 + 1) * G + lane] = l;
         }
-        store_state<BF16, D, G>(acc, reinterpret_cast<float*>(kt), lane);
+        if constexpr (FOUR) store_state_four<D, G>(acc, reinterpret_cast<float*>(kt), lane);
+        else store_state<BF16, D, G>(acc, reinterpret_cast<float*>(kt), lane);
         lds_barrier();
         const int heads = hw * G;                 // query heads of the piece
         const size_t slot0 = (size_t)(slot - part) * heads;        // the pair's first partial
@@ -855,7 +831,7 @@ attention_kernel(AttnArgs a) {
                 const int wv = min(h_kv + hw * j, kWaves - 1);
                 mw[j] = j < nwt ? ml_lds[(wv * 2) * G + h] : -INFINITY;
                 lw[j] = ml_lds[(wv * 2 + 1) * G + h];
-                ow[j] = *reinterpret_cast<const floatx4*>(tiles + wv * R::kWaveLds + (h * (D + 4) + d) * 4);
+                ow[j] = *reinterpret_cast<const floatx4*>(tiles + wv * kWaveLds + (h * (D + 4) + d) * 4);
             }
             float M = mw[0];
 #pragma unroll
@@ -902,8 +878,8 @@ attention_kernel(AttnArgs a) {
                 constexpr int kFoldThreads = F::kSpan, kSlotGroups = F::kSlotGroups;
                 const int grp = threadIdx.x / kFoldThreads;
                 // a thread's state, in its wave's tile (the relevance values are still kept)
-                auto fold_o = [&](int th) { return reinterpret_cast<floatx4*>(tiles + th / 64 * R::kWaveLds) + th % 64; };
-                auto fold_ml = [&](int th) { return reinterpret_cast<float*>(tiles + th / 64 * R::kWaveLds + 1024) + th % 64 * 2; };
+                auto fold_o = [&](int th) { return reinterpret_cast<floatx4*>(tiles + th / 64 * kWaveLds) + th % 64; };
+                auto fold_ml = [&](int th) { return reinterpret_cast<float*>(tiles + th / 64 * kWaveLds + 1024) + th % 64 * 2; };
                 for (int e0 = 0; e0 < heads * D; e0 += kFoldThreads * 4) {
                     const int mine = e0 + threadIdx.x % kFoldThreads * 4;
                     const int e = min(mine, heads * D - 4);          // the others repeat the last
@@ -965,7 +941,7 @@ attention_kernel(AttnArgs a) {
                 if (threadIdx.x == 0) a.ticket[pair] = 0;      // ready for the next launch
             }
         }
-        store_kept(c0, t1);
+        store_kept(first, t1);
         lds_barrier();                           // the wave states have been read: tiles may be rewritten
     }
     }
@@ -974,7 +950,7 @@ attention_kernel(AttnArgs a) {
 template <int ROWS, int D, int G>
 size_t lds_bytes(int B) {
     using R = Row<ROWS, D>;
-    return (size_t)R::kWaves * R::kWaveLds + R::kWaves * 2 * G * 4 + (B > 64 ? (size_t)(2 * B + 1) * 4 : 0);
+    return (size_t)R::kWaves * R::wave_lds(G) + R::kWaves * 2 * G * 4 + (B > 64 ? (size_t)(2 * B + 1) * 4 : 0);
 }
 
 // Timing events, when given, are recorded by the dispatch itself, so they

@@ -24,10 +24,13 @@ constexpr int kHalfTiles = 8;
 constexpr int kTileBytes = 8192;
 constexpr int kRelRoomBytes = 8192;
 constexpr int kAttnWaves = 8;
+// 4-bit rows: tokens of a tile, and the room for relevance values
+constexpr int kFourTile = 64;
+constexpr int four_room(int head_dim) { return head_dim == 256 ? 4096 : 6144; }
 
 ASRKF_HD constexpr int tile_tokens(int row_bytes) { return kTileBytes / row_bytes; }
 // tiles whose relevance values a workgroup has room for
-constexpr int room_tiles(int tile) { return kRelRoomBytes / (tile * 4) * kAttnWaves; }
+constexpr int room_tiles(int tile, int room = kRelRoomBytes) { return room / (tile * 4) * kAttnWaves; }
 
 ASRKF_HD int lesser(int a, int b) { return a < b ? a : b; }
 ASRKF_HD int greater(int a, int b) { return a > b ? a : b; }
@@ -152,9 +155,9 @@ ASRKF_HD bool next_piece(const Split& split, const Lists& lists, int w, int& x, 
 // How a step's attention is laid out when sequence b lists up to plen[b] + t
 // positions: KV heads a workgroup takes together, and how many workgroups to
 // launch (at least those with work, at most grid: idle ones delay the others).
-inline void attention_layout(const int32_t* plen, int batch, int t, int n_kv_heads, int row_bytes, int grid,
+// Tiles of `tile` tokens; a wave has `room` bytes for relevance values.
+inline void attention_layout(const int32_t* plen, int batch, int t, int n_kv_heads, int tile, int room, int grid,
                              int* heads_per_group, int* launch) {
-    const int tile = tile_tokens(row_bytes);
     int64_t tiles = 0;
     for (int b = 0; b < batch; ++b) tiles += (plen[b] + tile) / tile;
     // One KV head per piece while every pair can have a workgroup and the pieces are
@@ -175,7 +178,7 @@ inline void attention_layout(const int32_t* plen, int batch, int t, int n_kv_hea
     // grow long from short prompts stay with the heads chosen for those (64 sequences
     // grown from nothing to 18k tokens: 712 us a launch).
     int hw = 1;
-    if (tiles * n_kv_heads > (int64_t)room_tiles(tile) * grid) hw = n_kv_heads < 8 ? n_kv_heads : 8;
+    if (tiles * n_kv_heads > (int64_t)room_tiles(tile, room) * grid) hw = n_kv_heads < 8 ? n_kv_heads : 8;
     while (hw < 8 && hw < n_kv_heads && (int64_t)batch * n_kv_heads / hw > grid) hw *= 2;
     const int64_t groups = n_kv_heads / hw;
     const int cost = kPieceCost / hw > 1 ? kPieceCost / hw : 1;
@@ -186,6 +189,10 @@ inline void attention_layout(const int32_t* plen, int batch, int t, int n_kv_hea
     *heads_per_group = hw;
     *launch = live < grid ? (live > 1 ? (int)live : 1) : grid;
 }
-
+// ... of rows of 16 or 32 bits
+inline void attention_layout(const int32_t* plen, int batch, int t, int n_kv_heads, int row_bytes, int grid,
+                             int* heads_per_group, int* launch) {
+    attention_layout(plen, batch, t, n_kv_heads, tile_tokens(row_bytes), kRelRoomBytes, grid, heads_per_group, launch);
+}
 
 }  // namespace asrkf

@@ -42,6 +42,14 @@ __device__ __forceinline__ intx4 load16(__amdgpu_buffer_rsrc_t r, int off) {
     return __builtin_bit_cast(intx4, __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0));
 }
 
+template <int N, typename F>
+__device__ __forceinline__ void unroll(F f) {
+    if constexpr (N > 0) {
+        unroll<N - 1>(f);
+        f(std::integral_constant<int, N - 1>{});
+    }
+}
+
 // The sequence of the batch whose units (blocks, given by their first ones) hold unit x.
 __device__ __forceinline__ int find_sequence(const PromptBatch& b, int x) {
     int lo = 0, hi = b.n - 1;                 // the last with first <= x
@@ -149,8 +157,7 @@ struct Tile {
     // rows 4 apart of 128 bytes (V, fp32), meet no bank twice
     static constexpr int kKStride = kRow + 16;
     static constexpr int kVStride = kRow + (BF16 ? 64 : 32);
-    static constexpr int kVAt = kKeys * kKStride;         // V's place in a buffer
-    static constexpr int kBuffer = kVAt + kKeys * kVStride;
+    static constexpr int kKBuffer = kKeys * kKStride, kVBuffer = kKeys * kVStride;     // two of each
     static constexpr int kLoads = kKeys * kRow / 16 / kThreads;   // 16-byte pieces of K (or V) per thread
     static constexpr int kQRegs = BF16 ? D / 16 : D / 8;  // 16-byte pieces of q per lane
     static_assert(kLoads * kThreads * 16 == kKeys * kRow, "whole pieces per thread");
@@ -185,7 +192,7 @@ prompt_attention_kernel(PromptArgs a, PromptBatch batch) {
     using T = Tile<BF16, D, WAVES>;
     constexpr int NL = T::kLoads, KB = T::kKB, NQ = T::kQRegs, DB = D / 32;
     constexpr int kPieces = T::kRow / 16;                 // pieces of a row
-    __shared__ __align__(16) char lds[2 * T::kBuffer];
+    __shared__ __align__(16) char lds[2 * (T::kKBuffer + T::kVBuffer)];
     __shared__ int holds_infinite[2];                     // the tile whose V values are not all finite
 
     const int kvh = blockIdx.x % a.Hkv;
@@ -218,23 +225,27 @@ prompt_attention_kernel(PromptArgs a, PromptBatch batch) {
     const char* v0 = a.v + (size_t)batch.start[si] * a.v_stride + kvh * T::kRow;
     intx4 kx[NL], vx[NL];
     // rows past the sequence's end read as zeros
-    auto request = [&](int j) __attribute__((always_inline)) {
+    auto request = [&](const char* base, int64_t stride, int j, intx4 (&x)[NL]) __attribute__((always_inline)) {
         const int left = min(T::kKeys, n - j * T::kKeys);
-        const auto rk = buffer(k0 + (size_t)j * T::kKeys * a.k_stride, left > 0 ? (int)((left - 1) * a.k_stride + T::kRow) : 0);
-        const auto rv = buffer(v0 + (size_t)j * T::kKeys * a.v_stride, left > 0 ? (int)((left - 1) * a.v_stride + T::kRow) : 0);
+        const auto r = buffer(base + (size_t)j * T::kKeys * stride, left > 0 ? (int)((left - 1) * stride + T::kRow) : 0);
 #pragma unroll
         for (int u = 0; u < NL; ++u) {
             const int i = threadIdx.x + u * T::kThreads;
-            kx[u] = load16(rk, (i / kPieces) * (int)a.k_stride + i % kPieces * 16);
-        }
-#pragma unroll
-        for (int u = 0; u < NL; ++u) {
-            const int i = threadIdx.x + u * T::kThreads;
-            vx[u] = load16(rv, (i / kPieces) * (int)a.v_stride + i % kPieces * 16);
+            x[u] = load16(r, (i / kPieces) * (int)stride + i % kPieces * 16);
         }
     };
-    auto keep = [&](int j) __attribute__((always_inline)) {
-        char* to = lds + (j & 1) * T::kBuffer;
+    auto request_k = [&](int j) __attribute__((always_inline)) { request(k0, a.k_stride, j, kx); };
+    auto request_v = [&](int j) __attribute__((always_inline)) { request(v0, a.v_stride, j, vx); };
+    auto keep_k = [&](int j) __attribute__((always_inline)) {
+        char* to = lds + (j & 1) * T::kKBuffer;
+#pragma unroll
+        for (int u = 0; u < NL; ++u) {
+            const int i = threadIdx.x + u * T::kThreads;
+            *reinterpret_cast<intx4*>(to + i / kPieces * T::kKStride + i % kPieces * 16) = kx[u];
+        }
+    };
+    auto keep_v = [&](int j) __attribute__((always_inline)) {
+        char* to = lds + 2 * T::kKBuffer + (j & 1) * T::kVBuffer;
         // Where a tile holds keys behind some query of the block, a weight of zero must not
         // meet an infinity or a NaN: those values are added on their own.
         if (j * T::kKeys + T::kKeys - 1 > first_token) {
@@ -246,8 +257,7 @@ prompt_attention_kernel(PromptArgs a, PromptBatch batch) {
 #pragma unroll
         for (int u = 0; u < NL; ++u) {
             const int i = threadIdx.x + u * T::kThreads;
-            *reinterpret_cast<intx4*>(to + i / kPieces * T::kKStride + i % kPieces * 16) = kx[u];
-            *reinterpret_cast<intx4*>(to + T::kVAt + i / kPieces * T::kVStride + i % kPieces * 16) = vx[u];
+            *reinterpret_cast<intx4*>(to + i / kPieces * T::kVStride + i % kPieces * 16) = vx[u];
         }
     };
 
@@ -258,32 +268,17 @@ prompt_attention_kernel(PromptArgs a, PromptBatch batch) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[d][i] = 0.f;
 
-    if (threadIdx.x < 2) holds_infinite[threadIdx.x] = -1;
-    request(0);
-    __syncthreads();
-    keep(0);
-    request(1);
-    for (int j = 0; j < tiles; ++j) {
-        __syncthreads();                                  // tile j is in place, tile j - 1 has been read
-        if (j + 1 < tiles) {
-            keep(j + 1);
-            request(j + 2);
-        }
-        if (j * T::kKeys > wave_last) continue;           // all of it lies behind the wave's queries
-        const char* kt = lds + (j & 1) * T::kBuffer;
-        const char* vt = kt + T::kVAt;
-
-        floatx16 s[KB];
-#pragma unroll
-        for (int b = 0; b < KB; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) s[b][i] = 0.f;
+    auto scores = [&](int j, floatx16 (&s)[KB]) __attribute__((always_inline)) {
+        const char* kt = lds + (j & 1) * T::kKBuffer;
 #pragma unroll
         for (int i = 0; i < NQ; ++i)
 #pragma unroll
             for (int b = 0; b < KB; ++b) {
                 const intx4 kr = *reinterpret_cast<const intx4*>(
                     kt + (b * 32 + col) * T::kKStride + (BF16 ? i * 32 + half * 16 : half * (T::kRow / 2) + i * 16));
+                if (i == 0)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) s[b][e] = 0.f;
                 if constexpr (BF16) {
                     s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kr),
                                                                    __builtin_bit_cast(bf16x8, q[i]), s[b], 0, 0, 0);
@@ -293,9 +288,13 @@ prompt_attention_kernel(PromptArgs a, PromptBatch batch) {
                         s[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(__int_as_float(kr[e]), __int_as_float(q[i][e]), s[b], 0, 0, 0);
                 }
             }
+    };
+    auto tile = [&](int j) __attribute__((always_inline)) {
+        floatx16 s[KB];
+        scores(j, s);
+        const char* vt = lds + 2 * T::kKBuffer + (j & 1) * T::kVBuffer;
         // key of value i in block b: 32 b + 8 (i / 4) + 4 half + i % 4
-        const bool masked = j * T::kKeys + T::kKeys - 1 > wave_first;
-        if (masked) {
+        if (j * T::kKeys + T::kKeys - 1 > wave_first) {
             const int left = token - j * T::kKeys - half * 4;     // keys up to the lane's token, from its first
 #pragma unroll
             for (int b = 0; b < KB; ++b)
@@ -320,43 +319,40 @@ prompt_attention_kernel(PromptArgs a, PromptBatch batch) {
                 for (int i = 0; i < 16; ++i) acc[d][i] *= sc;
         }
         const float bias = -(m == -INFINITY ? 0.f : m * a.scale_log2) - kLazy;
+        // V's transposed reads (bf16): 4 keys of 16 dims per 16 lanes
+        const char* vb = vt + (half * 4 + (lane & 15) / 4) * T::kVStride + (lane >> 4 & 1) * 32 + (lane & 3) * 8;
+        constexpr int kGroups = KB * 2;                   // of 16 keys
+        unroll<kGroups>([&](auto B) __attribute__((always_inline)) {
+            constexpr int b = decltype(B)::value;
+            float p[8];
 #pragma unroll
-        for (int b = 0; b < KB; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                s[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], a.scale_log2, bias));
-                l += s[b][i];
+            for (int e = 0; e < 8; ++e) {
+                p[e] = __builtin_amdgcn_exp2f(fmaf(s[b / 2][b % 2 * 8 + e], a.scale_log2, bias));
+                l += p[e];
             }
-
-        if constexpr (BF16) {
-            // V's transposed reads: 4 keys of 16 dims per 16 lanes
-            const char* vb = vt + (half * 4 + (lane & 15) / 4) * T::kVStride + (lane >> 4 & 1) * 32 + (lane & 3) * 8;
+            if constexpr (BF16) {
+                bf16x8 w;
 #pragma unroll
-            for (int b = 0; b < KB * 2; ++b) {            // 16 keys
-                bf16x8 p;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) p[e] = (__bf16)s[b / 2][b % 2 * 8 + e];
+                for (int e = 0; e < 8; ++e) w[e] = (__bf16)p[e];
 #pragma unroll
                 for (int d = 0; d < DB; ++d) {
                     const char* at = vb + b * 16 * T::kVStride + d * 64;
                     const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4)at);
                     const shortx4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4)(at + 8 * T::kVStride));
                     const bf16x8 v = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-                    acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p, acc[d], 0, 0, 0);
+                    acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w, acc[d], 0, 0, 0);
                 }
-            }
-        } else {
+            } else {
 #pragma unroll
-            for (int b = 0; b < KB; ++b)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const char* at = vt + (b * 32 + i / 4 * 8 + half * 4 + i % 4) * T::kVStride + col * 4;
+                for (int e = 0; e < 8; ++e) {
+                    const char* at = vt + (b * 16 + e / 4 * 8 + half * 4 + e % 4) * T::kVStride + col * 4;
 #pragma unroll
                     for (int d = 0; d < DB; ++d)
                         acc[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(*reinterpret_cast<const float*>(at + d * 128),
-                                                                      s[b][i], acc[d], 0, 0, 0);
+                                                                      p[e], acc[d], 0, 0, 0);
                 }
-        }
+            }
+        });
         if (holds_infinite[j & 1] == j) {
             // the values that are not finite, from memory, to the queries that see their key
             // (whatever their weight)
@@ -374,6 +370,24 @@ prompt_attention_kernel(PromptArgs a, PromptBatch batch) {
                     }
             }
         }
+    };
+    if (threadIdx.x < 2) holds_infinite[threadIdx.x] = -1;
+    request_k(0);
+    request_v(0);
+    __syncthreads();
+    keep_k(0);
+    keep_v(0);
+    request_k(1);
+    request_v(1);
+    for (int j = 0; j < tiles; ++j) {
+        __syncthreads();                                  // tile j is in place, tile j - 1 has been read
+        if (j + 1 < tiles) {
+            keep_k(j + 1);
+            keep_v(j + 1);
+            request_k(j + 2);
+            request_v(j + 2);
+        }
+        if (j * T::kKeys <= wave_last) tile(j);           // else all of it lies behind the wave's queries
     }
 
     const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);

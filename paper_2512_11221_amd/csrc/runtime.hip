@@ -1042,8 +1042,12 @@ asrkf_status decode_step_impl(asrkf_ctx* ctx, int32_t layer, const void* q, cons
     HIP_OK(ctx, follow_last_stream(ctx, s));
     mark_queued(ctx, s, capture);
     if (layer == 0) {
-        attention_layout(ctx->plen_host.data(), c.batch, t, c.n_kv_heads, (int)(c.head_dim * ctx->esz), ctx->grid,
-                         &ctx->heads_per_group, &ctx->launch);
+        if (ctx->four)
+            attention_layout(ctx->plen_host.data(), c.batch, t, c.n_kv_heads, kFourTile, four_room(c.head_dim), ctx->grid,
+                             &ctx->heads_per_group, &ctx->launch);
+        else
+            attention_layout(ctx->plen_host.data(), c.batch, t, c.n_kv_heads, (int)(c.head_dim * ctx->esz), ctx->grid,
+                             &ctx->heads_per_group, &ctx->launch);
         if (capture) ctx->launch = ctx->grid;    // replayed at later, longer steps
     }
     if (!ctx->lists_ready) {
