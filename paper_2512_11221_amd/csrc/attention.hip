@@ -244,11 +244,11 @@ struct Row {
     static constexpr bool kFour = ROWS == kRowsFour;
     static constexpr int kElem = ROWS == kRowsF32 ? 4 : 2;
     static constexpr int kBytes = D * kElem;              // one token, one KV head, of the arguments and in LDS
-    static constexpr int kPoolBytes = kFour ? D / 2 : kBytes;     // the same in the cache
+    static constexpr int kPoolBytes = kFour ? four_row_bytes(D) : kBytes;     // the same in the cache
     static constexpr int kLanes = kBytes / 16;            // lanes per row in a load
     // tokens per tile: 16 KB of K and V rows, in a wave's registers while they travel
-    // (4-bit rows: the 64 tokens of a wave's score products)
-    static constexpr int kTile = kFour ? kFourTile : tile_tokens(kBytes);
+    // (4-bit rows: 64, or 32 of 256 values)
+    static constexpr int kTile = kFour ? four_tile(D) : tile_tokens(kBytes);
     static constexpr int kBlocks = kTile / 16;            // score blocks of 16 tokens
     static constexpr int kLoads = kTile * kLanes / 64;    // load instructions per tile (K or V)
     // 4-bit rows: a lane loads 16 bytes of codes, a group of 32 values with one scale
@@ -415,7 +415,7 @@ attention_kernel(AttnArgs a) {
     constexpr bool kTwice = two_passes<BF16, G>();
     static_assert(G * (D + 4) * 4 <= R::kTileLds, "wave state fits its tile");
     static_assert(64 * 24 <= R::kTileLds, "a wave's folded states fit its tile");
-    static_assert(!FOUR || kTile * R::kPoolBytes <= R::kTileLds, "K's codes fit the tile");
+    static_assert(!FOUR || kTile * D / 2 <= R::kTileLds, "K's codes fit the tile");
 
     extern __shared__ __align__(16) char lds[];
     char* tiles = lds;                                            // [kWaves][kWaveLds]
@@ -550,8 +550,6 @@ attention_kernel(AttnArgs a) {
             f.list = rl;
             f.k = rk;
             f.v = rv;
-            f.ks = buffer(a.kscale + pool_row0 * R::kScales, a.pool_rows * R::kScales);
-            f.vs = buffer(a.vscale + pool_row0 * R::kScales, a.pool_rows * R::kScales);
             const int row = b * a.Hkv + g;        // of the new token's rows, and of the queries' heads
             f.begin(a, t0 + wt, t0, row, pool_row0);
             for (int c0 = t0, kept = 0;; kept = 0) {
@@ -801,7 +799,7 @@ attention_kernel(AttnArgs a) {
 
         // ---- merge the waves: every wave's state (its head's G x D sums) into its own tile ----
         if constexpr (FOUR) {                     // the lane's own tokens: of one part of its column
-            if constexpr (G < 8) l += __shfl_xor(l, 4);
+            if constexpr (four_columns(D, G) == 4) l += __shfl_xor(l, 4);
             l += __shfl_xor(l, 8);
         }
         l += __shfl_xor(l, 16);

@@ -43,6 +43,10 @@ __device__ __forceinline__ intx4 decode8(uint32_t c, float f) {
     return intx4{(int)decode2<0>(c, f), (int)decode2<1>(c, f), (int)decode2<2>(c, f), (int)decode2<3>(c, f)};
 }
 
+// Columns of a part of the score products: a tile of four parts holds 64 tokens, of
+// two parts 32 (rows of 256, whose loads and sums take the registers).
+constexpr int four_columns(int head_dim, int group) { return group == 8 || head_dim == 256 ? 8 : 4; }
+
 // the value of the lane N places along the lane's row of 16 (which way is the same
 // for every use)
 template <int N>
@@ -60,18 +64,21 @@ __device__ __forceinline__ void store_state_four(const Acc& acc, float* st, int 
     for (int k = 0; k < D / 16; ++k) {
         float* col = st + k * 16 + c16;
         const floatx4 v = acc[k];
-        if constexpr (G == 1) {
+        if constexpr (four_columns(D, G) == 8) {
+            const int h = (q4 & 1) * 4 + (q4 >> 1);
+#pragma unroll
+            for (int i = 0; i < 4; i += 2) {
+                const float x = add_halves(v[i], v[i + 1]);
+                if (h + i < G) col[(h + i) * S] = x;
+            }
+        } else if constexpr (G == 1) {
             const float x = add_halves(add_rows16(v[0], v[0]), 0.f);
             if (q4 == 0) col[0] = x;
         } else if constexpr (G == 2) {
             const float x = add_halves(add_rows16(v[0], v[1]), 0.f);
             if (q4 < 2) col[q4 * S] = x;
-        } else if constexpr (G == 4) {
-            col[q4 * S] = add_halves(add_rows16(v[0], v[1]), add_rows16(v[2], v[3]));
         } else {
-            const int h = (q4 & 1) * 4 + (q4 >> 1);
-#pragma unroll
-            for (int i = 0; i < 4; i += 2) col[(h + i) * S] = add_halves(v[i], v[i + 1]);
+            col[q4 * S] = add_halves(add_rows16(v[0], v[1]), add_rows16(v[2], v[3]));
         }
     }
 }
@@ -79,18 +86,18 @@ __device__ __forceinline__ void store_state_four(const Acc& acc, float* st, int 
 template <int D, int G>
 struct FourStream {
     using R = Row<kRowsFour, D>;
-    static constexpr int GC = G < 4 ? 4 : G;              // columns of a part
+    static constexpr int GC = four_columns(D, G);         // columns of a part
     static constexpr int kParts = 16 / GC;
-    static constexpr int kC = 64 / (16 * kParts);         // C tiles of a tile
-    static constexpr int kPieces = D / 32 * GC / 4 == D / 32 ? D / 32 : D / 64;   // 16-byte pieces of K per lane
+    static constexpr int kTile = R::kTile;
+    static constexpr int kC = kTile / (16 * kParts);      // C tiles of a tile
+    static constexpr int kPieces = kParts == 4 ? D / 32 : D / 64;     // 16-byte pieces of K per lane
     static constexpr int NL = R::kFourLoads, NB = D / 16;
-    static_assert(R::kTile == 64, "a tile is what the lanes of a load of scales cover");
 
     int lane, t, t1, n, step, rel_abs;
     char* lds;
     float* rel_kept;
     float scale_log2;
-    __amdgpu_buffer_rsrc_t list, k, v, ks, vs;
+    __amdgpu_buffer_rsrc_t list, k, v;
 
     int next_rows, t_new;
     bool owns_new;
@@ -100,34 +107,35 @@ struct FourStream {
     const char* q;                                        // the lane's operand of the score products
 
     __device__ __forceinline__ char* k_scales() const { return lds + R::kTileLds + R::kRelLds; }
-    __device__ __forceinline__ char* v_scales() const { return k_scales() + 64 * R::kScales; }
-    __device__ __forceinline__ char* queries() const { return v_scales() + 64 * R::kScales; }
+    __device__ __forceinline__ char* v_scales() const { return k_scales() + kTile * R::kScales; }
+    __device__ __forceinline__ char* queries() const { return v_scales() + kTile * R::kScales; }
 
     // The list entry that a lane holds, among a tile's: row lane / kScales of load
     // lane % NL, so that the lanes of a row have what they need in every load.
     __device__ __forceinline__ int entry() const { return R::kFourRows * (lane % NL) + lane / R::kScales; }
     template <int J>
     __device__ __forceinline__ int from_entry(int x) const {
-        if constexpr (D == 256) return __builtin_amdgcn_ds_bpermute(((lane & ~7) | J) * 4, x);
-        else return __builtin_amdgcn_update_dpp(0, x, D == 64 ? J | J << 2 | (2 + J) << 4 | (2 + J) << 6 : J * 0x55, 0xF, 0xF, false);
+        return __builtin_amdgcn_update_dpp(0, x, D == 64 ? J | J << 2 | (2 + J) << 4 | (2 + J) << 6 : J * 0x55, 0xF, 0xF, false);
     }
     __device__ __forceinline__ int rows(int t) const {
-        return __builtin_amdgcn_raw_buffer_load_b32(list, t < t1 ? (t * 64 + entry()) * 4 : kNowhere, 0, 0);
+        return __builtin_amdgcn_raw_buffer_load_b32(list, t < t1 ? (t * kTile + entry()) * 4 : kNowhere, 0, 0);
     }
+    // a device has fewer than 2^24 rows of a head
+    __device__ static __forceinline__ int row_at(int row) { return (int)__umul24(row, R::kPoolBytes); }
     // the list's last entry is the new token: its row comes from the arguments
-    __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t r, __amdgpu_buffer_rsrc_t rs, int t, int row, FourTile<D>& x) const {
-        const int lim = t < t1 ? n - 1 - t * 64 : 0;
+    __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t r, int t, int row, FourTile<D>& x) const {
+        const int lim = t < t1 ? n - 1 - t * kTile : 0;
         __builtin_amdgcn_sched_barrier(0);
         unroll<NL>([&](auto J) __attribute__((always_inline)) {
             constexpr int j = decltype(J)::value;
-            const int o = from_entry<j>(row) * R::kPoolBytes + lane % R::kScales * 16;
+            const int o = row_at(from_entry<j>(row)) + lane % R::kScales * 16;
             x.codes[j] = load16<kStreamPolicy>(r, j * R::kFourRows + lane / R::kScales < lim ? o : kNowhere);
         });
-        const int so = entry() < lim ? row * R::kScales : kNowhere;
-        if constexpr (D == 64) x.scale[0] = __builtin_amdgcn_raw_buffer_load_b16(rs, so, 0, 0);
-        else if constexpr (D == 128) x.scale[0] = __builtin_amdgcn_raw_buffer_load_b32(rs, so, 0, 0);
+        const int so = entry() < lim ? row_at(row) + D / 2 : kNowhere;
+        if constexpr (D == 64) x.scale[0] = __builtin_amdgcn_raw_buffer_load_b16(r, so, 0, kStreamPolicy);
+        else if constexpr (D == 128) x.scale[0] = __builtin_amdgcn_raw_buffer_load_b32(r, so, 0, kStreamPolicy);
         else {
-            const uintx2 w = __builtin_bit_cast(uintx2, __builtin_amdgcn_raw_buffer_load_b64(rs, so, 0, 0));
+            const uintx2 w = __builtin_bit_cast(uintx2, __builtin_amdgcn_raw_buffer_load_b64(r, so, 0, kStreamPolicy));
             x.scale[0] = w[0];
             x.scale[1] = w[1];
         }
@@ -150,7 +158,7 @@ struct FourStream {
     // the wave's tiles hold it.  row: of the arguments.
     __device__ __forceinline__ void begin(const AttnArgs& a, int first, int t0, int row, size_t pool_row0) {
         t = first;
-        t_new = (n - 1) / 64;
+        t_new = (n - 1) / kTile;
         owns_new = t_new >= first && t_new < t1 && (t_new - first) % step == 0;
         const int now = rows(t);
         constexpr int kQ = G * D / 8;                     // 16-byte pieces of the queries
@@ -167,8 +175,8 @@ struct FourStream {
         }
         const int new_row = __builtin_amdgcn_raw_buffer_load_b32(list, owns_new ? (n - 1) * 4 : kNowhere, 0, 0);
         next_rows = rows(t + step);
-        load(k, ks, t, now, kx);
-        load(v, vs, t, now, vx);
+        load(k, t, now, kx);
+        load(v, t, now, vx);
 #pragma unroll
         for (int i = 0; i < (kQ + 63) / 64; ++i) {
             const int e = i * 64 + lane;
@@ -184,11 +192,16 @@ struct FourStream {
             encode_group(kn, k_new, k_byte);
             encode_group(vn, v_new, v_byte);
             if (lane < R::kScales) {                      // the append
-                const size_t at = (pool_row0 + new_row) * R::kScales + lane;
-                *reinterpret_cast<intx4*>((char*)a.kpool_w + at * 16) = k_new;
-                *reinterpret_cast<intx4*>((char*)a.vpool_w + at * 16) = v_new;
-                a.kscale_w[at] = (uint8_t)k_byte;
-                a.vscale_w[at] = (uint8_t)v_byte;
+                const size_t at = (pool_row0 + new_row) * R::kPoolBytes;
+                char* kr = (char*)a.kpool_w + at;
+                char* vr = (char*)a.vpool_w + at;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    *reinterpret_cast<int*>(kr + lane * 16 + e * 4) = k_new[e];
+                    *reinterpret_cast<int*>(vr + lane * 16 + e * 4) = v_new[e];
+                }
+                kr[D / 2 + lane] = (char)k_byte;
+                vr[D / 2 + lane] = (char)v_byte;
             }
         }
     }
@@ -213,6 +226,7 @@ struct FourStream {
         for (int e = 0; e < kPieces; ++e) {
             const intx4 x = *reinterpret_cast<const intx4*>(lds + code_at(token, piece0 + e));
             const float f = scale_value(sc[e / 4] >> e % 4 * 8 & 255u);
+            if constexpr (D == 256) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
                 const intx4 b = *reinterpret_cast<const intx4*>(q + (e * 4 + w) * 16);
@@ -235,7 +249,7 @@ struct FourStream {
             for (int e = 0; e < 4; ++e)
                 *reinterpret_cast<intx4*>(row + e * 16) = decode8(vx.codes[kFrom + i][e], f);
         });
-        if (t == t_new && (n - 1) % 64 / R::kSpan == J && lane < R::kScales) {
+        if (t == t_new && (n - 1) % kTile / R::kSpan == J && lane < R::kScales) {
             char* row = lds + (n - 1) % R::kSpan * R::kVStride + lane * 64;
 #pragma unroll
             for (int e = 0; e < 4; ++e)
@@ -252,14 +266,14 @@ struct FourStream {
             *reinterpret_cast<intx4*>(lds + code_at(j * R::kFourRows + lane / R::kScales, lane % R::kScales)) = kx.codes[j];
         keep_scales(k_scales(), kx);
         if (t == t_new && lane < R::kScales) {
-            const int e = (n - 1) % 64;
+            const int e = (n - 1) % kTile;
             *reinterpret_cast<intx4*>(lds + code_at(e, lane)) = k_new;
             k_scales()[e * R::kScales + lane] = (char)k_byte;
         }
         __builtin_amdgcn_wave_barrier();
         const int row = next_rows;
         next_rows = rows(t + 2 * step);
-        load(k, ks, t + step, row, kx);
+        load(k, t + step, row, kx);
 
         floatx4 s[kC];
 #pragma unroll
@@ -271,8 +285,8 @@ struct FourStream {
         for (int c = 0; c < kC; ++c)
 #pragma unroll
             for (int i = 0; i < 4; ++i) y[c][i] = s[c][i] * scale_log2;
-        if (t * 64 + 64 > n) {                            // entries past the list's end
-            const int left = n - t * 64 - part * 16 - q4 * 4;
+        if (t * kTile + kTile > n) {                            // entries past the list's end
+            const int left = n - t * kTile - part * 16 - q4 * 4;
 #pragma unroll
             for (int c = 0; c < kC; ++c)
 #pragma unroll
@@ -280,7 +294,7 @@ struct FourStream {
         }
         // relevance: the sum of |q.k| over the KV head's query heads (neighbouring
         // columns), or the logits themselves
-        float* keep = rel_kept + (size_t)(kept * (rel_abs ? 1 : G) + (rel_abs ? 0 : c16 % GC)) * 64 + part * 16 + q4 * 4;
+        float* keep = rel_kept + (size_t)(kept * (rel_abs ? 1 : G) + (rel_abs ? 0 : c16 % GC)) * kTile + part * 16 + q4 * 4;
         if (rel_abs) {
 #pragma unroll
             for (int c = 0; c < kC; ++c) {
@@ -359,24 +373,25 @@ struct FourStream {
                 mid[c][i] = kParts == 4 ? row_rotate<4>(mid[c][i]) : row_rotate<8>(mid[c][i]);
                 if constexpr (kParts == 4) lo[c][i] = row_rotate<8>(lo[c][i]);
             }
-        // rows of block b (16 tokens): first pass, second pass (eight heads)
+        // rows of block b (16 tokens): first pass, second pass (eight heads); masks, because
+        // the compiler made branches of selects
         auto weights = [&](int b, int i) __attribute__((always_inline)) {
             const int c = b / kParts, p = b % kParts;
-            if constexpr (kParts == 2) return p == part ? hi[c][i] : mid[c][i];
-            return p == part ? hi[c][i] : p == part_mid ? mid[c][i] : p == part_lo ? lo[c][i] : 0;
+            const int w = (hi[c][i] & -(int)(p == part)) | (mid[c][i] & -(int)(p == part_mid));
+            return kParts == 2 ? w : w | (lo[c][i] & -(int)(p == part_lo));
         };
         auto weights_lo = [&](int b, int i) __attribute__((always_inline)) {
-            return b % kParts == part ? lo[b / kParts][i] : 0;
+            return lo[b / kParts][i] & -(int)(b % kParts == part);
         };
 
         // V, and O += P V
         keep_scales(v_scales(), vx);
         const char* vb = lds + (q4 * 4 + c16 / 4) * R::kVStride + (c16 % 4) * 8;
-        unroll<64 / R::kSpan>([&](auto J) __attribute__((always_inline)) {
+        unroll<kTile / R::kSpan>([&](auto J) __attribute__((always_inline)) {
             constexpr int j = decltype(J)::value;
             __builtin_amdgcn_wave_barrier();
             keep_values<j>();
-            if constexpr (j == 64 / R::kSpan - 1) load(v, vs, t + step, row, vx);
+            if constexpr (j == kTile / R::kSpan - 1) load(v, t + step, row, vx);
             __builtin_amdgcn_wave_barrier();
             if constexpr (R::kSpan == 16) {
                 const shortx4 w = __builtin_bit_cast(shortx4, intx2{weights(j, 0), weights(j, 1)});

@@ -25,7 +25,7 @@ constexpr int kTileBytes = 8192;
 constexpr int kRelRoomBytes = 8192;
 constexpr int kAttnWaves = 8;
 // 4-bit rows: tokens of a tile, and the room for relevance values
-constexpr int kFourTile = 64;
+constexpr int four_tile(int head_dim) { return head_dim == 256 ? 32 : 64; }
 constexpr int four_room(int head_dim) { return head_dim == 256 ? 4096 : 6144; }
 
 ASRKF_HD constexpr int tile_tokens(int row_bytes) { return kTileBytes / row_bytes; }

@@ -56,10 +56,6 @@ struct AttnArgs {
     const void* vnew;
     void* kpool_w;            // same as kpool, writable (append)
     void* vpool_w;
-    const uint8_t* kscale;    // 4-bit rows: layer base, [B][Hkv][pool_rows][D / 32], else null
-    const uint8_t* vscale;
-    uint8_t* kscale_w;        // the same, writable (append)
-    uint8_t* vscale_w;
     const int32_t* list;      // layer base, [B][cap] ascending positions
     const int32_t* list_row;  // layer base, [B][cap] device row of each listed position
                               // (spill mode only; in resident mode the row is the position)
@@ -196,14 +192,17 @@ struct PrefillArgs {
 };
 
 // Packed prompts of one layer (prompt.hip).
-constexpr int kPromptSeqs = 192;           // sequences of a launch, whose table is a kernel argument
+constexpr int kPromptSeqs = 128;           // sequences of a launch, whose table is a kernel argument
 constexpr int kPromptStoreTokens = 16;     // tokens of a workgroup that writes rows into the cache
 struct PromptBatch {
     int32_t n;                             // sequences, none of them empty
     int32_t start[kPromptSeqs];            // first token among the packed ones
     int32_t len[kPromptSeqs];              // tokens
-    int32_t first[kPromptSeqs];            // first work unit (set for each launch)
-    uint16_t seq[kPromptSeqs];             // sequence of the context
+    int32_t first[kPromptSeqs];            // first work unit of the attention, and of the rows'
+    int32_t first_store[kPromptSeqs];      //   store (set for the launch)
+    int32_t seq[kPromptSeqs];              // sequence of the context (32 bits like the others: beside
+                                           //   16-bit entries the compiler formed scalar loads off
+                                           //   word alignment, which read another entry)
 };
 struct PromptArgs {
     const char* q;            // [T][Hq][D], tokens q_stride bytes apart (16-byte aligned, as the strides)
@@ -213,19 +212,18 @@ struct PromptArgs {
     int64_t q_stride, k_stride, v_stride;
     char* kpool;              // layer base, [B][Hkv][pool_rows][row of the cache]
     char* vpool;
-    uint8_t* kscale;          // 4-bit rows: layer base, [B][Hkv][pool_rows][D / 32]
-    uint8_t* vscale;
     int32_t* plen;            // [B] prompt lengths (written)
     int32_t Hq, Hkv, pool_rows;
     int32_t head_bytes;       // one token, one KV head, of k and v
-    float scale_log2, lazy;   // set for the launch
+    int32_t four;             // the cache holds 4-bit rows
+    int32_t attention_blocks; // set for the launch: workgroups before those that store rows
+    int32_t fold;             // (per KV head) those from here on go in reverse order
+    float scale_log2, lazy;
 };
 // Rows of a sequence's cache, read back.
 struct RowsArgs {
     const char* kpool;        // the sequence's, [Hkv][pool_rows][row of the cache]
     const char* vpool;
-    const uint8_t* kscale;
-    const uint8_t* vscale;
     char* k;                  // [n][Hkv][D]
     char* v;
     int32_t first, n, Hkv, pool_rows;
@@ -288,9 +286,9 @@ hipError_t launch_delay(int microseconds, hipStream_t s);
 hipError_t launch_monitor(const EntropyArgs* e, const VerdictArgs& v, hipStream_t s);
 // A prompt's rows into the head-major cache: k, v [n][Hkv][row] -> [Hkv][pool_rows][row].
 hipError_t launch_prefill(const PrefillArgs& a, hipStream_t s);
-// Packed prompts: their rows into the cache; their attention (launch_* fill in what
-// the comments above leave to the launch).
-hipError_t launch_prompt_store(const PromptArgs& a, const PromptBatch& b, bool four, hipStream_t s);
+// Packed prompts: their rows into the cache; the same with their attention, in one
+// launch (both fill in what the comments above leave to the launch).
+hipError_t launch_prompt_store(const PromptArgs& a, const PromptBatch& b, hipStream_t s);
 hipError_t launch_prompt_attention(const PromptArgs& a, const PromptBatch& b, int bf16, int head_dim, hipStream_t s);
 hipError_t launch_get_rows(const RowsArgs& a, bool four, hipStream_t s);
 

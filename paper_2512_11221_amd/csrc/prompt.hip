@@ -30,6 +30,7 @@ typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 typedef int intx4 __attribute__((ext_vector_type(4)));
 typedef unsigned uintx4 __attribute__((ext_vector_type(4)));
+typedef uintx4 word_aligned __attribute__((aligned(4)));      // in a 4-bit row
 typedef short shortx4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) shortx4* lds_shortx4;
 
@@ -50,14 +51,15 @@ __device__ __forceinline__ void unroll(F f) {
     }
 }
 
-// The sequence of the batch whose units (blocks, given by their first ones) hold unit x.
-__device__ __forceinline__ int find_sequence(const PromptBatch& b, int x) {
-    int lo = 0, hi = b.n - 1;                 // the last with first <= x
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (b.first[mid] <= x) lo = mid; else hi = mid - 1;
-    }
-    return lo;
+// The sequence of the batch whose units (given by their first ones) hold unit x: one
+// round trip to the table, a sequence per lane.
+__device__ __forceinline__ int find_sequence(const int32_t* first, int n, int x) {
+    const int lane = threadIdx.x & 63;
+    int before = 0;
+#pragma unroll
+    for (int i = 0; i < kPromptSeqs; i += 64)
+        before += __popcll(__ballot(i + lane < n && first[i + lane] <= x));
+    return before - 1;
 }
 
 // ---- the rows into the cache ----
@@ -68,11 +70,10 @@ constexpr int kStoreThreads = 256;
 // tokens of a sequence.  A thread moves 16 bytes of a K and of a V row, or rounds a
 // group of 32 values of each to 4 bits.
 template <bool FOUR>
-__global__ void __launch_bounds__(kStoreThreads)
-prompt_store_kernel(PromptArgs a, PromptBatch batch) {
-    const int i = find_sequence(batch, blockIdx.x);
+__device__ __forceinline__ void store_rows(const PromptArgs& a, const PromptBatch& batch, int unit) {
+    const int i = find_sequence(batch.first_store, batch.n, unit);
     const int n = batch.len[i], seq = batch.seq[i];
-    const int t0 = ((int)blockIdx.x - batch.first[i]) * kPromptStoreTokens;
+    const int t0 = (unit - batch.first_store[i]) * kPromptStoreTokens;
     const int nt = min(kPromptStoreTokens, n - t0);
     if (t0 == 0 && threadIdx.x == 0) a.plen[seq] = n;
     constexpr int kUnit = FOUR ? 64 : 16;     // bytes of a source row that a thread takes
@@ -81,14 +82,14 @@ prompt_store_kernel(PromptArgs a, PromptBatch batch) {
     const char* k = a.k + (size_t)(batch.start[i] + t0) * a.k_stride;
     const char* v = a.v + (size_t)(batch.start[i] + t0) * a.v_stride;
     const size_t row0 = (size_t)seq * a.Hkv * a.pool_rows + t0;
-    for (int u = threadIdx.x; u < nt * per_token; u += kStoreThreads) {
+    for (int u = threadIdx.x; u < nt * per_token; u += blockDim.x) {
         const int t = u >> token_shift, e = u & (per_token - 1);
         const int g = e >> head_shift, p = e & (per_head - 1);
         const size_t row = row0 + (size_t)g * a.pool_rows + t;
         const uintx4* ks = reinterpret_cast<const uintx4*>(k + (size_t)t * a.k_stride + e * kUnit);
         const uintx4* vs = reinterpret_cast<const uintx4*>(v + (size_t)t * a.v_stride + e * kUnit);
         if constexpr (FOUR) {
-            auto round = [&](const uintx4* s, char* pool, uint8_t* scales) __attribute__((always_inline)) {
+            auto round = [&](const uintx4* s, char* pool) __attribute__((always_inline)) {
                 uintx4 x[4], c;
                 uint32_t top = 0;
 #pragma unroll
@@ -100,17 +101,24 @@ prompt_store_kernel(PromptArgs a, PromptBatch batch) {
                 const float f = scale_value(byte);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) c[j] = encode8(x[j][0], x[j][1], x[j][2], x[j][3], f);
-                *reinterpret_cast<uintx4*>(pool + (row * per_head + p) * 16) = c;
-                scales[row * per_head + p] = (uint8_t)byte;
+                pool += row * four_row_bytes(a.head_bytes / 2);
+                *reinterpret_cast<word_aligned*>(pool + p * 16) = c;
+                pool[a.head_bytes / 4 + p] = (char)byte;
             };
-            round(ks, a.kpool, a.kscale);
-            round(vs, a.vpool, a.vscale);
+            round(ks, a.kpool);
+            round(vs, a.vpool);
         } else {
             const uintx4 x = *ks, y = *vs;
             *reinterpret_cast<uintx4*>(a.kpool + (row * per_head + p) * 16) = x;
             *reinterpret_cast<uintx4*>(a.vpool + (row * per_head + p) * 16) = y;
         }
     }
+}
+
+template <bool FOUR>
+__global__ void __launch_bounds__(kStoreThreads)
+prompt_store_kernel(PromptArgs a, PromptBatch batch) {
+    store_rows<FOUR>(a, batch, blockIdx.x);
 }
 
 // Rows first .. first + n - 1 of a sequence's cache as [n][Hkv][D].
@@ -124,43 +132,56 @@ rows_kernel(RowsArgs a) {
     for (int64_t u = (int64_t)blockIdx.x * kStoreThreads + threadIdx.x; u < total; u += (int64_t)gridDim.x * kStoreThreads) {
         const int t = (int)(u >> token_shift), e = (int)u & (per_token - 1);
         const int g = e >> head_shift, p = e & (per_head - 1);
-        const size_t unit = ((size_t)g * a.pool_rows + a.first + t) * per_head + p;
+        const size_t row = (size_t)g * a.pool_rows + a.first + t;
         if constexpr (FOUR) {
-            auto read = [&](const char* pool, const uint8_t* scales, char* to) __attribute__((always_inline)) {
-                const uintx4 c = *reinterpret_cast<const uintx4*>(pool + unit * 16);
-                const float f = scale_value(scales[unit]);
+            auto read = [&](const char* pool, char* to) __attribute__((always_inline)) {
+                pool += row * four_row_bytes(a.head_bytes / 2);
+                const uintx4 c = *reinterpret_cast<const word_aligned*>(pool + p * 16);
+                const float f = scale_value((uint8_t)pool[a.head_bytes / 4 + p]);
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
                     reinterpret_cast<uintx4*>(to + u * 64)[j] =
                         uintx4{decode2<0>(c[j], f), decode2<1>(c[j], f), decode2<2>(c[j], f), decode2<3>(c[j], f)};
             };
-            read(a.kpool, a.kscale, a.k);
-            read(a.vpool, a.vscale, a.v);
+            read(a.kpool, a.k);
+            read(a.vpool, a.v);
         } else {
-            *reinterpret_cast<uintx4*>(a.k + u * 16) = *reinterpret_cast<const uintx4*>(a.kpool + unit * 16);
-            *reinterpret_cast<uintx4*>(a.v + u * 16) = *reinterpret_cast<const uintx4*>(a.vpool + unit * 16);
+            *reinterpret_cast<uintx4*>(a.k + u * 16) = *reinterpret_cast<const uintx4*>(a.kpool + (row * per_head + p) * 16);
+            *reinterpret_cast<uintx4*>(a.v + u * 16) = *reinterpret_cast<const uintx4*>(a.vpool + (row * per_head + p) * 16);
         }
     }
 }
 
 // ---- attention ----
 
-template <bool BF16, int D, int WAVES>
+// How a workgroup goes about its rows.  kTeam: its waves take 32 rows each and share
+// the tiles of keys, two buffers of them behind a barrier a tile.  kSplit: its waves
+// take the same 32 rows and every WAVES-th tile each, without a barrier, and their
+// states are merged at the end.
+enum Walk { kTeam, kSplit };
+
+template <bool BF16, int D, int WAVES, Walk WALK>
 struct Tile {
+    static constexpr bool kSplits = WALK == kSplit;
     static constexpr int kElem = BF16 ? 2 : 4;
     static constexpr int kRow = D * kElem;                // bytes of a row of one head
-    static constexpr int kKeys = kRow <= 256 ? 64 : 32;   // keys of a tile
+    static constexpr int kKeys = kRow <= 256 && !kSplits ? 64 : 32;   // keys of a tile
     static constexpr int kKB = kKeys / 32;                // score blocks of 32 keys
-    static constexpr int kRows = WAVES * 32;              // query rows of a workgroup
-    static constexpr int kThreads = WAVES * 64;
+    static constexpr int kRows = kSplits ? 32 : WAVES * 32;           // query rows of a workgroup
+    static constexpr int kThreads = kSplits ? 64 : WAVES * 64;        // that load a tile
     // LDS row strides: 16 rows of a 16-byte piece (K), and 4 rows of 64 bytes (V, bf16) or
     // rows 4 apart of 128 bytes (V, fp32), meet no bank twice
     static constexpr int kKStride = kRow + 16;
     static constexpr int kVStride = kRow + (BF16 ? 64 : 32);
-    static constexpr int kKBuffer = kKeys * kKStride, kVBuffer = kKeys * kVStride;     // two of each
+    static constexpr int kKBuffer = kKeys * kKStride, kVBuffer = kKeys * kVStride;
+    static constexpr int kBuffers = kSplits ? 1 : 2;
+    static constexpr int kTiles = kBuffers * (kKBuffer + kVBuffer);   // of the workgroup, or of a wave
+    static constexpr int kLds = kTiles * (kSplits ? WAVES : 1);
     static constexpr int kLoads = kKeys * kRow / 16 / kThreads;   // 16-byte pieces of K (or V) per thread
     static constexpr int kQRegs = BF16 ? D / 16 : D / 8;  // 16-byte pieces of q per lane
+    static constexpr int kState = D + 4;                  // floats of a row of a wave's state
     static_assert(kLoads * kThreads * 16 == kKeys * kRow, "whole pieces per thread");
+    static_assert(!kSplits || 32 * kState * 4 <= kTiles, "a wave's state fits its tile");
 };
 
 // x with 0 in the place of infinities and NaNs; bad says whether there were any
@@ -186,18 +207,31 @@ __device__ __forceinline__ intx4 finite_part(intx4 x, bool& bad) {
 // number of tokens.
 constexpr float kLazy = 8.f;
 
-template <bool BF16, int D, int G, int WAVES>
-__global__ void __launch_bounds__(WAVES * 64, (D * (BF16 ? 1 : 2) > 128 ? 1 : 2))
+// waves of a SIMD that the registers leave room for
+constexpr int prompt_waves(bool bf16, int head_dim, int waves, Walk walk) {
+    const int row = head_dim * (bf16 ? 2 : 4);
+    return waves == 8 || row < 256 || (walk == kTeam && row == 256) ? 2 : 1;
+}
+
+template <bool BF16, int D, int G, int WAVES, Walk WALK>
+__global__ void __launch_bounds__(WAVES * 64, (prompt_waves(BF16, D, WAVES, WALK)))
 prompt_attention_kernel(PromptArgs a, PromptBatch batch) {
-    using T = Tile<BF16, D, WAVES>;
+    using T = Tile<BF16, D, WAVES, WALK>;
     constexpr int NL = T::kLoads, KB = T::kKB, NQ = T::kQRegs, DB = D / 32;
     constexpr int kPieces = T::kRow / 16;                 // pieces of a row
-    __shared__ __align__(16) char lds[2 * (T::kKBuffer + T::kVBuffer)];
+    __shared__ __align__(16) char lds[T::kLds];
     __shared__ int holds_infinite[2];                     // the tile whose V values are not all finite
+    __shared__ float ml_lds[T::kSplits ? WAVES * 2 * 32 : 1];
 
+    if ((int)blockIdx.x >= a.attention_blocks) {          // the rest of the grid fills the cache
+        if (a.four) store_rows<true>(a, batch, blockIdx.x - a.attention_blocks);
+        else store_rows<false>(a, batch, blockIdx.x - a.attention_blocks);
+        return;
+    }
     const int kvh = blockIdx.x % a.Hkv;
-    const int unit = blockIdx.x / a.Hkv;
-    const int si = find_sequence(batch, unit);
+    int unit = blockIdx.x / a.Hkv;
+    if (unit >= a.fold) unit = a.attention_blocks / a.Hkv - 1 - (unit - a.fold);
+    const int si = find_sequence(batch.first, batch.n, unit);
     const int n = batch.len[si];
     const int blocks = (n * G + T::kRows - 1) / T::kRows;
     const int block = blocks - 1 - (unit - batch.first[si]);      // the longest ones first
@@ -208,10 +242,13 @@ prompt_attention_kernel(PromptArgs a, PromptBatch batch) {
 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
-    const int row = r0 + wave * 32 + col;                 // the lane's query row
+    const int loader = T::kSplits ? lane : threadIdx.x;   // among those that load a tile
+    const int wr0 = T::kSplits ? r0 : r0 + wave * 32;
+    const int row = wr0 + col;                            // the lane's query row
     const int token = min(row / G, n - 1);                // rows past the end repeat the last token's
-    const int wave_first = (r0 + wave * 32) / G;
-    const int wave_last = min(n - 1, (r0 + wave * 32 + 31) / G);
+    const int wave_first = wr0 / G;
+    const int wave_last = min(n - 1, (wr0 + 31) / G);
+    char* tiles_lds = T::kSplits ? lds + wave * T::kTiles : lds;
 
     intx4 q[NQ];
     {
@@ -230,35 +267,36 @@ prompt_attention_kernel(PromptArgs a, PromptBatch batch) {
         const auto r = buffer(base + (size_t)j * T::kKeys * stride, left > 0 ? (int)((left - 1) * stride + T::kRow) : 0);
 #pragma unroll
         for (int u = 0; u < NL; ++u) {
-            const int i = threadIdx.x + u * T::kThreads;
+            const int i = loader + u * T::kThreads;
             x[u] = load16(r, (i / kPieces) * (int)stride + i % kPieces * 16);
         }
     };
     auto request_k = [&](int j) __attribute__((always_inline)) { request(k0, a.k_stride, j, kx); };
     auto request_v = [&](int j) __attribute__((always_inline)) { request(v0, a.v_stride, j, vx); };
     auto keep_k = [&](int j) __attribute__((always_inline)) {
-        char* to = lds + (j & 1) * T::kKBuffer;
+        char* to = tiles_lds + j % T::kBuffers * T::kKBuffer;
 #pragma unroll
         for (int u = 0; u < NL; ++u) {
-            const int i = threadIdx.x + u * T::kThreads;
+            const int i = loader + u * T::kThreads;
             *reinterpret_cast<intx4*>(to + i / kPieces * T::kKStride + i % kPieces * 16) = kx[u];
         }
     };
+    // whether some value of the caller's pieces was not finite
     auto keep_v = [&](int j) __attribute__((always_inline)) {
-        char* to = lds + 2 * T::kKBuffer + (j & 1) * T::kVBuffer;
+        char* to = tiles_lds + T::kBuffers * T::kKBuffer + j % T::kBuffers * T::kVBuffer;
+        bool bad = false;
         // Where a tile holds keys behind some query of the block, a weight of zero must not
         // meet an infinity or a NaN: those values are added on their own.
         if (j * T::kKeys + T::kKeys - 1 > first_token) {
-            bool bad = false;
 #pragma unroll
             for (int u = 0; u < NL; ++u) vx[u] = finite_part<BF16>(vx[u], bad);
-            if (bad) holds_infinite[j & 1] = j;
         }
 #pragma unroll
         for (int u = 0; u < NL; ++u) {
-            const int i = threadIdx.x + u * T::kThreads;
+            const int i = loader + u * T::kThreads;
             *reinterpret_cast<intx4*>(to + i / kPieces * T::kVStride + i % kPieces * 16) = vx[u];
         }
+        return bad;
     };
 
     float m = -INFINITY, l = 0.f;                         // of the lane's row (l: the lane's own keys)
@@ -269,7 +307,7 @@ prompt_attention_kernel(PromptArgs a, PromptBatch batch) {
         for (int i = 0; i < 16; ++i) acc[d][i] = 0.f;
 
     auto scores = [&](int j, floatx16 (&s)[KB]) __attribute__((always_inline)) {
-        const char* kt = lds + (j & 1) * T::kKBuffer;
+        const char* kt = tiles_lds + j % T::kBuffers * T::kKBuffer;
 #pragma unroll
         for (int i = 0; i < NQ; ++i)
 #pragma unroll
@@ -289,10 +327,10 @@ prompt_attention_kernel(PromptArgs a, PromptBatch batch) {
                 }
             }
     };
-    auto tile = [&](int j) __attribute__((always_inline)) {
+    auto tile = [&](int j, bool infinite) __attribute__((always_inline)) {
         floatx16 s[KB];
         scores(j, s);
-        const char* vt = lds + 2 * T::kKBuffer + (j & 1) * T::kVBuffer;
+        const char* vt = tiles_lds + T::kBuffers * T::kKBuffer + j % T::kBuffers * T::kVBuffer;
         // key of value i in block b: 32 b + 8 (i / 4) + 4 half + i % 4
         if (j * T::kKeys + T::kKeys - 1 > wave_first) {
             const int left = token - j * T::kKeys - half * 4;     // keys up to the lane's token, from its first
@@ -328,12 +366,17 @@ prompt_attention_kernel(PromptArgs a, PromptBatch batch) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 p[e] = __builtin_amdgcn_exp2f(fmaf(s[b / 2][b % 2 * 8 + e], a.scale_log2, bias));
-                l += p[e];
+                if constexpr (!BF16) l += p[e];
             }
             if constexpr (BF16) {
+                // the weights as the product takes them; their sums too, so that an output is an
+                // average under the weights it was formed with
                 bf16x8 w;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) w[e] = (__bf16)p[e];
+#pragma unroll
+                for (int e = 0; e < 8; e += 2)
+                    l = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{w[e], w[e + 1]}, bf16x2{(__bf16)1.f, (__bf16)1.f}, l, false);
 #pragma unroll
                 for (int d = 0; d < DB; ++d) {
                     const char* at = vb + b * 16 * T::kVStride + d * 64;
@@ -353,7 +396,7 @@ prompt_attention_kernel(PromptArgs a, PromptBatch batch) {
                 }
             }
         });
-        if (holds_infinite[j & 1] == j) {
+        if (infinite) {
             // the values that are not finite, from memory, to the queries that see their key
             // (whatever their weight)
             for (int key = j * T::kKeys; key <= min(wave_last, j * T::kKeys + T::kKeys - 1); ++key) {
@@ -371,61 +414,153 @@ prompt_attention_kernel(PromptArgs a, PromptBatch batch) {
             }
         }
     };
-    if (threadIdx.x < 2) holds_infinite[threadIdx.x] = -1;
-    request_k(0);
-    request_v(0);
-    __syncthreads();
-    keep_k(0);
-    keep_v(0);
-    request_k(1);
-    request_v(1);
-    for (int j = 0; j < tiles; ++j) {
-        __syncthreads();                                  // tile j is in place, tile j - 1 has been read
-        if (j + 1 < tiles) {
-            keep_k(j + 1);
-            keep_v(j + 1);
-            request_k(j + 2);
-            request_v(j + 2);
+    if constexpr (T::kSplits) {
+        request_k(wave);
+        request_v(wave);
+        for (int j = wave; j < tiles; j += WAVES) {
+            keep_k(j);
+            const bool infinite = __any(keep_v(j));
+            __builtin_amdgcn_wave_barrier();
+            request_k(j + WAVES);
+            request_v(j + WAVES);
+            tile(j, infinite);
+            __builtin_amdgcn_wave_barrier();
         }
-        if (j * T::kKeys <= wave_last) tile(j);           // else all of it lies behind the wave's queries
+    } else {
+        if (threadIdx.x < 2) holds_infinite[threadIdx.x] = -1;
+        request_k(0);
+        request_v(0);
+        __syncthreads();
+        keep_k(0);
+        if (keep_v(0)) holds_infinite[0] = 0;
+        request_k(1);
+        request_v(1);
+        for (int j = 0; j < tiles; ++j) {
+            __syncthreads();                              // tile j is in place, tile j - 1 has been read
+            if (j + 1 < tiles) {
+                keep_k(j + 1);
+                if (keep_v(j + 1)) holds_infinite[(j + 1) & 1] = j + 1;
+                request_k(j + 2);
+                request_v(j + 2);
+            }
+            // else all of it lies behind the wave's queries
+            if (j * T::kKeys <= wave_last) tile(j, holds_infinite[j & 1] == j);
+        }
     }
 
     const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
-    const float inv = 1.f / (__uint_as_float(x[0]) + __uint_as_float(x[1]));
-    if (row < n * G) {
-        char* o = a.out + ((size_t)(batch.start[si] + token) * a.Hq + kvh * G + row % G) * T::kRow;
+    l = __uint_as_float(x[0]) + __uint_as_float(x[1]);
+    const auto write = [&](int r, int dim, floatx4 o) __attribute__((always_inline)) {
+        if (r >= n * G) return;
+        char* to = a.out + ((size_t)(batch.start[si] + r / G) * a.Hq + kvh * G + r % G) * T::kRow + dim * T::kElem;
+        if constexpr (BF16) {
+            typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+            *reinterpret_cast<bf16x4*>(to) = __builtin_convertvector(o, bf16x4);
+        } else {
+            *reinterpret_cast<floatx4*>(to) = o;
+        }
+    };
+    if constexpr (!T::kSplits) {
+        const float inv = 1.f / l;
 #pragma unroll
         for (int d = 0; d < DB; ++d)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {                 // dims 32 d + 8 i + 4 half ..
-                const int dim = d * 32 + i * 8 + half * 4;
                 floatx4 r;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) r[e] = acc[d][i * 4 + e] * inv;
-                if constexpr (BF16) {
-                    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-                    *reinterpret_cast<bf16x4*>(o + dim * 2) = __builtin_convertvector(r, bf16x4);
-                } else {
-                    *reinterpret_cast<floatx4*>(o + dim * 4) = r;
-                }
+                write(row, d * 32 + i * 8 + half * 4, r);
             }
+    } else {
+        float* state = reinterpret_cast<float*>(tiles_lds);
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                *reinterpret_cast<floatx4*>(state + col * T::kState + d * 32 + i * 8 + half * 4) =
+                    floatx4{acc[d][i * 4], acc[d][i * 4 + 1], acc[d][i * 4 + 2], acc[d][i * 4 + 3]};
+        if (half == 0) {
+            ml_lds[wave * 64 + col] = m;
+            ml_lds[wave * 64 + 32 + col] = l;
+        }
+        __syncthreads();
+        for (int e = threadIdx.x; e < 32 * (D / 4); e += WAVES * 64) {
+            const int r = e / (D / 4), dim = e % (D / 4) * 4;
+            float M = -INFINITY;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) M = fmaxf(M, ml_lds[w * 64 + r]);
+            const float Mr = M == -INFINITY ? 0.f : M;    // waves without a tile weigh 0
+            float L = 0.f;
+            floatx4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) {
+                const float mw = ml_lds[w * 64 + r];
+                const float f = mw == M ? 1.f : __builtin_amdgcn_exp2f((mw - Mr) * a.scale_log2);
+                const floatx4 v = *reinterpret_cast<const floatx4*>(lds + w * T::kTiles + (r * T::kState + dim) * 4);
+                L = fmaf(f, ml_lds[w * 64 + 32 + r], L);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[i] = fmaf(f, v[i], o[i]);
+            }
+            const float inv = 1.f / L;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[i] *= inv;
+            write(r0 + r, dim, o);
+        }
     }
 }
 
-template <bool BF16, int D, int G>
-hipError_t launch_rows(const PromptArgs& a, PromptBatch& b, hipStream_t s) {
-    constexpr int kWaves = 4;
+int store_blocks(PromptBatch& b) {
+    int blocks = 0;
+    for (int i = 0; i < b.n; ++i) {
+        b.first_store[i] = blocks;
+        blocks += (b.len[i] + kPromptStoreTokens - 1) / kPromptStoreTokens;
+    }
+    return blocks;
+}
+
+template <bool BF16, int D, int G, int WAVES, Walk WALK>
+hipError_t launch_walk(PromptArgs& a, PromptBatch& b, hipStream_t s) {
+    using T = Tile<BF16, D, WAVES, WALK>;
     int blocks = 0;
     for (int i = 0; i < b.n; ++i) {
         b.first[i] = blocks;
-        blocks += (b.len[i] * G + kWaves * 32 - 1) / (kWaves * 32);
+        blocks += (b.len[i] * G + T::kRows - 1) / T::kRows;
     }
-    hipLaunchKernelGGL((prompt_attention_kernel<BF16, D, G, kWaves>), dim3(blocks * a.Hkv), dim3(kWaves * 64), 0, s, a, b);
+    a.attention_blocks = blocks * a.Hkv;
+    // The longest blocks come first.  Where every CU gets two workgroups at once, the second
+    // half goes the other way, so that a CU's two are a long and a short one (two prompts of
+    // 1024, 32/8 heads of 128: 42 us without, 35 with).
+    constexpr int kCUs = 256;
+    a.fold = WALK == kTeam && WAVES == 4 && a.attention_blocks > kCUs && a.attention_blocks <= 2 * kCUs ? blocks / 2 : blocks;
+    const int grid = a.attention_blocks + store_blocks(b);
+    hipLaunchKernelGGL((prompt_attention_kernel<BF16, D, G, WAVES, WALK>), dim3(grid), dim3(WAVES * 64), 0, s, a, b);
     return hipGetLastError();
 }
 
+// Which walk, by the launch's work: units of 32 rows of a KV head.
+//  kSplit  with so few units that they leave compute units idle, a unit's keys are split
+//          over four waves.  bf16 rows of 128 up to 256 units (1024 tokens of 8/8 heads:
+//          17.2 us against 26.4; 512 units, 512 tokens of 32/8: 20.2 against 17.5), rows
+//          of 64, two workgroups a CU, up to 1024 (2048 tokens of 16/2: 23.9 against
+//          31.2); fp32 rows, whose products take 16 times as long, up to 1024 (700 tokens
+//          of 32/8: 71 against 105 us; 2000: 378 against 311).  Rows of 256 bf16 have no
+//          registers left for it.
+//  kTeam   four waves until every CU has its eight at least twice over, then eight, which
+//          read a tile once for 256 rows (2048 tokens of 32/8: 62 us with four, 68 with
+//          eight; 4096: 188 and 176; four prompts of 1000 to 4000, 16/8 heads of 256: 433
+//          and 341).
+template <bool BF16, int D, int G>
+hipError_t launch_rows(PromptArgs& a, PromptBatch& b, hipStream_t s) {
+    int64_t units = 0;
+    for (int i = 0; i < b.n; ++i) units += ((int64_t)b.len[i] * G + 31) / 32 * a.Hkv;
+    if constexpr (!BF16 || D < 256)
+        if (units <= (BF16 && D == 128 ? 256 : 1024)) return launch_walk<BF16, D, G, 4, kSplit>(a, b, s);
+    if (units < 4096) return launch_walk<BF16, D, G, 4, kTeam>(a, b, s);
+    return launch_walk<BF16, D, G, 8, kTeam>(a, b, s);
+}
+
 template <bool BF16, int D>
-hipError_t launch_group(const PromptArgs& a, PromptBatch& b, int group, hipStream_t s) {
+hipError_t launch_group(PromptArgs& a, PromptBatch& b, int group, hipStream_t s) {
     switch (group) {
         case 1: return launch_rows<BF16, D, 1>(a, b, s);
         case 2: return launch_rows<BF16, D, 2>(a, b, s);
@@ -454,14 +589,10 @@ hipError_t launch_prompt_attention(const PromptArgs& a, const PromptBatch& batch
     return hipErrorInvalidValue;
 }
 
-hipError_t launch_prompt_store(const PromptArgs& a, const PromptBatch& batch, bool four, hipStream_t s) {
+hipError_t launch_prompt_store(const PromptArgs& a, const PromptBatch& batch, hipStream_t s) {
     PromptBatch b = batch;
-    int blocks = 0;
-    for (int i = 0; i < b.n; ++i) {
-        b.first[i] = blocks;
-        blocks += (b.len[i] + kPromptStoreTokens - 1) / kPromptStoreTokens;
-    }
-    if (four) hipLaunchKernelGGL(prompt_store_kernel<true>, dim3(blocks), dim3(kStoreThreads), 0, s, a, b);
+    const int blocks = store_blocks(b);
+    if (a.four) hipLaunchKernelGGL(prompt_store_kernel<true>, dim3(blocks), dim3(kStoreThreads), 0, s, a, b);
     else hipLaunchKernelGGL(prompt_store_kernel<false>, dim3(blocks), dim3(kStoreThreads), 0, s, a, b);
     return hipGetLastError();
 }
