@@ -30,7 +30,6 @@ typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 typedef int intx4 __attribute__((ext_vector_type(4)));
 typedef unsigned uintx4 __attribute__((ext_vector_type(4)));
-typedef uintx4 word_aligned __attribute__((aligned(4)));      // in a 4-bit row
 typedef short shortx4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) shortx4* lds_shortx4;
 
@@ -66,9 +65,29 @@ __device__ __forceinline__ int find_sequence(const int32_t* first, int n, int x)
 
 constexpr int kStoreThreads = 256;
 
+// Eight values of a row, whose group's others the lane's three neighbours hold, as
+// codes, and (lanes at the start of a row's 16, or of rows of 64 values at the start of
+// its 8) the scale bytes of those lanes' groups.
+__device__ __forceinline__ uint32_t round8(uintx4 x, bool rows_of_64, uint32_t& scales) {
+    uint32_t top = max_magnitude(max_magnitude(x[0], x[1]), max_magnitude(x[2], x[3]));
+    top = max(top & 0xFFFFu, top >> 16);
+    top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0xB1, 0xF, 0xF, false));   // quad_perm [1,0,3,2]
+    top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0x4E, 0xF, 0xF, false));   // quad_perm [2,3,0,1]
+    const uint32_t byte = scale_byte(top);
+    scales = byte << (threadIdx.x / 4 & (rows_of_64 ? 1 : 3)) * 8;
+    if (rows_of_64) {
+        scales |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)scales, 0x141, 0xF, 0xF, false);     // row_half_mirror
+    } else {
+        scales |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)scales, 0x124, 0xF, 0xF, false);     // row_ror 4
+        scales |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)scales, 0x128, 0xF, 0xF, false);     // row_ror 8
+    }
+    return encode8(x[0], x[1], x[2], x[3], scale_value(byte));
+}
+
 // Packed rows [T][Hkv][D] into the head-major cache, a workgroup per kPromptStoreTokens
-// tokens of a sequence.  A thread moves 16 bytes of a K and of a V row, or rounds a
-// group of 32 values of each to 4 bits.
+// tokens of a sequence.  A thread takes 16 bytes of K and of V at a time, several in
+// flight; four neighbouring threads have a group of 32 values (a thread with a whole
+// group took 148 us where this takes 127, for 8 x 16k tokens of 8 heads of 128, 0.68 GB).
 template <bool FOUR>
 __device__ __forceinline__ void store_rows(const PromptArgs& a, const PromptBatch& batch, int unit) {
     const int i = find_sequence(batch.first_store, batch.n, unit);
@@ -76,41 +95,47 @@ __device__ __forceinline__ void store_rows(const PromptArgs& a, const PromptBatc
     const int t0 = (unit - batch.first_store[i]) * kPromptStoreTokens;
     const int nt = min(kPromptStoreTokens, n - t0);
     if (t0 == 0 && threadIdx.x == 0) a.plen[seq] = n;
-    constexpr int kUnit = FOUR ? 64 : 16;     // bytes of a source row that a thread takes
-    const int per_head = a.head_bytes / kUnit, per_token = per_head * a.Hkv;      // powers of two
+    const int per_head = a.head_bytes / 16, per_token = per_head * a.Hkv;     // powers of two
     const int head_shift = __ffs(per_head) - 1, token_shift = __ffs(per_token) - 1;
+    const int pool_bytes = FOUR ? four_row_bytes(a.head_bytes / 2) : a.head_bytes;
     const char* k = a.k + (size_t)(batch.start[i] + t0) * a.k_stride;
     const char* v = a.v + (size_t)(batch.start[i] + t0) * a.v_stride;
     const size_t row0 = (size_t)seq * a.Hkv * a.pool_rows + t0;
-    for (int u = threadIdx.x; u < nt * per_token; u += blockDim.x) {
-        const int t = u >> token_shift, e = u & (per_token - 1);
-        const int g = e >> head_shift, p = e & (per_head - 1);
-        const size_t row = row0 + (size_t)g * a.pool_rows + t;
-        const uintx4* ks = reinterpret_cast<const uintx4*>(k + (size_t)t * a.k_stride + e * kUnit);
-        const uintx4* vs = reinterpret_cast<const uintx4*>(v + (size_t)t * a.v_stride + e * kUnit);
-        if constexpr (FOUR) {
-            auto round = [&](const uintx4* s, char* pool) __attribute__((always_inline)) {
-                uintx4 x[4], c;
-                uint32_t top = 0;
+    const int total = nt * per_token;
+    constexpr int kFlight = 4;
+    for (int u0 = threadIdx.x; u0 < total; u0 += kFlight * blockDim.x) {
+        uintx4 x[kFlight], y[kFlight];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) x[j] = s[j];
+        for (int f = 0; f < kFlight; ++f) {
+            const int u = u0 + f * blockDim.x, t = u >> token_shift, e = u & (per_token - 1);
+            if (u < total) {
+                x[f] = __builtin_nontemporal_load(reinterpret_cast<const uintx4*>(k + (size_t)t * a.k_stride + e * 16));
+                y[f] = __builtin_nontemporal_load(reinterpret_cast<const uintx4*>(v + (size_t)t * a.v_stride + e * 16));
+            }
+        }
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    top = max_magnitude(top, max_magnitude(max_magnitude(x[j][0], x[j][1]), max_magnitude(x[j][2], x[j][3])));
-                const uint32_t byte = scale_byte(max(top & 0xFFFFu, top >> 16));
-                const float f = scale_value(byte);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) c[j] = encode8(x[j][0], x[j][1], x[j][2], x[j][3], f);
-                pool += row * four_row_bytes(a.head_bytes / 2);
-                *reinterpret_cast<word_aligned*>(pool + p * 16) = c;
-                pool[a.head_bytes / 4 + p] = (char)byte;
-            };
-            round(ks, a.kpool);
-            round(vs, a.vpool);
-        } else {
-            const uintx4 x = *ks, y = *vs;
-            *reinterpret_cast<uintx4*>(a.kpool + (row * per_head + p) * 16) = x;
-            *reinterpret_cast<uintx4*>(a.vpool + (row * per_head + p) * 16) = y;
+        for (int f = 0; f < kFlight; ++f) {
+            const int u = u0 + f * blockDim.x, t = u >> token_shift, e = u & (per_token - 1);
+            if (u >= total) continue;
+            const int g = e >> head_shift, p = e & (per_head - 1);
+            const size_t at = (row0 + (size_t)g * a.pool_rows + t) * pool_bytes;
+            if constexpr (FOUR) {
+                const bool of_64 = per_head == 8;
+                uint32_t ks, vs;
+                *reinterpret_cast<uint32_t*>(a.kpool + at + p * 4) = round8(x[f], of_64, ks);
+                *reinterpret_cast<uint32_t*>(a.vpool + at + p * 4) = round8(y[f], of_64, vs);
+                const size_t to = at + per_head * 4 + p / 4;          // the first of the lanes' groups
+                if (of_64 && p == 0) {
+                    *reinterpret_cast<uint16_t*>(a.kpool + to) = (uint16_t)ks;
+                    *reinterpret_cast<uint16_t*>(a.vpool + to) = (uint16_t)vs;
+                } else if (!of_64 && p % 16 == 0) {
+                    *reinterpret_cast<uint32_t*>(a.kpool + to) = ks;
+                    *reinterpret_cast<uint32_t*>(a.vpool + to) = vs;
+                }
+            } else {
+                *reinterpret_cast<uintx4*>(a.kpool + at + p * 16) = x[f];
+                *reinterpret_cast<uintx4*>(a.vpool + at + p * 16) = y[f];
+            }
         }
     }
 }
@@ -121,33 +146,49 @@ prompt_store_kernel(PromptArgs a, PromptBatch batch) {
     store_rows<FOUR>(a, batch, blockIdx.x);
 }
 
-// Rows first .. first + n - 1 of a sequence's cache as [n][Hkv][D].
+// Rows first .. first + n - 1 of a sequence's cache as [n][Hkv][D], 16 bytes of K and
+// of V to a thread at a time, several in flight.
 template <bool FOUR>
 __global__ void __launch_bounds__(kStoreThreads)
 rows_kernel(RowsArgs a) {
-    constexpr int kUnit = FOUR ? 64 : 16;     // bytes of an output row that a thread writes
-    const int per_head = a.head_bytes / kUnit, per_token = per_head * a.Hkv;
+    const int per_head = a.head_bytes / 16, per_token = per_head * a.Hkv;
     const int head_shift = __ffs(per_head) - 1, token_shift = __ffs(per_token) - 1;
-    const int64_t total = (int64_t)a.n << token_shift;
-    for (int64_t u = (int64_t)blockIdx.x * kStoreThreads + threadIdx.x; u < total; u += (int64_t)gridDim.x * kStoreThreads) {
-        const int t = (int)(u >> token_shift), e = (int)u & (per_token - 1);
-        const int g = e >> head_shift, p = e & (per_head - 1);
-        const size_t row = (size_t)g * a.pool_rows + a.first + t;
-        if constexpr (FOUR) {
-            auto read = [&](const char* pool, char* to) __attribute__((always_inline)) {
-                pool += row * four_row_bytes(a.head_bytes / 2);
-                const uintx4 c = *reinterpret_cast<const word_aligned*>(pool + p * 16);
-                const float f = scale_value((uint8_t)pool[a.head_bytes / 4 + p]);
+    const int pool_bytes = FOUR ? four_row_bytes(a.head_bytes / 2) : a.head_bytes;
+    const int64_t total = (int64_t)a.n << token_shift, step = (int64_t)gridDim.x * kStoreThreads;
+    constexpr int kFlight = 4;
+    typedef std::conditional_t<FOUR, uint32_t, uintx4> Piece;
+    for (int64_t u0 = (int64_t)blockIdx.x * kStoreThreads + threadIdx.x; u0 < total; u0 += kFlight * step) {
+        Piece x[kFlight], y[kFlight];
+        uint8_t xs[kFlight], ys[kFlight];
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    reinterpret_cast<uintx4*>(to + u * 64)[j] =
-                        uintx4{decode2<0>(c[j], f), decode2<1>(c[j], f), decode2<2>(c[j], f), decode2<3>(c[j], f)};
-            };
-            read(a.kpool, a.k);
-            read(a.vpool, a.v);
-        } else {
-            *reinterpret_cast<uintx4*>(a.k + u * 16) = *reinterpret_cast<const uintx4*>(a.kpool + (row * per_head + p) * 16);
-            *reinterpret_cast<uintx4*>(a.v + u * 16) = *reinterpret_cast<const uintx4*>(a.vpool + (row * per_head + p) * 16);
+        for (int f = 0; f < kFlight; ++f) {
+            const int64_t u = u0 + f * step;
+            if (u >= total) continue;
+            const int t = (int)(u >> token_shift), e = (int)u & (per_token - 1);
+            const int g = e >> head_shift, p = e & (per_head - 1);
+            const size_t at = ((size_t)g * a.pool_rows + a.first + t) * pool_bytes;
+            x[f] = *reinterpret_cast<const Piece*>(a.kpool + at + p * sizeof(Piece));
+            y[f] = *reinterpret_cast<const Piece*>(a.vpool + at + p * sizeof(Piece));
+            if constexpr (FOUR) {
+                xs[f] = (uint8_t)a.kpool[at + per_head * 4 + p / 4];
+                ys[f] = (uint8_t)a.vpool[at + per_head * 4 + p / 4];
+            }
+        }
+#pragma unroll
+        for (int f = 0; f < kFlight; ++f) {
+            const int64_t u = u0 + f * step;
+            if (u >= total) continue;
+            uintx4 k, v;
+            if constexpr (FOUR) {
+                const float kf = scale_value(xs[f]), vf = scale_value(ys[f]);
+                k = uintx4{decode2<0>(x[f], kf), decode2<1>(x[f], kf), decode2<2>(x[f], kf), decode2<3>(x[f], kf)};
+                v = uintx4{decode2<0>(y[f], vf), decode2<1>(y[f], vf), decode2<2>(y[f], vf), decode2<3>(y[f], vf)};
+            } else {
+                k = x[f];
+                v = y[f];
+            }
+            __builtin_nontemporal_store(k, reinterpret_cast<uintx4*>(a.k + u * 16));
+            __builtin_nontemporal_store(v, reinterpret_cast<uintx4*>(a.v + u * 16));
         }
     }
 }
@@ -598,9 +639,9 @@ hipError_t launch_prompt_store(const PromptArgs& a, const PromptBatch& batch, hi
 }
 
 hipError_t launch_get_rows(const RowsArgs& a, bool four, hipStream_t s) {
-    const int64_t units = (int64_t)a.n * a.Hkv * a.head_bytes / (four ? 64 : 16);
-    const int64_t blocks = (units + kStoreThreads - 1) / kStoreThreads;
-    const dim3 grid((unsigned)(blocks < 4096 ? blocks : 4096));
+    const int64_t units = (int64_t)a.n * a.Hkv * a.head_bytes / 16;
+    const int64_t blocks = (units + 4 * kStoreThreads - 1) / (4 * kStoreThreads);
+    const dim3 grid((unsigned)(blocks < 2048 ? blocks : 2048));
     if (four) hipLaunchKernelGGL(rows_kernel<true>, grid, dim3(kStoreThreads), 0, s, a);
     else hipLaunchKernelGGL(rows_kernel<false>, grid, dim3(kStoreThreads), 0, s, a);
     return hipGetLastError();
