@@ -6,6 +6,7 @@ status codes to exceptions.  torch is used for device memory and streams.
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import math
 import os
@@ -195,9 +196,8 @@ def asrkf_prefill_packed(ctx, layer, seqs, n_tokens, q, k, v, out, stream=None):
     if len(n_tokens) != n:
         raise ValueError(f"{n} sequences, {len(n_tokens)} lengths")
     _dense("out", out)
-    a = (ctypes.c_int32 * n)(*seqs)
-    b = (ctypes.c_int32 * n)(*n_tokens)
-    _check(load().asrkf_prefill_packed(ctx, layer, n, a, b, _ptr(q), _token_stride("q", q), _ptr(k),
+    a, b = array.array("i", seqs), array.array("i", n_tokens)
+    _check(load().asrkf_prefill_packed(ctx, layer, n, a.buffer_info()[0], b.buffer_info()[0], _ptr(q), _token_stride("q", q), _ptr(k),
                                        _token_stride("k", k), _ptr(v), _token_stride("v", v), _ptr(out),
                                        _stream(stream)))
 
