@@ -34,6 +34,8 @@ def parse():
     ap.add_argument("--workload", choices=sorted(WORKLOADS), default="32layer")
     ap.add_argument("--cpu-seconds", type=float, default=15.0,
                     help="budget of the oracle sample (0 disables the cpu_baseline leg)")
+    ap.add_argument("--kv-bits", type=int, choices=[0, 4], default=0,
+                    help="4: the cache holds K and V in 4 bits (default 0: in the workload's type)")
     ap.add_argument("--relevance", choices=["abs", "softmax"], default=None,
                     help="relevance reading (default: the workload's, Eq. 2 |q.k|)")
     ap.add_argument("--scope", choices=["layer", "token"], default=None,
@@ -331,7 +333,7 @@ def main():
                         entropy_spike=w.entropy_spike, conf_drop=w.conf_drop,
                         wr_last_N=w.wr_last_N, dtype=w.dtype, spill_min_D=w.spill_min_D,
                         history_W=w.history_W, relevance=w.relevance, scope=w.scope,
-                        candidates=w.candidates)
+                        candidates=w.candidates, kv_bits=args.kv_bits)
     dg = DeviceGen(w)
     S = W + K
     Q = torch.empty((S, L, B, Hq, D), dtype=tdt, device="cuda")
@@ -438,11 +440,13 @@ def main():
 
     attended = st["attended_total"]
     bytes_per_token = w.kv_bytes_per_token()          # K + V of one token, one layer
+    if args.kv_bits == 4:                             # codes and scales
+        bytes_per_token = 2 * Hkv * (D // 2 + D // 32)
     algo_bytes = bytes_per_token * attended + 4 * w.vocab * B * K
     attn_s = st_timed["attn_kernel_ms"] / 1e3
     achieved = bytes_per_token * attended / attn_s / 1e9
     default_path = (w.relevance == "abs" and w.scope == "layer" and not w.history_W
-                    and not w.spill_min_D and w.candidates == "outside")
+                    and not w.spill_min_D and w.candidates == "outside" and not args.kv_bits)
     ratio = measured_traffic(w.name) if default_path else None
     launches = max(1, st_timed["attn_launches"])
     traffic = ratio[0] * bytes_per_token * attended / launches if ratio else None
@@ -471,7 +475,7 @@ def main():
                    "head_dim": D, "window_K": w.window_K, "tau": w.tau, "k": w.k_soft,
                    "vocab": w.vocab, "mode": "spill" if w.spill_min_D else "resident",
                    "relevance": w.relevance, "scope": w.scope, "history_W": w.history_W,
-                   "candidates": w.candidates},
+                   "candidates": w.candidates, **({"kv_bits": args.kv_bits} if args.kv_bits else {})},
         "decode_steps_per_s": K / elapsed,
         "hbm_fraction_step": algo_bytes / elapsed / 1e9 / PEAK_HBM_GBS,
         "attended_fraction": attended / max(1, sum(p + t for p in w.prefill
@@ -486,7 +490,7 @@ def main():
                                        f"({ratio[1].get('layers', 'all')} layer(s), "
                                        f"{ratio[1].get('steps')} timed steps), times this run's "
                                        f"algorithmic bytes per launch") if ratio else None,
-                     "kernel": f"attention_kernel<{w.dtype}, D={D}, G={Hq // Hkv}, Hkv={Hkv}>",
+                     "kernel": f"attention_kernel<{'4-bit' if args.kv_bits else w.dtype}, D={D}, G={Hq // Hkv}, Hkv={Hkv}>",
                      "algorithmic_unit": f"{bytes_per_token} B per attended token-layer (K + V rows)",
                      "launches": st_timed["attn_launches"],
                      "avg_launch_us": 1e3 * st_timed["attn_kernel_ms"] / max(1, st_timed["attn_launches"]),
@@ -497,7 +501,8 @@ def main():
                                "inside the loop"},
     }
     line["roofline"].update(regimes(w, W, K, series, bytes_per_token))
-    line["metadata"] = metadata_bytes(w, W, K, attended, algo_bytes, traffic, line["roofline"])
+    if not args.kv_bits:
+        line["metadata"] = metadata_bytes(w, W, K, attended, algo_bytes, traffic, line["roofline"])
     if w.spill_min_D:
         row = bytes_per_token // 2                      # one K or V row
         line["spill"] = {"spill_min_D": w.spill_min_D, "rows_to_host": st["rows_to_host"],

@@ -148,8 +148,7 @@ typedef struct {
                                 for what lies above); a group with an infinity or a NaN reads
                                 as NaN.  Rows are rounded when they enter the cache, and every
                                 step attends to what the codes stand for, the new token's own
-                                row too.  A row of D values takes D / 2 + D / 32 bytes
-                                (of 64 values: 36) */
+                                row too.  A row of D values takes D / 2 + D / 32 bytes */
 } asrkf_config;
 
 typedef struct {

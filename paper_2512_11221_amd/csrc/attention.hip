@@ -244,7 +244,7 @@ struct Row {
     static constexpr bool kFour = ROWS == kRowsFour;
     static constexpr int kElem = ROWS == kRowsF32 ? 4 : 2;
     static constexpr int kBytes = D * kElem;              // one token, one KV head, of the arguments and in LDS
-    static constexpr int kPoolBytes = kFour ? four_row_bytes(D) : kBytes;     // the same in the cache
+    static constexpr int kPoolBytes = kFour ? D / 2 : kBytes;     // the same in the cache
     static constexpr int kLanes = kBytes / 16;            // lanes per row in a load
     // tokens per tile: 16 KB of K and V rows, in a wave's registers while they travel
     // (4-bit rows: 64, or 32 of 256 values)
@@ -550,6 +550,8 @@ attention_kernel(AttnArgs a) {
             f.list = rl;
             f.k = rk;
             f.v = rv;
+            f.ks = buffer(a.kscale + pool_row0 * R::kScales, a.pool_rows * R::kScales);
+            f.vs = buffer(a.vscale + pool_row0 * R::kScales, a.pool_rows * R::kScales);
             const int row = b * a.Hkv + g;        // of the new token's rows, and of the queries' heads
             f.begin(a, t0 + wt, t0, row, pool_row0);
             for (int c0 = t0, kept = 0;; kept = 0) {

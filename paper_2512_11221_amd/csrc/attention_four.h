@@ -23,8 +23,10 @@
 // instruction); K's codes pass through LDS into the rows that the lanes hold, V's
 // values as bf16, 32 tokens at a time, into transposed reads.
 //
-// Dense launches over 8 sequences of 32k, 8 KV heads of 128, four query heads each:
-// repeated columns @@.
+// Dense launches over 8 sequences of 32k, 8 KV heads of 128, four query heads each (285 MB):
+// 79.4 us with repeated columns and the 16-bit rows' layouts, 71.8 with several tokens a
+// tile, 64.6 with non-temporal loads of the scales too; the arithmetic alone takes 58, the
+// loads alone 53 to 62, and two waves a SIMD overlap them that far.
 
 // A group of 32 values as codes, with its scale byte.
 __device__ __forceinline__ void encode_group(const intx4 (&x)[4], intx4& codes, uint32_t& byte) {
@@ -97,9 +99,9 @@ struct FourStream {
     char* lds;
     float* rel_kept;
     float scale_log2;
-    __amdgpu_buffer_rsrc_t list, k, v;
+    __amdgpu_buffer_rsrc_t list, k, v, ks, vs;
 
-    int next_rows, t_new;
+    int next_rows, next_scale_rows, t_new;
     bool owns_new;
     FourTile<D> kx, vx;
     intx4 k_new, v_new;
@@ -111,7 +113,8 @@ struct FourStream {
     __device__ __forceinline__ char* queries() const { return v_scales() + kTile * R::kScales; }
 
     // The list entry that a lane holds, among a tile's: row lane / kScales of load
-    // lane % NL, so that the lanes of a row have what they need in every load.
+    // lane % NL, so that the lanes of a row have what they need in every load; and
+    // entry `lane`, for the scales, which a load takes in the list's order.
     __device__ __forceinline__ int entry() const { return R::kFourRows * (lane % NL) + lane / R::kScales; }
     template <int J>
     __device__ __forceinline__ int from_entry(int x) const {
@@ -120,29 +123,31 @@ struct FourStream {
     __device__ __forceinline__ int rows(int t) const {
         return __builtin_amdgcn_raw_buffer_load_b32(list, t < t1 ? (t * kTile + entry()) * 4 : kNowhere, 0, 0);
     }
-    // a device has fewer than 2^24 rows of a head
-    __device__ static __forceinline__ int row_at(int row) { return (int)__umul24(row, R::kPoolBytes); }
+    __device__ __forceinline__ int scale_rows(int t) const {
+        return __builtin_amdgcn_raw_buffer_load_b32(list, t < t1 ? (t * kTile + lane) * 4 : kNowhere, 0, 0);
+    }
     // the list's last entry is the new token: its row comes from the arguments
-    __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t r, int t, int row, FourTile<D>& x) const {
+    __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t r, __amdgpu_buffer_rsrc_t rs, int t, int row, int scale_row, FourTile<D>& x) const {
         const int lim = t < t1 ? n - 1 - t * kTile : 0;
         __builtin_amdgcn_sched_barrier(0);
         unroll<NL>([&](auto J) __attribute__((always_inline)) {
             constexpr int j = decltype(J)::value;
-            const int o = row_at(from_entry<j>(row)) + lane % R::kScales * 16;
+            const int o = from_entry<j>(row) * R::kPoolBytes + lane % R::kScales * 16;
             x.codes[j] = load16<kStreamPolicy>(r, j * R::kFourRows + lane / R::kScales < lim ? o : kNowhere);
         });
-        const int so = entry() < lim ? row_at(row) + D / 2 : kNowhere;
-        if constexpr (D == 64) x.scale[0] = __builtin_amdgcn_raw_buffer_load_b16(r, so, 0, kStreamPolicy);
-        else if constexpr (D == 128) x.scale[0] = __builtin_amdgcn_raw_buffer_load_b32(r, so, 0, kStreamPolicy);
+        const int so = lane < lim && lane < kTile ? scale_row * R::kScales : kNowhere;
+        if constexpr (D == 64) x.scale[0] = __builtin_amdgcn_raw_buffer_load_b16(rs, so, 0, kStreamPolicy);
+        else if constexpr (D == 128) x.scale[0] = __builtin_amdgcn_raw_buffer_load_b32(rs, so, 0, kStreamPolicy);
         else {
-            const uintx2 w = __builtin_bit_cast(uintx2, __builtin_amdgcn_raw_buffer_load_b64(r, so, 0, kStreamPolicy));
+            const uintx2 w = __builtin_bit_cast(uintx2, __builtin_amdgcn_raw_buffer_load_b64(rs, so, 0, kStreamPolicy));
             x.scale[0] = w[0];
             x.scale[1] = w[1];
         }
         __builtin_amdgcn_sched_barrier(0);
     }
     __device__ __forceinline__ void keep_scales(char* to, const FourTile<D>& x) const {
-        to += entry() * R::kScales;
+        if (lane >= kTile) return;
+        to += lane * R::kScales;
         if constexpr (D == 64) *reinterpret_cast<uint16_t*>(to) = (uint16_t)x.scale[0];
         else if constexpr (D == 128) *reinterpret_cast<uint32_t*>(to) = x.scale[0];
         else *reinterpret_cast<uintx2*>(to) = uintx2{x.scale[0], x.scale[1]};
@@ -160,7 +165,7 @@ struct FourStream {
         t = first;
         t_new = (n - 1) / kTile;
         owns_new = t_new >= first && t_new < t1 && (t_new - first) % step == 0;
-        const int now = rows(t);
+        const int now = rows(t), scales_now = scale_rows(t);
         constexpr int kQ = G * D / 8;                     // 16-byte pieces of the queries
         const auto rq = buffer((const char*)a.q + (size_t)row * G * R::kBytes, G * R::kBytes);
         intx4 qx[(kQ + 63) / 64];
@@ -175,8 +180,9 @@ struct FourStream {
         }
         const int new_row = __builtin_amdgcn_raw_buffer_load_b32(list, owns_new ? (n - 1) * 4 : kNowhere, 0, 0);
         next_rows = rows(t + step);
-        load(k, t, now, kx);
-        load(v, t, now, vx);
+        next_scale_rows = scale_rows(t + step);
+        load(k, ks, t, now, scales_now, kx);
+        load(v, vs, t, now, scales_now, vx);
 #pragma unroll
         for (int i = 0; i < (kQ + 63) / 64; ++i) {
             const int e = i * 64 + lane;
@@ -192,16 +198,11 @@ struct FourStream {
             encode_group(kn, k_new, k_byte);
             encode_group(vn, v_new, v_byte);
             if (lane < R::kScales) {                      // the append
-                const size_t at = (pool_row0 + new_row) * R::kPoolBytes;
-                char* kr = (char*)a.kpool_w + at;
-                char* vr = (char*)a.vpool_w + at;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    *reinterpret_cast<int*>(kr + lane * 16 + e * 4) = k_new[e];
-                    *reinterpret_cast<int*>(vr + lane * 16 + e * 4) = v_new[e];
-                }
-                kr[D / 2 + lane] = (char)k_byte;
-                vr[D / 2 + lane] = (char)v_byte;
+                const size_t at = (pool_row0 + new_row) * R::kScales + lane;
+                *reinterpret_cast<intx4*>((char*)a.kpool_w + at * 16) = k_new;
+                *reinterpret_cast<intx4*>((char*)a.vpool_w + at * 16) = v_new;
+                a.kscale_w[at] = (uint8_t)k_byte;
+                a.vscale_w[at] = (uint8_t)v_byte;
             }
         }
     }
@@ -272,8 +273,10 @@ struct FourStream {
         }
         __builtin_amdgcn_wave_barrier();
         const int row = next_rows;
+        const int scale_row = next_scale_rows;
         next_rows = rows(t + 2 * step);
-        load(k, t + step, row, kx);
+        next_scale_rows = scale_rows(t + 2 * step);
+        load(k, ks, t + step, row, scale_row, kx);
 
         floatx4 s[kC];
 #pragma unroll
@@ -391,7 +394,7 @@ struct FourStream {
             constexpr int j = decltype(J)::value;
             __builtin_amdgcn_wave_barrier();
             keep_values<j>();
-            if constexpr (j == kTile / R::kSpan - 1) load(v, t + step, row, vx);
+            if constexpr (j == kTile / R::kSpan - 1) load(v, vs, t + step, row, scale_row, vx);
             __builtin_amdgcn_wave_barrier();
             if constexpr (R::kSpan == 16) {
                 const shortx4 w = __builtin_bit_cast(shortx4, intx2{weights(j, 0), weights(j, 1)});

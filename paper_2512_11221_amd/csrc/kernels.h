@@ -56,6 +56,10 @@ struct AttnArgs {
     const void* vnew;
     void* kpool_w;            // same as kpool, writable (append)
     void* vpool_w;
+    const uint8_t* kscale;    // 4-bit rows: layer base, [B][Hkv][pool_rows][D / 32], else null
+    const uint8_t* vscale;
+    uint8_t* kscale_w;        // the same, writable (append)
+    uint8_t* vscale_w;
     const int32_t* list;      // layer base, [B][cap] ascending positions
     const int32_t* list_row;  // layer base, [B][cap] device row of each listed position
                               // (spill mode only; in resident mode the row is the position)
@@ -212,6 +216,8 @@ struct PromptArgs {
     int64_t q_stride, k_stride, v_stride;
     char* kpool;              // layer base, [B][Hkv][pool_rows][row of the cache]
     char* vpool;
+    uint8_t* kscale;          // 4-bit rows: layer base, [B][Hkv][pool_rows][D / 32]
+    uint8_t* vscale;
     int32_t* plen;            // [B] prompt lengths (written)
     int32_t Hq, Hkv, pool_rows;
     int32_t head_bytes;       // one token, one KV head, of k and v
@@ -224,6 +230,8 @@ struct PromptArgs {
 struct RowsArgs {
     const char* kpool;        // the sequence's, [Hkv][pool_rows][row of the cache]
     const char* vpool;
+    const uint8_t* kscale;
+    const uint8_t* vscale;
     char* k;                  // [n][Hkv][D]
     char* v;
     int32_t first, n, Hkv, pool_rows;

@@ -97,7 +97,7 @@ __device__ __forceinline__ void store_rows(const PromptArgs& a, const PromptBatc
     if (t0 == 0 && threadIdx.x == 0) a.plen[seq] = n;
     const int per_head = a.head_bytes / 16, per_token = per_head * a.Hkv;     // powers of two
     const int head_shift = __ffs(per_head) - 1, token_shift = __ffs(per_token) - 1;
-    const int pool_bytes = FOUR ? four_row_bytes(a.head_bytes / 2) : a.head_bytes;
+    const int pool_bytes = FOUR ? a.head_bytes / 4 : a.head_bytes;
     const char* k = a.k + (size_t)(batch.start[i] + t0) * a.k_stride;
     const char* v = a.v + (size_t)(batch.start[i] + t0) * a.v_stride;
     const size_t row0 = (size_t)seq * a.Hkv * a.pool_rows + t0;
@@ -118,19 +118,19 @@ __device__ __forceinline__ void store_rows(const PromptArgs& a, const PromptBatc
             const int u = u0 + f * blockDim.x, t = u >> token_shift, e = u & (per_token - 1);
             if (u >= total) continue;
             const int g = e >> head_shift, p = e & (per_head - 1);
-            const size_t at = (row0 + (size_t)g * a.pool_rows + t) * pool_bytes;
+            const size_t row = row0 + (size_t)g * a.pool_rows + t, at = row * pool_bytes;
             if constexpr (FOUR) {
                 const bool of_64 = per_head == 8;
                 uint32_t ks, vs;
                 *reinterpret_cast<uint32_t*>(a.kpool + at + p * 4) = round8(x[f], of_64, ks);
                 *reinterpret_cast<uint32_t*>(a.vpool + at + p * 4) = round8(y[f], of_64, vs);
-                const size_t to = at + per_head * 4 + p / 4;          // the first of the lanes' groups
+                const size_t to = (row * per_head + p) / 4;           // the first of the lanes' groups
                 if (of_64 && p == 0) {
-                    *reinterpret_cast<uint16_t*>(a.kpool + to) = (uint16_t)ks;
-                    *reinterpret_cast<uint16_t*>(a.vpool + to) = (uint16_t)vs;
+                    *reinterpret_cast<uint16_t*>(a.kscale + to) = (uint16_t)ks;
+                    *reinterpret_cast<uint16_t*>(a.vscale + to) = (uint16_t)vs;
                 } else if (!of_64 && p % 16 == 0) {
-                    *reinterpret_cast<uint32_t*>(a.kpool + to) = ks;
-                    *reinterpret_cast<uint32_t*>(a.vpool + to) = vs;
+                    *reinterpret_cast<uint32_t*>(a.kscale + to) = ks;
+                    *reinterpret_cast<uint32_t*>(a.vscale + to) = vs;
                 }
             } else {
                 *reinterpret_cast<uintx4*>(a.kpool + at + p * 16) = x[f];
@@ -153,7 +153,7 @@ __global__ void __launch_bounds__(kStoreThreads)
 rows_kernel(RowsArgs a) {
     const int per_head = a.head_bytes / 16, per_token = per_head * a.Hkv;
     const int head_shift = __ffs(per_head) - 1, token_shift = __ffs(per_token) - 1;
-    const int pool_bytes = FOUR ? four_row_bytes(a.head_bytes / 2) : a.head_bytes;
+    const int pool_bytes = FOUR ? a.head_bytes / 4 : a.head_bytes;
     const int64_t total = (int64_t)a.n << token_shift, step = (int64_t)gridDim.x * kStoreThreads;
     constexpr int kFlight = 4;
     typedef std::conditional_t<FOUR, uint32_t, uintx4> Piece;
@@ -166,12 +166,12 @@ rows_kernel(RowsArgs a) {
             if (u >= total) continue;
             const int t = (int)(u >> token_shift), e = (int)u & (per_token - 1);
             const int g = e >> head_shift, p = e & (per_head - 1);
-            const size_t at = ((size_t)g * a.pool_rows + a.first + t) * pool_bytes;
+            const size_t row = (size_t)g * a.pool_rows + a.first + t, at = row * pool_bytes;
             x[f] = *reinterpret_cast<const Piece*>(a.kpool + at + p * sizeof(Piece));
             y[f] = *reinterpret_cast<const Piece*>(a.vpool + at + p * sizeof(Piece));
             if constexpr (FOUR) {
-                xs[f] = (uint8_t)a.kpool[at + per_head * 4 + p / 4];
-                ys[f] = (uint8_t)a.vpool[at + per_head * 4 + p / 4];
+                xs[f] = a.kscale[(row * per_head + p) / 4];
+                ys[f] = a.vscale[(row * per_head + p) / 4];
             }
         }
 #pragma unroll

@@ -11,10 +11,10 @@
 // computed from them is as exact as from bf16 rows.
 //
 // A row of one KV head is D / 2 bytes of codes (value 2 i in the low half of byte i),
-// so that 16 bytes are one group, and behind them its D / 32 scale bytes, filled up
-// to a word.  Scales in an array of their own, 4 bytes a row, cost the attention's
-// loads a seventh of their time for a sixteenth of the bytes (8 x 32k tokens, 8 KV
-// heads of 128, loads alone: 61.9 us a launch, 52.6 without the scales).
+// so that 16 bytes are one group; the D / 32 scale bytes stand in an array of their
+// own, row by row.  Behind the codes, in rows of 68 bytes (D = 128), they spare a dense
+// launch a second stream (8 x 32k tokens, 8 KV heads: 66.3 us against 67.4), but the
+// rows of a list with gaps then straddle lines: 47.6 us against 38.4 where 35 % attend.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -23,10 +23,6 @@
 namespace asrkf {
 
 constexpr int kScaleGroup = 32;
-
-__host__ __device__ constexpr int four_row_bytes(int head_dim) {
-    return head_dim / 2 + (head_dim / kScaleGroup < 4 ? 4 : head_dim / kScaleGroup);
-}
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef unsigned short ushortx2 __attribute__((ext_vector_type(2)));

@@ -2,7 +2,8 @@
 //
 // HBM layout of a context (cap = max_ctx + 1 rounded up to 64 positions;
 // pool_rows = cap in resident mode, the configured device rows in spill mode):
-//   K, V cache      [L][B][Hkv][pool_rows][D]   dtype   head-major rows (or 4-bit ones, rows.h)
+//   K, V cache      [L][B][Hkv][pool_rows][D]   dtype   head-major rows (or 4-bit codes, rows.h)
+//   K, V scales     [L][B][Hkv][pool_rows][D/32] uint8  4-bit rows only
 //   unfreeze U      [L][B][cap]           int32   token attends at step t iff U <= t
 //   count c         [L][B][cap]           int32   low-relevance detections (Eq. 3)
 //   score flag      [L][B][cap]           uint8   s_j < tau at the current step (Eq. 2)
@@ -108,6 +109,7 @@ struct asrkf_ctx {
     int group = 0;
     size_t esz = 0;
     size_t row_bytes = 0;        // one token, all KV heads, in the cache
+    size_t scale_bytes = 0;      // the same, scale bytes of 4-bit rows (else 0)
     bool four = false;           // rows held in 4 bits
     int grid = 0;                // attention grid (resident workgroups)
     int heads_per_group = 1;     // KV heads a workgroup takes together (set for each step)
@@ -117,6 +119,8 @@ struct asrkf_ctx {
     // device memory
     void* kpool = nullptr;
     void* vpool = nullptr;
+    uint8_t* kscale = nullptr;      // 4-bit rows
+    uint8_t* vscale = nullptr;
     int32_t* unfreeze = nullptr;
     int32_t* count = nullptr;
     uint8_t* flag = nullptr;
@@ -243,7 +247,7 @@ asrkf_status dev_alloc(asrkf_ctx* ctx, T** p, size_t bytes) {
 }
 
 void free_all(asrkf_ctx* ctx) {
-    void* ptrs[] = {ctx->kpool, ctx->vpool, ctx->unfreeze, ctx->count, ctx->flag, ctx->list, ctx->small,
+    void* ptrs[] = {ctx->kpool, ctx->vpool, ctx->kscale, ctx->vscale, ctx->unfreeze, ctx->count, ctx->flag, ctx->list, ctx->small,
                     ctx->part_acc, ctx->rel, ctx->rel_sum, ctx->row_of, ctx->on_host, ctx->list_row, ctx->last_row,
                     ctx->row_owner, ctx->pop_buf, ctx->out_pos, ctx->out_row, ctx->in_pos, ctx->in_row,
                     ctx->hmask, ctx->hlast, ctx->seg_count};
@@ -409,6 +413,10 @@ PromptArgs prompt_args(const asrkf_ctx* ctx, int layer) {
     const size_t rows = (size_t)layer * c.batch * ctx->pool_rows;
     p.kpool = static_cast<char*>(ctx->kpool) + rows * ctx->row_bytes;
     p.vpool = static_cast<char*>(ctx->vpool) + rows * ctx->row_bytes;
+    if (ctx->four) {
+        p.kscale = ctx->kscale + rows * ctx->scale_bytes;
+        p.vscale = ctx->vscale + rows * ctx->scale_bytes;
+    }
     p.plen = ctx->plen;
     p.Hq = c.n_q_heads;
     p.Hkv = c.n_kv_heads;
@@ -445,7 +453,8 @@ asrkf_status asrkf_init(const asrkf_config* cfg, asrkf_ctx** out) {
     ctx->group = c.n_q_heads / c.n_kv_heads;
     ctx->esz = c.dtype == ASRKF_BF16 ? 2 : 4;
     ctx->four = c.kv_bits == 4;
-    ctx->row_bytes = (size_t)c.n_kv_heads * (ctx->four ? four_row_bytes(c.head_dim) : c.head_dim * ctx->esz);
+    ctx->row_bytes = (size_t)c.n_kv_heads * (ctx->four ? c.head_dim / 2 : c.head_dim * ctx->esz);
+    ctx->scale_bytes = ctx->four ? (size_t)c.n_kv_heads * c.head_dim / kScaleGroup : 0;
     ctx->plen_host.assign(c.batch, 0);
     ctx->prefilled.assign(c.batch, 0);
 
@@ -498,6 +507,10 @@ asrkf_status asrkf_init(const asrkf_config* cfg, asrkf_ctx** out) {
     const size_t pool_bytes = inst * ctx->pool_rows * ctx->row_bytes;
     ALLOC(kpool, pool_bytes);
     ALLOC(vpool, pool_bytes);
+    if (ctx->four) {
+        ALLOC(kscale, inst * ctx->pool_rows * ctx->scale_bytes);
+        ALLOC(vscale, inst * ctx->pool_rows * ctx->scale_bytes);
+    }
     ALLOC(unfreeze, st_pos * 4);
     ALLOC(count, st_pos * 4);
     ALLOC(flag, st_pos);
@@ -816,6 +829,10 @@ asrkf_status asrkf_get_rows(asrkf_ctx* ctx, int32_t layer, int32_t seq, int32_t 
     RowsArgs r{};
     r.kpool = p.kpool + rows * ctx->row_bytes;
     r.vpool = p.vpool + rows * ctx->row_bytes;
+    if (ctx->four) {
+        r.kscale = p.kscale + rows * ctx->scale_bytes;
+        r.vscale = p.vscale + rows * ctx->scale_bytes;
+    }
     r.k = static_cast<char*>(k);
     r.v = static_cast<char*>(v);
     r.first = first;
@@ -1055,6 +1072,11 @@ asrkf_status decode_step_impl(asrkf_ctx* ctx, int32_t layer, const void* q, cons
     a.vpool = (const char*)ctx->vpool + pool_off;
     a.kpool_w = (char*)ctx->kpool + pool_off;
     a.vpool_w = (char*)ctx->vpool + pool_off;
+    if (ctx->four) {
+        const size_t scale_off = inst0 * ctx->pool_rows * ctx->scale_bytes;
+        a.kscale = a.kscale_w = ctx->kscale + scale_off;
+        a.vscale = a.vscale_w = ctx->vscale + scale_off;
+    }
     a.q = q;
     a.knew = k_new;
     a.vnew = v_new;

@@ -6,7 +6,8 @@ VALUES = np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])
 
 def rounded(x):
     """The values that the codes of x stand for; groups of 32 along the last axis."""
-    x = np.asarray(x, dtype=np.float64)
+    with np.errstate(invalid="ignore"):
+        x = np.asarray(x, dtype=np.float64)
     g = x.reshape(-1, 32)
     out = np.empty_like(g)
     bad = ~np.isfinite(g).all(axis=1)

@@ -224,6 +224,56 @@ def test_decode_large_batches_and_splits():
     _run(_workload(batch=1, prefill=[6000], steps=3, f_hh=[0.3], head_dim=128, n_q_heads=8, n_kv_heads=2), with_logits=False)
 
 
+def _long_step(lens, Hq, Hkv, D, tau, relevance):
+    """One step over long lists against 64 bits on the GPU, from the rows as they are held: the
+    outputs, and which tokens are found low (those whose score lies clear of tau)."""
+    import torch
+    B, G, top = len(lens), Hq // Hkv, max(lens)
+    import paper_2512_11221_amd as A
+    ctx = A.asrkf_init(A.make_config(1, B, Hq, Hkv, D, top + 2, 16, tau, 1.0, 32, relevance=relevance, kv_bits=4))
+    try:
+        g = torch.Generator(device="cuda")
+        g.manual_seed(11)
+        rnd = lambda *s: torch.randn(s, generator=g, device="cuda", dtype=torch.bfloat16)   # noqa: E731
+        T = sum(lens)
+        A.asrkf_prefill_packed(ctx, 0, range(B), lens, None, rnd(T, Hkv, D), rnd(T, Hkv, D), None)
+        q, out = rnd(B, Hq, D), torch.empty((B, Hq, D), device="cuda")
+        A.asrkf_decode_step(ctx, 0, q, rnd(B, Hkv, D), rnd(B, Hkv, D), out)
+        A.asrkf_restore(ctx, None, A.NONE)
+        for b, n in enumerate(lens):
+            k, v = (torch.empty((n + 1, Hkv, D), device="cuda", dtype=torch.bfloat16) for _ in range(2))
+            A.asrkf_get_rows(ctx, 0, b, 0, n + 1, k, v)
+            K, V = k.double().permute(1, 2, 0).contiguous(), v.double().transpose(0, 1).contiguous()
+            x = torch.matmul(q[b].double().view(Hkv, G, D), K)
+            p = torch.softmax(x / math.sqrt(D), -1)
+            ref, size = torch.matmul(p, V).view(Hq, D), torch.matmul(p, V.abs()).view(Hq, D)
+            # scores in fp32 (D 2^-24 of sum |q k| <= 8 D here, over sqrt(D)), twice; sums of n weights
+            rel = 2 * D * 2.0 ** -24 * 8 * math.sqrt(D) + 2 * n * 2.0 ** -24 + 2.0 ** -21
+            assert ((out[b].double() - ref).abs() <= rel * size).all()
+            s = (x.abs() if relevance == "abs" else p).sum((0, 1)) / Hq
+            low = (s < tau)[: n + 1 - 16].cpu().numpy()
+            clear = ((s - tau).abs() > tau * rel)[: n + 1 - 16].cpu().numpy()
+            st = A.asrkf_get_state(ctx, 0, b, top + 2)
+            # the check says something: the band left out, 2 rel tau wide (rel <= 3e-3 and tau <= 13:
+            # 0.08), holds a small share of scores that spread over several units (softmax: 2 rel
+            # of the weights)
+            assert n < 1000 or clear.mean() > 0.9 and 0 < low.mean() < 1
+            np.testing.assert_array_equal((st["count"][: n + 1 - 16] == 1)[clear], low[clear])
+            assert (st["count"][n + 1 - 16:] == 0).all()
+    finally:
+        A.asrkf_destroy(ctx)
+
+
+@pytest.mark.parametrize("lens,Hq,Hkv,D,tau,relevance", [
+    ([20000, 9000], 8, 2, 128, 8.0, "abs"),             # many workgroups share a pair
+    ([33000] * 8 + [1, 700], 16, 8, 64, 6.3, "abs"),    # every wave a head of its own: the relevance room is emptied on the way
+    ([33000] * 4, 32, 8, 64, 4e-5, "softmax"),          # a plane per query head: the room holds a quarter of the tiles
+    ([17000] * 5, 16, 8, 256, 12.7, "abs"),
+], ids=["shared", "heads", "softmax", "rows256"])
+def test_long_lists(lens, Hq, Hkv, D, tau, relevance):
+    _long_step(lens, Hq, Hkv, D, tau, relevance)
+
+
 def test_static_entry_graph_and_repeat_are_bitwise_the_same():
     import torch
     A, ctx = _init(2, 8, 2, 128, 600)
