@@ -208,6 +208,8 @@ struct FourStream {
     }
 
     // C tile c of the scores: value i is token 32 c + 16 p + 4 q4 + i under the lane's column.
+    // A row of A holds a token of every part, so that a NaN would reach the others' scores
+    // through their zeros in B: a token with one is computed without and set to NaN behind.
     __device__ __forceinline__ floatx4 scores(int c) const {
         const int c16 = lane & 15, q4 = lane >> 4;
         const int token = kParts == 4 ? lane : c * 32 + (q4 >> 1) * 16 + c16;
@@ -222,6 +224,14 @@ struct FourStream {
             sc[0] = w[0];
             sc[1] = w[1];
         }
+        uint32_t none = 0;                                // nonzero: some scale byte is 255
+#pragma unroll
+        for (int i = 0; i < (kPieces + 3) / 4; ++i) none |= (~sc[i] - 0x01010101u) & sc[i] & 0x80808080u;
+        const uint64_t nans = __ballot(none != 0);        // (lanes of the tokens)
+        if (nans && none) {
+#pragma unroll
+            for (int i = 0; i < (kPieces + 3) / 4; ++i) sc[i] = 0x7F7F7F7Fu;
+        }
         floatx4 sum[2] = {};
 #pragma unroll
         for (int e = 0; e < kPieces; ++e) {
@@ -235,7 +245,15 @@ struct FourStream {
                     __builtin_bit_cast(bf16x8, decode8(x[w], f)), __builtin_bit_cast(bf16x8, b), sum[w % 2], 0, 0, 0);
             }
         }
-        return sum[0] + sum[1];
+        floatx4 r = sum[0] + sum[1];
+        if (nans) {
+            // four parts: a lane to a token; two: lanes c16 and 16 + c16 of each half have halves of one
+            const int first = c16 / GC * (kParts == 4 ? 16 : 32) + q4 * 4;
+            const uint64_t of = (kParts == 4 ? nans : nans | nans >> 16) >> first;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) r[i] = of >> i & 1 ? __builtin_nanf("") : r[i];
+        }
+        return r;
     }
 
     // V's rows kSpan J .. of the tile, codes -> LDS as bf16

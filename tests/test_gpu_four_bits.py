@@ -342,6 +342,42 @@ def test_groups_that_are_not_finite_read_as_nan():
         A.asrkf_destroy(ctx)
 
 
+@pytest.mark.parametrize("Hq,Hkv,D", [(2, 2, 64), (8, 2, 64), (16, 2, 64), (8, 2, 128), (16, 2, 128), (8, 2, 256)])
+def test_keys_that_are_not_finite_leave_other_tokens_scores(Hq, Hkv, D):
+    """Eq. 2 scores are each token's own.  Under a threshold above all of them every token outside
+    the window is detected but those whose key holds a NaN, as with bf16 rows of the same values."""
+    import torch
+    import paper_2512_11221_amd as A
+    n, K = 200, 4
+    g = torch.Generator(device="cuda")
+    g.manual_seed(D)
+    k, v = (torch.randn((n, Hkv, D), generator=g, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    bad = (0, 37, 90, 133)
+    for i, p in enumerate(bad):
+        k[p, i % Hkv, i * 11 % D] = (math.nan, math.inf, -math.inf, math.nan)[i]
+    q = torch.randn((1, Hq, D), generator=g, device="cuda", dtype=torch.bfloat16)
+    out = torch.empty((1, Hq, D), device="cuda")
+    counts = []
+    rows = k, v
+    for bits in (4, 0):
+        ctx = A.asrkf_init(A.make_config(1, 1, Hq, Hkv, D, n + 8, K, 1e9, 2.0, 32, kv_bits=bits))
+        try:
+            A.asrkf_prefill_packed(ctx, 0, [0], [n], None, *rows, None)
+            if bits:
+                rows = torch.empty_like(k), torch.empty_like(v)
+                A.asrkf_get_rows(ctx, 0, 0, 0, n, *rows)
+            A.asrkf_decode_step(ctx, 0, q, k[50:51].contiguous(), v[50:51].contiguous(), out)
+            A.asrkf_restore(ctx, None, A.NONE)
+            counts.append(A.asrkf_get_state(ctx, 0, 0, n + 8)["count"])
+        finally:
+            torch.cuda.synchronize()
+            A.asrkf_destroy(ctx)
+    np.testing.assert_array_equal(counts[0], counts[1])
+    want = np.ones(n - 2 * K, np.int32)               # well before the window
+    want[list(bad)] = 0
+    np.testing.assert_array_equal(counts[0][:n - 2 * K], want)
+
+
 def test_refusals():
     import torch
     A, ctx = _init(1, 8, 2, 64, 64)
