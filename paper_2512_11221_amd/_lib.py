@@ -175,10 +175,12 @@ def asrkf_prefill(ctx, layer, seq, k, v, n_tokens, stream=None):
 def _token_stride(name, x):
     """Elements from one token to the next of packed rows [T][heads][dim]: a tensor's
     own stride where it has three dimensions (a slice of a fused projection), else 0
-    (dense).  The rows of a token must be dense."""
+    (dense).  The rows of a token must be dense, and tokens may not share memory."""
     if x is None or not hasattr(x, "stride"):
         return 0
     if x.dim() == 3 and x.shape[0] > 1 and x.stride(2) == 1 and x.stride(1) == x.shape[2]:
+        if x.stride(0) < x.shape[1] * x.shape[2]:
+            raise ValueError(f"{name}: tokens overlap")
         return x.stride(0)
     if not x.is_contiguous():
         raise ValueError(f"{name}: the heads of a token must be dense rows")

@@ -34,6 +34,16 @@ def test_binding_takes_token_strides_and_refuses_other_layouts():
             f("q", bad)
 
 
+def test_binding_refuses_tokens_that_share_memory():
+    """An expanded tensor's token stride of 0 is not the 0 that stands for dense rows."""
+    import torch
+    x = torch.zeros((1, 2, 64)).expand(7, 2, 64)
+    y = torch.zeros(4096).as_strided((7, 2, 64), (64, 64, 1))
+    for bad in (x, y):
+        with pytest.raises(ValueError):
+            A._lib._token_stride("k", bad)
+
+
 def test_four_bit_reference():
     """The reference itself: its values are its own, X is the smallest that the rule allows, and
     no value is off by more than X."""
