@@ -212,6 +212,7 @@ asrkf_status asrkf_prefill(asrkf_ctx* ctx, int32_t layer, int32_t seq,
  *             a prompt's outputs go into the next product in that type.  Sums
  *             and softmax statistics are held in fp32; bf16 contexts round the
  *             softmax weights to bf16 for the product with v.
+ * Without tokens (T = 0) no pointer to them is looked at.
  * The attention is over k and v as given, also where the cache holds 4 bits.  A
  * value of v that is not finite reaches the tokens from its own on.  All
  * pointers 16-byte aligned, in memory of the context's device (EINVAL

@@ -724,7 +724,7 @@ asrkf_status asrkf_prefill_packed(asrkf_ctx* ctx, int32_t layer, int32_t n_seqs,
         return fail(ASRKF_ESTATE, "prefill after the first decode step");
     if (layer < 0 || layer >= c.n_layers) return fail(ASRKF_EINVAL, "layer out of range");
     if (n_seqs < 1 || n_seqs > c.batch) return fail(ASRKF_EINVAL, "n_seqs must be in 1..%d", c.batch);
-    if (!seqs || !n_tokens || !k || !v) return fail(ASRKF_EINVAL, "null argument");
+    if (!seqs || !n_tokens) return fail(ASRKF_EINVAL, "null argument");
     if (!q != !out) return fail(ASRKF_EINVAL, "q and out go together");
     st = on_device(ctx);
     if (st != ASRKF_OK) return st;
@@ -743,6 +743,7 @@ asrkf_status asrkf_prefill_packed(asrkf_ctx* ctx, int32_t layer, int32_t n_seqs,
                         ctx->plen_host[seq]);
         total += n;
     }
+    if (total > 0 && (!k || !v)) return fail(ASRKF_EINVAL, "null k or v");
     if (total >= ((int64_t)1 << 31)) return fail(ASRKF_EINVAL, "%lld packed tokens", (long long)total);
     PromptArgs p = prompt_args(ctx, layer);
     struct Packed { const char* name; const void* p; int64_t stride; int heads; int64_t* bytes; };

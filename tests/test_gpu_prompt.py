@@ -419,6 +419,22 @@ def test_refusals():
         A.asrkf_destroy(ctx)
 
 
+def test_prompts_that_are_all_empty():
+    """Empty tensors have null pointers; the sequences then have no prompt, as if never named."""
+    import torch
+    A, ctx = _init(2, 8, 2, 64, "bf16", 64)
+    try:
+        q, k = (torch.empty((0, h, 64), device="cuda", dtype=torch.bfloat16) for h in (8, 2))
+        A.asrkf_prefill_packed(ctx, 0, [1, 0], [0, 0], q, k, k, torch.empty_like(q))
+        A.asrkf_prefill_packed(ctx, 0, [0, 1], [0, 0], None, None, None, None)
+        qn, kn = (torch.randn((2, h, 64), device="cuda").to(torch.bfloat16) for h in (8, 2))
+        out = torch.empty((2, 8, 64), device="cuda")
+        A.asrkf_decode_step(ctx, 0, qn, kn, kn, out)
+        assert torch.equal(out, kn.float().repeat_interleave(4, 1))
+    finally:
+        A.asrkf_destroy(ctx)
+
+
 def test_rows_are_refused_in_spill_mode_and_prompts_are_not():
     import torch
     A, ctx = _init(1, 8, 2, 64, "bf16", 64, spill_min_D=2, device_rows=30)
