@@ -216,7 +216,8 @@ asrkf_status asrkf_prefill(asrkf_ctx* ctx, int32_t layer, int32_t seq,
  * The attention is over k and v as given, also where the cache holds 4 bits.  A
  * value of v that is not finite reaches the tokens from its own on.  All
  * pointers 16-byte aligned, in memory of the context's device (EINVAL
- * otherwise, or where they reach past the end of an allocation).  Only before
+ * otherwise, or where they reach past the end of an allocation, or where out
+ * overlaps q, k or v).  Only before
  * the first decode step (else ESTATE).  Asynchronous; the host arrays may be
  * reused on return. */
 asrkf_status asrkf_prefill_packed(asrkf_ctx* ctx, int32_t layer, int32_t n_seqs,
@@ -228,7 +229,8 @@ asrkf_status asrkf_prefill_packed(asrkf_ctx* ctx, int32_t layer, int32_t n_seqs,
  * export; also a prompt's rows to keep elsewhere): positions first .. first +
  * n - 1 of the n_t that the host knows of.  With 4-bit rows the values that
  * the codes stand for, which enter such a cache again unchanged.
- *   k, v: device, [n][n_kv_heads][head_dim] of cfg.dtype, 16-byte aligned (written)
+ *   k, v: device, [n][n_kv_heads][head_dim] of cfg.dtype, 16-byte aligned (written;
+ *         EINVAL where they overlap)
  * ESTATE in spill mode.  Asynchronous. */
 asrkf_status asrkf_get_rows(asrkf_ctx* ctx, int32_t layer, int32_t seq, int32_t first, int32_t n,
                             void* k, void* v, void* stream);

@@ -406,6 +406,11 @@ asrkf_status on_device(const asrkf_ctx* ctx) {
     return ASRKF_OK;
 }
 
+bool overlap(const void* p, size_t p_bytes, const void* q, size_t q_bytes) {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+    return a < b + q_bytes && b < a + p_bytes;
+}
+
 // What a launch over packed prompts of a layer takes from the context.
 PromptArgs prompt_args(const asrkf_ctx* ctx, int layer) {
     const asrkf_config& c = ctx->cfg;
@@ -767,6 +772,9 @@ asrkf_status asrkf_prefill_packed(asrkf_ctx* ctx, int32_t layer, int32_t n_seqs,
         if (!kernel_readable(ctx, x.p, bytes, &inside))
             return fail(ASRKF_EINVAL, "%s must be in memory of the context's device", x.name);
         if (!inside) return fail(ASRKF_EINVAL, "%s is smaller than %lld tokens", x.name, (long long)total);
+        // out is written while other workgroups still read (x.bytes: q, k and v)
+        if (out && x.bytes && overlap(x.p, bytes, out, (size_t)total * c.n_q_heads * p.head_bytes))
+            return fail(ASRKF_EINVAL, "out overlaps %s", x.name);
     }
     p.q = static_cast<const char*>(q);
     p.k = static_cast<const char*>(k);
@@ -817,6 +825,7 @@ asrkf_status asrkf_get_rows(asrkf_ctx* ctx, int32_t layer, int32_t seq, int32_t 
     st = on_device(ctx);
     if (st != ASRKF_OK) return st;
     const size_t bytes = (size_t)n * c.n_kv_heads * c.head_dim * ctx->esz;
+    if (overlap(k, bytes, v, bytes)) return fail(ASRKF_EINVAL, "k overlaps v");
     for (const void* x : {(const void*)k, (const void*)v}) {
         bool inside;
         if (!kernel_readable(ctx, x, bytes, &inside))

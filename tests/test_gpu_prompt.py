@@ -435,6 +435,28 @@ def test_prompts_that_are_all_empty():
         A.asrkf_destroy(ctx)
 
 
+def test_outputs_over_inputs_are_refused():
+    import torch
+    n = 20
+    A, ctx = _init(1, 2, 2, 64, "bf16", 64)
+    try:
+        x = torch.zeros((5 * n, 2, 64), dtype=torch.bfloat16, device="cuda")
+        q, k, v, out = (x[i * n:(i + 1) * n] for i in range(4))
+        for args in ((q, k, v, q), (q, k, v, k), (q, k, v, v), (q, k, v, x[n - 1:2 * n - 1]), (q, k, v, x[3 * n - 1:])):
+            with pytest.raises(A.AsrkfError) as e:
+                A.asrkf_prefill_packed(ctx, 0, [0], [n], *args)
+            assert e.value.code == A._lib.EINVAL and "overlaps" in A.asrkf_last_error()
+        A.asrkf_prefill_packed(ctx, 0, [0], [n], q, k, v, out)              # side by side
+        A.asrkf_prefill_packed(ctx, 0, [0], [n], q, q, q, out)              # inputs may be the same
+        for a, b in ((k, k), (k, x[2 * n - 1:3 * n - 1])):
+            with pytest.raises(A.AsrkfError) as e:
+                A.asrkf_get_rows(ctx, 0, 0, 0, n, a, b)
+            assert e.value.code == A._lib.EINVAL
+        A.asrkf_get_rows(ctx, 0, 0, 0, n, k, v)
+    finally:
+        A.asrkf_destroy(ctx)
+
+
 def test_rows_are_refused_in_spill_mode_and_prompts_are_not():
     import torch
     A, ctx = _init(1, 8, 2, 64, "bf16", 64, spill_min_D=2, device_rows=30)
