@@ -399,6 +399,11 @@ void mark_queued(asrkf_ctx* ctx, hipStream_t s, bool capture) {
 // 64 tokens stay below 2 GiB.
 constexpr int64_t kMaxTokenStride = (int64_t)16 << 20;
 
+// Tokens of a launch over several packed prompts, at most: its workgroups of 512 threads,
+// one for 256 query rows and one for 16 tokens' store, then stay below the 2^32 threads
+// of a grid.  (A sequence has below 2^24 tokens: 2 GiB in 128-byte rows.)
+constexpr int64_t kPromptTokens = (int64_t)1 << 25;
+
 asrkf_status on_device(const asrkf_ctx* ctx) {
     int d = -1;
     if (hipGetDevice(&d) != hipSuccess || d != ctx->device)
@@ -734,7 +739,7 @@ asrkf_status asrkf_prefill_packed(asrkf_ctx* ctx, int32_t layer, int32_t n_seqs,
     st = on_device(ctx);
     if (st != ASRKF_OK) return st;
     int64_t total = 0;
-    std::vector<char> seen(c.batch, 0);
+    bool seen[kMaxBatch] = {};
     for (int i = 0; i < n_seqs; ++i) {
         const int seq = seqs[i], n = n_tokens[i];
         if (seq < 0 || seq >= c.batch) return fail(ASRKF_EINVAL, "sequence %d out of range", seq);
@@ -783,19 +788,22 @@ asrkf_status asrkf_prefill_packed(asrkf_ctx* ctx, int32_t layer, int32_t n_seqs,
     hipStream_t s = static_cast<hipStream_t>(stream);
     HIP_OK(ctx, follow_last_stream(ctx, s));
     // the longest prompts first, so that the launch does not end on one of them
-    std::vector<int32_t> start(n_seqs), order;
-    int32_t at = 0;
+    int32_t start[kMaxBatch], order[kMaxBatch];       // no allocation that could throw
+    int32_t at = 0, filled = 0;
     for (int i = 0; i < n_seqs; ++i) {
         start[i] = at;
         at += n_tokens[i];
-        if (n_tokens[i] > 0) order.push_back(i);
+        if (n_tokens[i] > 0) order[filled++] = i;
     }
-    std::stable_sort(order.begin(), order.end(), [&](int x, int y) { return n_tokens[x] > n_tokens[y]; });
-    for (size_t i0 = 0; i0 < order.size(); i0 += kPromptSeqs) {
+    std::sort(order, order + filled, [&](int x, int y) { return n_tokens[x] != n_tokens[y] ? n_tokens[x] > n_tokens[y] : x < y; });
+    for (int i = 0; i < filled;) {
         PromptBatch b{};
-        for (size_t i = i0; i < order.size() && b.n < kPromptSeqs; ++i, ++b.n) {
+        for (int64_t sum = 0; i < filled && b.n < kPromptSeqs; ++i, ++b.n) {
+            const int len = n_tokens[order[i]];
+            sum += len;
+            if (b.n > 0 && sum > kPromptTokens) break;
             b.start[b.n] = start[order[i]];
-            b.len[b.n] = n_tokens[order[i]];
+            b.len[b.n] = len;
             b.seq[b.n] = seqs[order[i]];
         }
         HIP_OK(ctx, q ? launch_prompt_attention(p, b, c.dtype == ASRKF_BF16, c.head_dim, s)
