@@ -9,6 +9,10 @@
 //          and plane.  The end-of-step verdict sums the planes and compares
 //          with tau, so no score crosses workgroups here.
 //
+// Rows are bf16 or fp32, read as below, or codes of 4 bits with bf16 queries, whose walk
+// over a wave's tiles is attention_four.h; the plan, the merge and the verdicts' planes
+// are the same for all.
+//
 // Work decomposition.  The cache is head-major, so a (sequence, KV head) pair
 // is one stream of contiguous rows: its active list, cut into tiles of 32
 // tokens, is a list of tiles.  The tile lists of all pairs, concatenated (each

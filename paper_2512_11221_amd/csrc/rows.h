@@ -13,8 +13,9 @@
 // A row of one KV head is D / 2 bytes of codes (value 2 i in the low half of byte i),
 // so that 16 bytes are one group; the D / 32 scale bytes stand in an array of their
 // own, row by row.  Behind the codes, in rows of 68 bytes (D = 128), they spare a dense
-// launch a second stream (8 x 32k tokens, 8 KV heads: 66.3 us against 67.4), but the
-// rows of a list with gaps then straddle lines: 47.6 us against 38.4 where 35 % attend.
+// launch a second stream, which no longer showed once that stream went past the caches
+// (8 x 32k tokens, 8 KV heads: 66.3 us behind the codes, 64.6 in their own array), and the
+// rows of a list with gaps straddle lines: 47.6 us against 38.4 where 35 % attend.
 #pragma once
 
 #include <hip/hip_runtime.h>
