@@ -198,30 +198,34 @@ rows_kernel(RowsArgs a) {
 // How a workgroup goes about its rows.  kTeam: its waves take 32 rows each and share
 // the tiles of keys, two buffers of them behind a barrier a tile.  kSplit: its waves
 // take the same 32 rows and every WAVES-th tile each, without a barrier, and their
-// states are merged at the end.
-enum Walk { kTeam, kSplit };
+// states are merged at the end.  kHalves: as kTeam, but two waves take the same 32 rows,
+// with the first and the second half of every tile's keys, and their states are merged.
+enum Walk { kTeam, kSplit, kHalves };
 
 template <bool BF16, int D, int WAVES, Walk WALK>
 struct Tile {
-    static constexpr bool kSplits = WALK == kSplit;
+    static constexpr bool kSplits = WALK == kSplit, kHalved = WALK == kHalves;
     static constexpr int kElem = BF16 ? 2 : 4;
     static constexpr int kRow = D * kElem;                // bytes of a row of one head
-    static constexpr int kKeys = kRow <= 256 && !kSplits ? 64 : 32;   // keys of a tile
+    static constexpr int kKeys = kRow <= 256 && !kSplits ? 64 : 32;   // keys of a wave's tile
+    static constexpr int kTileKeys = kHalved ? 2 * kKeys : kKeys;     // keys of a tile in LDS
     static constexpr int kKB = kKeys / 32;                // score blocks of 32 keys
-    static constexpr int kRows = kSplits ? 32 : WAVES * 32;           // query rows of a workgroup
+    static constexpr int kRowWaves = kSplits ? 1 : kHalved ? WAVES / 2 : WAVES;
+    static constexpr int kRows = kRowWaves * 32;          // query rows of a workgroup
     static constexpr int kThreads = kSplits ? 64 : WAVES * 64;        // that load a tile
     // LDS row strides: 16 rows of a 16-byte piece (K), and 4 rows of 64 bytes (V, bf16) or
     // rows 4 apart of 128 bytes (V, fp32), meet no bank twice
     static constexpr int kKStride = kRow + 16;
     static constexpr int kVStride = kRow + (BF16 ? 64 : 32);
-    static constexpr int kKBuffer = kKeys * kKStride, kVBuffer = kKeys * kVStride;
+    static constexpr int kKBuffer = kTileKeys * kKStride, kVBuffer = kTileKeys * kVStride;
     static constexpr int kBuffers = kSplits ? 1 : 2;
     static constexpr int kTiles = kBuffers * (kKBuffer + kVBuffer);   // of the workgroup, or of a wave
     static constexpr int kLds = kTiles * (kSplits ? WAVES : 1);
-    static constexpr int kLoads = kKeys * kRow / 16 / kThreads;   // 16-byte pieces of K (or V) per thread
+    static constexpr int kLoads = kTileKeys * kRow / 16 / kThreads;   // 16-byte pieces of K (or V) per thread
     static constexpr int kQRegs = BF16 ? D / 16 : D / 8;  // 16-byte pieces of q per lane
     static constexpr int kState = D + 4;                  // floats of a row of a wave's state
-    static_assert(kLoads * kThreads * 16 == kKeys * kRow, "whole pieces per thread");
+    static_assert(kLoads * kThreads * 16 == kTileKeys * kRow, "whole pieces per thread");
+    static_assert(!kHalved || kRowWaves * 64 * (D / 2 + 2) * 4 <= kLds, "the states of half the waves fit the tiles");
     static_assert(!kSplits || 32 * kState * 4 <= kTiles, "a wave's state fits its tile");
 };
 
@@ -279,12 +283,13 @@ prompt_attention_kernel(PromptArgs a, PromptBatch batch) {
     const int r0 = block * T::kRows;
     const int first_token = r0 / G;
     const int last_token = min(n - 1, (r0 + T::kRows - 1) / G);
-    const int tiles = last_token / T::kKeys + 1;
+    const int tiles = last_token / T::kTileKeys + 1;
 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
     const int loader = T::kSplits ? lane : threadIdx.x;   // among those that load a tile
-    const int wr0 = T::kSplits ? r0 : r0 + wave * 32;
+    const int wr0 = r0 + wave % T::kRowWaves * 32;
+    const int key0 = T::kHalved ? wave / T::kRowWaves * T::kKeys : 0;    // the wave's keys within a tile
     const int row = wr0 + col;                            // the lane's query row
     const int token = min(row / G, n - 1);                // rows past the end repeat the last token's
     const int wave_first = wr0 / G;
@@ -304,8 +309,8 @@ prompt_attention_kernel(PromptArgs a, PromptBatch batch) {
     intx4 kx[NL], vx[NL];
     // rows past the sequence's end read as zeros
     auto request = [&](const char* base, int64_t stride, int j, intx4 (&x)[NL]) __attribute__((always_inline)) {
-        const int left = min(T::kKeys, n - j * T::kKeys);
-        const auto r = buffer(base + (size_t)j * T::kKeys * stride, left > 0 ? (int)((left - 1) * stride + T::kRow) : 0);
+        const int left = min(T::kTileKeys, n - j * T::kTileKeys);
+        const auto r = buffer(base + (size_t)j * T::kTileKeys * stride, left > 0 ? (int)((left - 1) * stride + T::kRow) : 0);
 #pragma unroll
         for (int u = 0; u < NL; ++u) {
             const int i = loader + u * T::kThreads;
@@ -328,7 +333,7 @@ prompt_attention_kernel(PromptArgs a, PromptBatch batch) {
         bool bad = false;
         // Where a tile holds keys behind some query of the block, a weight of zero must not
         // meet an infinity or a NaN: those values are added on their own.
-        if (j * T::kKeys + T::kKeys - 1 > first_token) {
+        if (j * T::kTileKeys + T::kTileKeys - 1 > first_token) {
 #pragma unroll
             for (int u = 0; u < NL; ++u) vx[u] = finite_part<BF16>(vx[u], bad);
         }
@@ -348,7 +353,7 @@ prompt_attention_kernel(PromptArgs a, PromptBatch batch) {
         for (int i = 0; i < 16; ++i) acc[d][i] = 0.f;
 
     auto scores = [&](int j, floatx16 (&s)[KB]) __attribute__((always_inline)) {
-        const char* kt = tiles_lds + j % T::kBuffers * T::kKBuffer;
+        const char* kt = tiles_lds + j % T::kBuffers * T::kKBuffer + key0 * T::kKStride;
 #pragma unroll
         for (int i = 0; i < NQ; ++i)
 #pragma unroll
@@ -371,10 +376,11 @@ prompt_attention_kernel(PromptArgs a, PromptBatch batch) {
     auto tile = [&](int j, bool infinite) __attribute__((always_inline)) {
         floatx16 s[KB];
         scores(j, s);
-        const char* vt = tiles_lds + T::kBuffers * T::kKBuffer + j % T::kBuffers * T::kVBuffer;
+        const char* vt = tiles_lds + T::kBuffers * T::kKBuffer + j % T::kBuffers * T::kVBuffer + key0 * T::kVStride;
+        const int from = j * T::kTileKeys + key0;
         // key of value i in block b: 32 b + 8 (i / 4) + 4 half + i % 4
-        if (j * T::kKeys + T::kKeys - 1 > wave_first) {
-            const int left = token - j * T::kKeys - half * 4;     // keys up to the lane's token, from its first
+        if (from + T::kKeys - 1 > wave_first) {
+            const int left = token - from - half * 4;     // keys up to the lane's token, from its first
 #pragma unroll
             for (int b = 0; b < KB; ++b)
 #pragma unroll
@@ -440,7 +446,7 @@ prompt_attention_kernel(PromptArgs a, PromptBatch batch) {
         if (infinite) {
             // the values that are not finite, from memory, to the queries that see their key
             // (whatever their weight)
-            for (int key = j * T::kKeys; key <= min(wave_last, j * T::kKeys + T::kKeys - 1); ++key) {
+            for (int key = from; key <= min(wave_last, from + T::kKeys - 1); ++key) {
                 const char* at = v0 + (size_t)key * a.v_stride + half * 4 * T::kElem;
 #pragma unroll
                 for (int d = 0; d < DB; ++d)
@@ -485,7 +491,7 @@ prompt_attention_kernel(PromptArgs a, PromptBatch batch) {
                 request_v(j + 2);
             }
             // else all of it lies behind the wave's queries
-            if (j * T::kKeys <= wave_last) tile(j, holds_infinite[j & 1] == j);
+            if (j * T::kTileKeys + key0 <= wave_last) tile(j, holds_infinite[j & 1] == j);
         }
     }
 
@@ -501,6 +507,30 @@ prompt_attention_kernel(PromptArgs a, PromptBatch batch) {
             *reinterpret_cast<floatx4*>(to) = o;
         }
     };
+    if constexpr (T::kHalved) {
+        // the second halves' states, value by value in the same lanes
+        float* state = reinterpret_cast<float*>(lds) + wave % T::kRowWaves * 64 * (D / 2 + 2) + lane;
+        __syncthreads();
+        if (key0) {
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) state[(d * 16 + i) * 64] = acc[d][i];
+            state[D / 2 * 64] = m;
+            state[(D / 2 + 1) * 64] = l;
+        }
+        __syncthreads();
+        if (key0) return;
+        const float m2 = state[D / 2 * 64];
+        const float M = fmaxf(m, m2), Mr = M == -INFINITY ? 0.f : M;     // waves without a key weigh 0
+        const float f = m == M ? 1.f : __builtin_amdgcn_exp2f((m - Mr) * a.scale_log2);
+        const float f2 = m2 == M ? 1.f : __builtin_amdgcn_exp2f((m2 - Mr) * a.scale_log2);
+        l = l * f + state[(D / 2 + 1) * 64] * f2;
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[d][i] = fmaf(state[(d * 16 + i) * 64], f2, acc[d][i] * f);
+    }
     if constexpr (!T::kSplits) {
         const float inv = 1.f / l;
 #pragma unroll
@@ -581,23 +611,42 @@ hipError_t launch_walk(PromptArgs& a, PromptBatch& b, hipStream_t s) {
 // Which walk, by the launch's work: units of 32 rows of a KV head.
 //  kSplit  with so few units that they leave compute units idle, a unit's keys are split
 //          over four waves.  bf16 rows of 128 up to 256 units (1024 tokens of 8/8 heads:
-//          17.2 us against 26.4; 512 units, 512 tokens of 32/8: 20.2 against 17.5), rows
-//          of 64, two workgroups a CU, up to 1024 (2048 tokens of 16/2: 23.9 against
-//          31.2); fp32 rows, whose products take 16 times as long, up to 1024 (700 tokens
-//          of 32/8: 71 against 105 us; 2000: 378 against 311).  Rows of 256 bf16 have no
-//          registers left for it.
+//          16.4 us against 22.8 in halves; 512 units, 512 tokens of 32/8: 19.9 against
+//          16.6), rows of 64, two workgroups a CU, up to 1024 (2048 tokens of 16/2: 24.6
+//          against 25.9); fp32 rows, whose products take 16 times as long, up to 1024 (700
+//          tokens of 32/8: 70 against 96 us; 1100: 163 against 148).  Rows of 256 bf16 have
+//          no registers left for it, nor for halves.
+//  kHalves where the launch would wait for the longest workgroup of four waves, alone on its
+//          CU: prompts of 512 tokens or more with that workgroup's tiles 1.2 times the mean of
+//          a CU's (32/8 heads of 128: 1280 tokens 29.1 us, 36.2 with four waves; 1536: 35.9
+//          and 42.3; 2048: 57.8 and 56.6; two prompts of 512: 17.8 and 19.1; of 1024: 39.1
+//          and 34.3; four of 375: 24.0 and 20.8).  fp32 rows, whose products hide the merge,
+//          always (2000 tokens of 32/8: 287 us, 384 with four waves; 4000: 1036 and 1132).
 //  kTeam   four waves until every CU has its eight at least twice over, then eight, which
 //          read a tile once for 256 rows (2048 tokens of 32/8: 62 us with four, 68 with
 //          eight; 4096: 188 and 176; four prompts of 1000 to 4000, 16/8 heads of 256: 433
 //          and 341).
 template <bool BF16, int D, int G>
 hipError_t launch_rows(PromptArgs& a, PromptBatch& b, hipStream_t s) {
-    int64_t units = 0;
-    for (int i = 0; i < b.n; ++i) units += ((int64_t)b.len[i] * G + 31) / 32 * a.Hkv;
+    int64_t units = 0, pairs = 0;
+    int longest = 0;
+    for (int i = 0; i < b.n; ++i) {
+        units += ((int64_t)b.len[i] * G + 31) / 32 * a.Hkv;
+        pairs += (int64_t)b.len[i] * (b.len[i] + 64);
+        longest = b.len[i] > longest ? b.len[i] : longest;
+    }
     if constexpr (!BF16 || D < 256)
         if (units <= (BF16 && D == 128 ? 256 : 1024)) return launch_walk<BF16, D, G, 4, kSplit>(a, b, s);
-    if (units < 4096) return launch_walk<BF16, D, G, 4, kTeam>(a, b, s);
-    return launch_walk<BF16, D, G, 8, kTeam>(a, b, s);
+    if (units >= 4096) return launch_walk<BF16, D, G, 8, kTeam>(a, b, s);
+    if constexpr (!BF16) {
+        return launch_walk<BF16, D, G, 8, kHalves>(a, b, s);
+    } else {
+        // workgroups of 128 rows and tiles of 64 keys: longest / 64 against
+        // pairs / 2 / 64 * Hq / 128 / 256 CUs
+        if constexpr (D < 256)
+            if (longest >= 512 && (int64_t)longest * 65536 * 5 > pairs * a.Hq * 6) return launch_walk<BF16, D, G, 8, kHalves>(a, b, s);
+        return launch_walk<BF16, D, G, 4, kTeam>(a, b, s);
+    }
 }
 
 template <bool BF16, int D>

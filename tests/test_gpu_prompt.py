@@ -194,6 +194,51 @@ def test_values_that_are_not_finite_stay_behind_their_token(dtype, D, bad):
         A.asrkf_destroy(ctx)
 
 
+# two waves to a row, with half of a tile's keys each: medium prompts
+HALVES = [(32, 8, 128, "bf16", [513, 65, 1]), (32, 8, 128, "bf16", [0, 640]), (8, 8, 128, "bf16", [2049, 300]),
+          (64, 8, 128, "bf16", [512]), (32, 8, 64, "bf16", [1100]), (32, 8, 64, "f32", [1030, 1, 0, 40]),
+          (32, 8, 128, "f32", [1025, 31]), (32, 8, 128, "f32", [140] * 8)]
+
+
+@pytest.mark.parametrize("Hq,Hkv,D,dtype,lens", HALVES, ids=str)
+@pytest.mark.parametrize("what", ["plain", "grow", "fall", "inf", "nan"])
+def test_medium_prompts(Hq, Hkv, D, dtype, lens, what):
+    """Outputs, scores that rise or fall along the prompt, and values that are not finite in
+    either half of a tile, which reach the tokens from their own on in their dim."""
+    import torch
+    T, n = sum(lens), max(lens)
+    first = sum(lens[:lens.index(n)])
+    A, ctx = _init(len(lens), Hq, Hkv, D, dtype, n + 2)
+    try:
+        q, k, v = _inputs(lens, Hq, Hkv, D, dtype, seed=9)
+        if what in ("grow", "fall"):
+            ramp = torch.arange(T, device="cuda", dtype=torch.float32) / T * 40
+            k[:, :, 3] += (ramp if what == "grow" else ramp.flip(0))[:, None].to(k.dtype)
+            q[:, :, 3] = 20
+        ref, tol = _reference(lens, q, k, v)
+        hit = torch.zeros(q.shape, dtype=torch.bool, device="cuda")
+        bad = {"inf": math.inf, "nan": math.nan}.get(what)
+        vb = v.clone()
+        if bad is not None:
+            G = Hq // Hkv
+            for i, p in enumerate((0, 33, 70, 101, 128 if n > 128 else 127, n - 1)):
+                h = i % min(Hkv, 2)
+                vb[first + p, h, 7 * i] = bad
+                hit[first + p:first + n, h * G:(h + 1) * G, 7 * i] = True
+        out = torch.empty_like(q)
+        A.asrkf_prefill_packed(ctx, 0, range(len(lens)), lens, q, k, vb, out)
+        got = out[hit].float()
+        assert torch.isnan(got).all() if what == "nan" else (got == math.inf).all()
+        keep = ~hit
+        assert ((out.double() - ref).abs()[keep] <= tol[keep]).all()
+        again = torch.empty_like(q)
+        A.asrkf_prefill_packed(ctx, 0, range(len(lens)), lens, q, k, vb, again)
+        assert torch.equal(out.view(torch.int16 if dtype == "bf16" else torch.int32),
+                           again.view(torch.int16 if dtype == "bf16" else torch.int32))
+    finally:
+        A.asrkf_destroy(ctx)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_keys_that_are_not_finite(dtype):
     """A NaN key makes the outputs of its token and the later ones NaN (of its KV head); a
