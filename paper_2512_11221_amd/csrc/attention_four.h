@@ -25,7 +25,7 @@
 //
 // Dense launches over 8 sequences of 32k, 8 KV heads of 128, four query heads each (285 MB):
 // 79.4 us with repeated columns and the 16-bit rows' layouts, 71.8 with several tokens a
-// tile, 64.6 with non-temporal loads of the scales too; the arithmetic alone takes 58, the
+// tile, 62 to 67 with non-temporal loads of the scales too; the arithmetic alone takes 58, the
 // loads alone 53 to 62, and two waves a SIMD overlap them that far.
 
 // A group of 32 values as codes, with its scale byte.

@@ -623,9 +623,9 @@ hipError_t launch_walk(PromptArgs& a, PromptBatch& b, hipStream_t s) {
 //          and 34.3; four of 375: 24.0 and 20.8).  fp32 rows, whose products hide the merge,
 //          always (2000 tokens of 32/8: 287 us, 384 with four waves; 4000: 1036 and 1132).
 //  kTeam   four waves until every CU has its eight at least twice over, then eight, which
-//          read a tile once for 256 rows (2048 tokens of 32/8: 62 us with four, 68 with
-//          eight; 4096: 188 and 176; four prompts of 1000 to 4000, 16/8 heads of 256: 433
-//          and 341).
+//          read a tile once for 256 rows (2048 tokens of 32/8: 62 us with four, 70 with
+//          eight; 4096: 180 and 167, though four prompts of 1024 61 and 70; four prompts of
+//          1000 to 4000, 16/8 heads of 256: 435 and 325).
 template <bool BF16, int D, int G>
 hipError_t launch_rows(PromptArgs& a, PromptBatch& b, hipStream_t s) {
     int64_t units = 0, pairs = 0;
