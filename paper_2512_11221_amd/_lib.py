@@ -162,10 +162,18 @@ def make_config(n_layers, batch, n_q_heads, n_kv_heads, head_dim, max_ctx, windo
                         kv_bits)
 
 
+class Context(int):
+    """The handle of a context, with the layout that tensors are checked against."""
+    layout = None                # q heads, KV heads, head dim, torch type
+
+
 def asrkf_init(cfg):
+    import torch
     h = ctypes.c_void_p()
     _check(load().asrkf_init(ctypes.byref(cfg), ctypes.byref(h)))
-    return h.value
+    ctx = Context(h.value)
+    ctx.layout = (cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim, torch.bfloat16 if cfg.dtype == BF16 else torch.float32)
+    return ctx
 
 
 def asrkf_prefill(ctx, layer, seq, k, v, n_tokens, stream=None):
@@ -178,35 +186,67 @@ def _token_stride(name, x):
     (dense).  The rows of a token must be dense, and tokens may not share memory."""
     if x is None or not hasattr(x, "stride"):
         return 0
-    if x.dim() == 3 and x.shape[0] > 1 and x.stride(2) == 1 and x.stride(1) == x.shape[2]:
-        if x.stride(0) < x.shape[1] * x.shape[2]:
+    stride, shape = x.stride(), x.shape
+    if len(shape) == 3 and shape[0] > 1 and stride[2] == 1 and stride[1] == shape[2]:
+        if stride[0] < shape[1] * shape[2]:
             raise ValueError(f"{name}: tokens overlap")
-        return x.stride(0)
+        return stride[0]
     if not x.is_contiguous():
         raise ValueError(f"{name}: the heads of a token must be dense rows")
     return 0
 
 
-def _dense(name, x):
-    if hasattr(x, "is_contiguous") and not x.is_contiguous():
+def _holds(ctx, name, x, n, kv):
+    """Refuses a tensor of rows [T][heads][dim] with fewer than n tokens, or of another
+    type or head layout than the context's.  The library is given an address: what stands
+    behind the tensor in the same allocation would pass there as its rows."""
+    if n < 1 or not hasattr(x, "data_ptr"):
+        return
+    layout = ctx.layout if type(ctx) is Context else None
+    shape = x.shape
+    have = shape[0] if len(shape) == 3 else n
+    if layout is not None:
+        heads, dim = layout[kv], layout[2]
+        if x.dtype != layout[3]:
+            raise AsrkfError(EINVAL, f"{name} is {x.dtype}, the context {layout[3]}")
+        if len(shape) != 3:
+            have = x.numel() // (heads * dim)
+        elif shape[1] != heads or shape[2] != dim:
+            raise AsrkfError(EINVAL, f"{name}: tokens of {shape[1]} x {shape[2]}, the context's have {heads} heads of {dim}")
+    if have < n:
+        raise AsrkfError(EINVAL, f"{name} holds {have} of {n} tokens")
+
+
+def _dense(ctx, name, x, n, kv):
+    """... of a tensor that has to be dense."""
+    if not hasattr(x, "is_contiguous"):
+        return
+    if not x.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
+    _holds(ctx, name, x, n, kv)
 
 
 def asrkf_prefill_packed(ctx, layer, seqs, n_tokens, q, k, v, out, stream=None):
-    """seqs, n_tokens: Python sequences of ints of the same length."""
+    """seqs, n_tokens: Python sequences of ints of the same length.  Tensors of three
+    dimensions are [tokens][heads][dim]; all hold at least the lengths' sum of tokens."""
     n = len(seqs)
     if len(n_tokens) != n:
         raise ValueError(f"{n} sequences, {len(n_tokens)} lengths")
-    _dense("out", out)
     a, b = array.array("i", seqs), array.array("i", n_tokens)
-    _check(load().asrkf_prefill_packed(ctx, layer, n, a.buffer_info()[0], b.buffer_info()[0], _ptr(q), _token_stride("q", q), _ptr(k),
-                                       _token_stride("k", k), _ptr(v), _token_stride("v", v), _ptr(out),
-                                       _stream(stream)))
+    total = sum(b)
+    strides = _token_stride("q", q), _token_stride("k", k), _token_stride("v", v)
+    _dense(ctx, "out", out, total, 0)
+    _holds(ctx, "q", q, total, 0)
+    _holds(ctx, "k", k, total, 1)
+    _holds(ctx, "v", v, total, 1)
+    _check(load().asrkf_prefill_packed(ctx, layer, n, a.buffer_info()[0], b.buffer_info()[0], _ptr(q), strides[0], _ptr(k),
+                                       strides[1], _ptr(v), strides[2], _ptr(out), _stream(stream)))
 
 
 def asrkf_get_rows(ctx, layer, seq, first, n, k, v, stream=None):
-    _dense("k", k)
-    _dense("v", v)
+    """k, v: tensors of at least n tokens."""
+    _dense(ctx, "k", k, n, 1)
+    _dense(ctx, "v", v, n, 1)
     _check(load().asrkf_get_rows(ctx, layer, seq, first, n, _ptr(k), _ptr(v), _stream(stream)))
 
 

@@ -58,3 +58,62 @@ def test_four_bit_reference():
     assert np.isin(np.abs(r / X[:, None]), VALUES).all()
     assert np.isnan(rounded(np.r_[np.inf, np.zeros(31)])).all() and (rounded(np.zeros(32)) == 0).all()
     assert (rounded(np.full(32, 2.0 ** -130)) == 0).all()
+
+
+class _Called(Exception):
+    pass
+
+
+class _NoLibrary:
+    """In the place of the library: says that the call got that far."""
+    def asrkf_prefill_packed(self, *a):
+        raise _Called
+
+    asrkf_get_rows = asrkf_prefill_packed
+
+
+def _context():
+    import torch
+    ctx = A._lib.Context(1 << 12)
+    ctx.layout = (8, 2, 64, torch.bfloat16)
+    return ctx
+
+
+def test_binding_refuses_tensors_that_hold_too_little(monkeypatch):
+    """A tensor with fewer tokens than the lengths' sum, or of another type or head layout, lies in an
+    allocation that may go on behind it: the library would take its neighbour's bytes for rows."""
+    import torch
+    monkeypatch.setattr(A._lib, "load", _NoLibrary)
+    ctx = _context()
+    rows = lambda n, h, d=64, t=torch.bfloat16: torch.zeros((n, h, d), dtype=t)   # noqa: E731
+    q, k, out = rows(12, 8), rows(12, 2), rows(12, 8)
+    good = dict(q=q, k=k, v=k, out=out)
+
+    def call(lens=(5, 0, 7), ctx=ctx, **kw):
+        A.asrkf_prefill_packed(ctx, 0, range(len(lens)), lens, *{**good, **kw}.values(), stream=0)
+
+    fused = rows(12, 12)
+    taken = [dict(), dict(q=None, out=None), dict(lens=(3, 4)), dict(k=k.view(-1), v=k.view(12, 128)),
+             dict(q=fused[:, :8], k=fused[:, 8:10], v=fused[:, 10:]), dict(lens=(0,), q=None, k=None, v=None, out=None),
+             dict(lens=(0, 0), k=rows(0, 2)), dict(lens=(-3, 2))]      # (the library's to refuse)
+    for kw in taken:
+        with pytest.raises(_Called):
+            call(**kw)
+    wide = torch.float32
+    for name, h in (("q", 8), ("k", 2), ("v", 2), ("out", 8)):
+        for bad in (rows(11, h), rows(12, h, t=wide), rows(12, h).view(torch.int16), rows(12, h, 32), rows(24, h // 2),
+                    rows(12, 64, h), rows(12, h).view(-1)[:-1], rows(11, h).view(11, -1)):
+            with pytest.raises(A.AsrkfError) as e:
+                call(**{name: bad})
+            assert e.value.code == A._lib.EINVAL and str(e.value).split(": ")[1].startswith(name), e.value
+    for bad in (dict(q=rows(11, 8)), dict(v=rows(11, 2))):             # a bare handle knows no layout
+        with pytest.raises(A.AsrkfError):
+            call(ctx=int(ctx), **bad)
+
+    with pytest.raises(_Called):
+        A.asrkf_get_rows(ctx, 0, 0, 3, 12, k, k.clone(), stream=0)
+    for bad in (rows(11, 2), rows(12, 2, t=wide), rows(12, 8), rows(12, 2).view(-1)[:-1]):
+        for a, b in ((bad, k), (k, bad)):
+            with pytest.raises(A.AsrkfError) as e:
+                A.asrkf_get_rows(ctx, 0, 0, 0, 12, a, b, stream=0)
+            assert e.value.code == A._lib.EINVAL
