@@ -287,6 +287,38 @@ def test_large_values_do_not_overflow():
         A.asrkf_destroy(ctx)
 
 
+# (q heads, KV heads, head dim, lengths) in each walk: one key set for few rows, two waves to a
+# row, four waves, eight waves
+LARGE = [(4, 2, 64, "bf16", [300, 1]), (8, 2, 64, "bf16", [3000]), (32, 8, 128, "bf16", [700]), (32, 8, 128, "bf16", [400] * 3),
+         (32, 8, 128, "bf16", [2100] * 2), (8, 4, 256, "bf16", [513]), (8, 2, 64, "f32", [2000]),
+         (32, 8, 64, "f32", [1100]), (32, 8, 128, "f32", [700] * 6)]
+
+
+@pytest.mark.parametrize("Hq,Hkv,D,dtype,lens", LARGE, ids=str)
+@pytest.mark.parametrize("what", ["same", "even", "signs"])
+def test_values_at_the_largest(Hq, Hkv, D, dtype, lens, what):
+    """Outputs are averages: with values at their type's largest (fp32: below it by more than the sums'
+    rounding, 2 n 2^-24 < 2^-10) they are finite and as near as others.  All values alike under
+    scores that differ and that do not, and values of both signs."""
+    import torch
+    A, ctx = _init(len(lens), Hq, Hkv, D, dtype, max(lens) + 2)
+    try:
+        q, k, v = _inputs(lens, Hq, Hkv, D, dtype, seed=21)
+        big = torch.finfo(v.dtype).max * (1 - (2.0 ** -9 if dtype == "f32" else 0))
+        if what == "signs":
+            v = torch.where(v > 0.3, big, -big).to(v.dtype)
+        else:
+            v = torch.full_like(v, big)
+        if what == "even":
+            q.zero_()
+        out = torch.empty_like(q)
+        A.asrkf_prefill_packed(ctx, 0, range(len(lens)), lens, q, k, v, out)
+        assert torch.isfinite(out).all()
+        _check(out, *_reference(lens, q, k, v), sum(lens))
+    finally:
+        A.asrkf_destroy(ctx)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_token_strides(dtype):
     """q, k and v as slices of one fused projection, and rows far apart."""
