@@ -20,6 +20,7 @@
 #include <type_traits>
 
 #include "kernels.h"
+#include "prompt_walk.h"
 #include "rows.h"
 
 namespace asrkf {
@@ -195,13 +196,6 @@ rows_kernel(RowsArgs a) {
 
 // ---- attention ----
 
-// How a workgroup goes about its rows.  kTeam: its waves take 32 rows each and share
-// the tiles of keys, two buffers of them behind a barrier a tile.  kSplit: its waves
-// take the same 32 rows and every WAVES-th tile each, without a barrier, and their
-// states are merged at the end.  kHalves: as kTeam, but two waves take the same 32 rows,
-// with the first and the second half of every tile's keys, and their states are merged.
-enum Walk { kTeam, kSplit, kHalves };
-
 template <bool BF16, int D, int WAVES, Walk WALK>
 struct Tile {
     static constexpr bool kSplits = WALK == kSplit, kHalved = WALK == kHalves;
@@ -255,12 +249,6 @@ __device__ __forceinline__ intx4 finite_part(intx4 x, bool& bad) {
 // tokens: 4.9e-7 off in the 2-norm, 4.0e-7 so; 2000 tokens of 32/8 heads of 128: 290 us, 296 so).
 constexpr float kLazy = 8.f;
 
-// waves of a SIMD that the registers leave room for
-constexpr int prompt_waves(bool bf16, int head_dim, int waves, Walk walk) {
-    const int row = head_dim * (bf16 ? 2 : 4);
-    return waves == 8 || row < 256 || (walk == kTeam && row == 256) ? 2 : 1;
-}
-
 template <bool BF16, int D, int G, int WAVES, Walk WALK>
 __global__ void __launch_bounds__(WAVES * 64, (prompt_waves(BF16, D, WAVES, WALK)))
 prompt_attention_kernel(PromptArgs a, PromptBatch batch) {
@@ -277,8 +265,7 @@ prompt_attention_kernel(PromptArgs a, PromptBatch batch) {
         return;
     }
     const int kvh = blockIdx.x % a.Hkv;
-    int unit = blockIdx.x / a.Hkv;
-    if (unit >= a.fold) unit = a.attention_blocks / a.Hkv - 1 - (unit - a.fold);
+    const int unit = prompt_unit(blockIdx.x / a.Hkv, a.fold, a.attention_blocks / a.Hkv);
     const int si = find_sequence(batch.first, batch.n, unit);
     const int n = batch.len[si];
     const int blocks = (n * G + T::kRows - 1) / T::kRows;
@@ -599,61 +586,30 @@ int store_blocks(PromptBatch& b) {
 template <bool BF16, int D, int G, int WAVES, Walk WALK>
 hipError_t launch_walk(PromptArgs& a, PromptBatch& b, hipStream_t s) {
     using T = Tile<BF16, D, WAVES, WALK>;
+    constexpr PromptWalk w{WALK, WAVES};
     int blocks = 0;
     for (int i = 0; i < b.n; ++i) {
         b.first[i] = blocks;
         blocks += (b.len[i] * G + T::kRows - 1) / T::kRows;
     }
     a.attention_blocks = blocks * a.Hkv;
-    // The longest blocks come first.  Where every CU gets two workgroups at once, the second
-    // half goes the other way, so that a CU's two are a long and a short one (two prompts of
-    // 1024, 32/8 heads of 128: 42 us without, 35 with).
-    constexpr int kCUs = 256;
-    a.fold = WALK == kTeam && WAVES == 4 && a.attention_blocks > kCUs && a.attention_blocks <= 2 * kCUs ? blocks / 2 : blocks;
+    a.fold = prompt_fold(w, BF16, D, blocks, a.Hkv);
     const int grid = a.attention_blocks + store_blocks(b);
     hipLaunchKernelGGL((prompt_attention_kernel<BF16, D, G, WAVES, WALK>), dim3(grid), dim3(WAVES * 64), 0, s, a, b);
     return hipGetLastError();
 }
 
-// Which walk, by the launch's work: units of 32 rows of a KV head.
-//  kSplit  with so few units that they leave compute units idle, a unit's keys are split
-//          over four waves.  bf16 rows of 128 up to 256 units (1024 tokens of 8/8 heads:
-//          16.4 us against 22.8 in halves; 512 units, 512 tokens of 32/8: 19.9 against
-//          16.6), rows of 64, two workgroups a CU, up to 1024 (2048 tokens of 16/2: 24.6
-//          against 25.9); fp32 rows, whose products take 16 times as long, up to 1024 (700
-//          tokens of 32/8: 70 against 96 us; 1100: 163 against 148).  Rows of 256 bf16 have
-//          no registers left for it, nor for halves.
-//  kHalves where the launch would wait for the longest workgroup of four waves, alone on its
-//          CU: prompts of 512 tokens or more with that workgroup's tiles 1.2 times the mean of
-//          a CU's (32/8 heads of 128: 1280 tokens 29.1 us, 36.2 with four waves; 1536: 35.9
-//          and 42.3; 2048: 57.8 and 56.6; two prompts of 512: 17.8 and 19.1; of 1024: 39.1
-//          and 34.3; four of 375: 24.0 and 20.8).  fp32 rows, whose products hide the merge,
-//          always (2000 tokens of 32/8: 287 us, 384 with four waves; 4000: 1036 and 1132).
-//  kTeam   four waves until every CU has its eight at least twice over, then eight, which
-//          read a tile once for 256 rows (2048 tokens of 32/8: 62 us with four, 70 with
-//          eight; 4096: 180 and 167, though four prompts of 1024 61 and 70; four prompts of
-//          1000 to 4000, 16/8 heads of 256: 435 and 325).
 template <bool BF16, int D, int G>
 hipError_t launch_rows(PromptArgs& a, PromptBatch& b, hipStream_t s) {
-    int64_t units = 0, pairs = 0;
-    int longest = 0;
-    for (int i = 0; i < b.n; ++i) {
-        units += ((int64_t)b.len[i] * G + 31) / 32 * a.Hkv;
-        pairs += (int64_t)b.len[i] * (b.len[i] + 64);
-        longest = b.len[i] > longest ? b.len[i] : longest;
+    const PromptWalk w = prompt_walk(BF16, D, G, a.Hkv, b.len, b.n);
+    if (w.walk == kTeam && w.waves == 8) return launch_walk<BF16, D, G, 8, kTeam>(a, b, s);
+    if constexpr (BF16)
+        if (w.walk == kTeam) return launch_walk<BF16, D, G, 4, kTeam>(a, b, s);
+    if constexpr (!BF16 || D < 256) {
+        if (w.walk == kSplit) return launch_walk<BF16, D, G, 4, kSplit>(a, b, s);
+        if (w.walk == kHalves) return launch_walk<BF16, D, G, 8, kHalves>(a, b, s);
     }
-    if constexpr (!BF16 || D < 256)
-        if (units <= (BF16 && D == 128 ? 256 : 1024)) return launch_walk<BF16, D, G, 4, kSplit>(a, b, s);
-    if (units >= 4096) return launch_walk<BF16, D, G, 8, kTeam>(a, b, s);
-    if constexpr (!BF16) {
-        return launch_walk<BF16, D, G, 8, kHalves>(a, b, s);
-    } else {
-        // workgroups of 128 rows and tiles of 64 keys: longest / 64 against
-        // pairs / 2 / 64 * Hq / 128 / 256 CUs
-        if constexpr (D < 256)
-            if (longest >= 512 && (int64_t)longest * 65536 * 5 > pairs * a.Hq * 6) return launch_walk<BF16, D, G, 8, kHalves>(a, b, s);
-        return launch_walk<BF16, D, G, 4, kTeam>(a, b, s);
-    }
+    return hipErrorInvalidValue;
 }
 
 template <bool BF16, int D>

@@ -1,0 +1,84 @@
+// How a launch over packed prompts goes about its rows (prompt.hip): which walk, and in
+// what order its workgroups take their blocks.  Plain arithmetic on the host, apart from
+// the kernel so that it is checked without a GPU.
+#pragma once
+
+#include <stdint.h>
+
+#ifdef __HIPCC__
+#define ASRKF_WALK_HD __host__ __device__
+#else
+#define ASRKF_WALK_HD
+#endif
+
+namespace asrkf {
+
+// kTeam: a workgroup's waves take 32 rows each and share the tiles of keys, two buffers
+// of them behind a barrier a tile.  kSplit: its waves take the same 32 rows and every
+// fourth tile each, without a barrier, and their states are merged at the end.  kHalves:
+// as kTeam, but two waves take the same 32 rows, with the first and the second half of
+// every tile's keys, and their states are merged.
+enum Walk { kTeam, kSplit, kHalves };
+
+struct PromptWalk {
+    Walk walk;
+    int waves;              // of a workgroup
+    int rows() const { return 32 * (walk == kSplit ? 1 : walk == kHalves ? waves / 2 : waves); }
+};
+
+// waves of a SIMD that the registers leave room for
+constexpr int prompt_waves(bool bf16, int head_dim, int waves, Walk walk) {
+    const int row = head_dim * (bf16 ? 2 : 4);
+    return waves == 8 || row < 256 || (walk == kTeam && row == 256) ? 2 : 1;
+}
+
+// Which walk, by the launch's work: units of 32 rows of a KV head.
+//  kSplit  with so few units that they leave compute units idle, a unit's keys are split
+//          over four waves.  bf16 rows of 128 up to 256 units (1024 tokens of 8/8 heads:
+//          16.4 us against 22.8 in halves; 512 units, 512 tokens of 32/8: 19.9 against
+//          16.6), rows of 64, two workgroups a CU, up to 1024 (2048 tokens of 16/2: 24.6
+//          against 25.9); fp32 rows, whose products take 16 times as long, up to 1024 (700
+//          tokens of 32/8: 70 against 96 us; 1100: 163 against 148).  Rows of 256 bf16 have
+//          no registers left for it, nor for halves.
+//  kHalves where the launch would wait for the longest workgroup of four waves, alone on its
+//          CU: prompts of 512 tokens or more with that workgroup's tiles 1.2 times the mean of
+//          a CU's (32/8 heads of 128: 1280 tokens 29.1 us, 36.2 with four waves; 1536: 35.9
+//          and 42.3; 2048: 57.8 and 56.6; two prompts of 512: 17.8 and 19.1; of 1024: 39.1
+//          and 34.3; four of 375: 24.0 and 20.8).  fp32 rows, whose products hide the merge,
+//          always (2000 tokens of 32/8: 287 us, 384 with four waves; 4000: 1036 and 1132).
+//  kTeam   four waves until every CU has its eight at least twice over, then eight, which
+//          read a tile once for 256 rows (2048 tokens of 32/8: 62 us with four, 70 with
+//          eight; 4096: 180 and 167, though four prompts of 1024 61 and 70; four prompts of
+//          1000 to 4000, 16/8 heads of 256: 435 and 325).
+inline PromptWalk prompt_walk(bool bf16, int head_dim, int group, int n_kv_heads, const int32_t* len, int n) {
+    int64_t units = 0, pairs = 0;
+    int longest = 0;
+    for (int i = 0; i < n; ++i) {
+        units += ((int64_t)len[i] * group + 31) / 32 * n_kv_heads;
+        pairs += (int64_t)len[i] * (len[i] + 64);
+        longest = len[i] > longest ? len[i] : longest;
+    }
+    if (!(bf16 && head_dim == 256) && units <= (bf16 && head_dim == 128 ? 256 : 1024)) return {kSplit, 4};
+    if (units >= 4096) return {kTeam, 8};
+    if (!bf16) return {kHalves, 8};
+    // workgroups of 128 rows and tiles of 64 keys: longest / 64 against
+    // pairs / 2 / 64 * Hq / 128 / 256 CUs
+    if (head_dim < 256 && longest >= 512 && (int64_t)longest * 65536 * 5 > pairs * group * n_kv_heads * 6) return {kHalves, 8};
+    return {kTeam, 4};
+}
+
+// The longest blocks come first.  Where every CU gets two workgroups at once, the second
+// half goes the other way, so that a CU's two are a long and a short one (two prompts of
+// 1024, 32/8 heads of 128: 42 us without, 35 with): the units from here on are in reverse.
+inline int prompt_fold(const PromptWalk& w, bool bf16, int head_dim, int blocks, int n_kv_heads) {
+    constexpr int kCUs = 256;
+    const int workgroups = blocks * n_kv_heads;
+    return w.walk == kTeam && w.waves == 4 && workgroups > kCUs && workgroups <= 2 * kCUs ? blocks / 2 : blocks;
+}
+
+// The unit that the workgroups of place `unit` take, of `blocks` units.
+ASRKF_WALK_HD inline int prompt_unit(int unit, int fold, int blocks) {
+    return unit < fold ? unit : blocks - 1 - (unit - fold);
+}
+
+}  // namespace asrkf
