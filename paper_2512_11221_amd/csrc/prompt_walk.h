@@ -68,12 +68,16 @@ inline PromptWalk prompt_walk(bool bf16, int head_dim, int group, int n_kv_heads
 }
 
 // The longest blocks come first.  Where every CU gets two workgroups at once, the second
-// half goes the other way, so that a CU's two are a long and a short one (two prompts of
-// 1024, 32/8 heads of 128: 42 us without, 35 with): the units from here on are in reverse.
+// half goes the other way, so that a CU's two are a long and a short one: the units from
+// here on are in reverse (two prompts of 1024, 32/8 heads of 128: 42 us without, 35 with).
+// A CU with room for one takes its second when the first ends, the longest first then too:
+// rows of 256, 16/8 heads, two prompts of 2048 191 us in reverse and 151 without, one of
+// 4000 280 and 229, five of 700 75 and 72.
 inline int prompt_fold(const PromptWalk& w, bool bf16, int head_dim, int blocks, int n_kv_heads) {
     constexpr int kCUs = 256;
     const int workgroups = blocks * n_kv_heads;
-    return w.walk == kTeam && w.waves == 4 && workgroups > kCUs && workgroups <= 2 * kCUs ? blocks / 2 : blocks;
+    const bool pairs = w.walk == kTeam && w.waves == 4 && prompt_waves(bf16, head_dim, w.waves, w.walk) >= 2;
+    return pairs && workgroups > kCUs && workgroups <= 2 * kCUs ? blocks / 2 : blocks;
 }
 
 // The unit that the workgroups of place `unit` take, of `blocks` units.

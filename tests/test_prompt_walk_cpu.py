@@ -67,3 +67,30 @@ def test_every_block_is_taken_once(lib):
         for walk, waves in ((0, 4), (0, 8), (1, 4), (2, 8)):
             fold, units = _order(lib, D, dtype, walk, waves, blocks, Hkv)
             assert sorted(units) == list(range(blocks)) and units[:fold] == list(range(fold))
+
+
+def _greedy(work, slots):
+    """The time at which the last of `slots` ends, each taking the next piece of work when it is free."""
+    free = [0] * slots
+    for w in work:
+        i = min(range(slots), key=free.__getitem__)
+        free[i] += w
+    return max(free)
+
+
+@pytest.mark.parametrize("lens", [[2048, 2048], [4000], [1500, 2500], [700] * 5], ids=str)
+def test_rows_of_256_keep_the_longest_blocks_in_front(lib, lens):
+    """A CU has room for one workgroup of four waves with rows of 256.  In the order of the launch the
+    last CU ends no later than with every prompt's blocks from its longest on."""
+    Hq, Hkv, D = 16, 8, 256
+    name, walk, waves, rows = _choice(lib, Hq, Hkv, D, "bf16", lens)
+    assert name == _walks.TEAM4
+    tiles = []                                   # of every unit of a KV head: the last block of a prompt first
+    for n in sorted(lens, reverse=True):
+        blocks = -(-n * (Hq // Hkv) // rows)
+        tiles += [min(n - 1, ((b + 1) * rows - 1) // (Hq // Hkv)) // 32 + 1 for b in reversed(range(blocks))]
+    _, units = _order(lib, D, "bf16", walk, waves, len(tiles), Hkv)
+    assert CUS < len(tiles) * Hkv <= 2 * CUS
+    ends = _greedy([tiles[u] for u in units for _ in range(Hkv)], CUS)
+    straight = _greedy([t for t in tiles for _ in range(Hkv)], CUS)
+    assert ends <= straight, (ends, straight)
