@@ -5,6 +5,8 @@
 #include <hip/hip_ext.h>
 #include <stdint.h>
 
+#include "prompt_walk.h"
+
 namespace asrkf {
 
 // Split-K attention: the tiles of every (sequence, KV head group) pair are dealt
@@ -196,8 +198,6 @@ struct PrefillArgs {
 };
 
 // Packed prompts of one layer (prompt.hip).
-constexpr int kPromptSeqs = 128;           // sequences of a launch, whose table is a kernel argument
-constexpr int kPromptStoreTokens = 16;     // tokens of a workgroup that writes rows into the cache
 struct PromptBatch {
     int32_t n;                             // sequences, none of them empty
     int32_t start[kPromptSeqs];            // first token among the packed ones

@@ -20,7 +20,6 @@
 #include <type_traits>
 
 #include "kernels.h"
-#include "prompt_walk.h"
 #include "rows.h"
 
 namespace asrkf {
@@ -218,6 +217,7 @@ struct Tile {
     static constexpr int kLoads = kTileKeys * kRow / 16 / kThreads;   // 16-byte pieces of K (or V) per thread
     static constexpr int kQRegs = BF16 ? D / 16 : D / 8;  // 16-byte pieces of q per lane
     static constexpr int kState = D + 4;                  // floats of a row of a wave's state
+    static_assert(kTileKeys <= kPromptTileKeys, "offsets within a tile");
     static_assert(kLoads * kThreads * 16 == kTileKeys * kRow, "whole pieces per thread");
     static_assert(!kHalved || kRowWaves * 64 * (D / 2 + 2) * 4 <= kLds, "the states of half the waves fit the tiles");
     static_assert(!kSplits || 32 * kState * 4 <= kTiles, "a wave's state fits its tile");

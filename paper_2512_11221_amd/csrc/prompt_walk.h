@@ -26,6 +26,25 @@ struct PromptWalk {
     int rows() const { return 32 * (walk == kSplit ? 1 : walk == kHalves ? waves / 2 : waves); }
 };
 
+// Keys of a tile in LDS, at most, and bytes from one token to the next of packed rows, at
+// most: offsets within a tile are 32-bit.
+constexpr int kPromptTileKeys = 128;
+constexpr int64_t kMaxTokenStride = (int64_t)16 << 20;
+static_assert(kPromptTileKeys * kMaxTokenStride <= (int64_t)1 << 31, "a tile's offsets, its last row included");
+
+constexpr int kPromptSeqs = 128;           // sequences of a launch, whose table is a kernel argument
+constexpr int kPromptStoreTokens = 16;     // tokens of a workgroup that writes rows into the cache
+
+// Tokens of a launch over several packed prompts, at most, for the 2^32 threads of a grid.
+// (A sequence has below 2^24 tokens: 2 GiB in 128-byte rows.)
+constexpr int64_t kPromptTokens = (int64_t)1 << 24;
+// Threads of a launch, at most: workgroups of 512, one for 256 query rows of a KV head
+// (launches of fewer rows have below 2^12 units) and one for the store.
+constexpr int64_t prompt_threads(int64_t tokens, int q_heads, int n_kv_heads) {
+    return 512 * ((tokens * q_heads / 256 + kPromptSeqs * n_kv_heads) + (tokens / kPromptStoreTokens + kPromptSeqs));
+}
+static_assert(prompt_threads(kPromptTokens, 64, 32) < (int64_t)1 << 32, "the grid of the longest launch");
+
 // waves of a SIMD that the registers leave room for
 constexpr int prompt_waves(bool bf16, int head_dim, int waves, Walk walk) {
     const int row = head_dim * (bf16 ? 2 : 4);

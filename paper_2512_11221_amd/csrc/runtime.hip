@@ -395,15 +395,6 @@ void mark_queued(asrkf_ctx* ctx, hipStream_t s, bool capture) {
     if (capture) ctx->captured = true;
 }
 
-// Bytes from one token to the next of packed rows, at most: offsets within a tile of
-// 64 tokens stay below 2 GiB.
-constexpr int64_t kMaxTokenStride = (int64_t)16 << 20;
-
-// Tokens of a launch over several packed prompts, at most: its workgroups of 512 threads,
-// one for 256 query rows and one for 16 tokens' store, then stay below the 2^32 threads
-// of a grid.  (A sequence has below 2^24 tokens: 2 GiB in 128-byte rows.)
-constexpr int64_t kPromptTokens = (int64_t)1 << 25;
-
 asrkf_status on_device(const asrkf_ctx* ctx) {
     int d = -1;
     if (hipGetDevice(&d) != hipSuccess || d != ctx->device)

@@ -21,4 +21,8 @@ int prompt_order(int bf16, int head_dim, int walk, int waves, int blocks, int n_
     return fold;
 }
 
+int64_t prompt_max_tokens() { return kPromptTokens; }
+int64_t prompt_max_stride() { return kMaxTokenStride; }
+int prompt_max_tile() { return kPromptTileKeys; }
+
 }  // extern "C"

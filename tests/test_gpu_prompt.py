@@ -8,6 +8,7 @@ import pytest
 
 from synth import gen
 from tests import _harness as H
+from tests import _walks
 
 pytestmark = pytest.mark.gpu
 
@@ -357,6 +358,32 @@ def test_longest_token_stride():
         A.asrkf_prefill_packed(ctx, 0, [0], [n], q, k, v, out)
         A.asrkf_prefill_packed(ctx, 0, [0], [n], q, far, v, out2)
         assert torch.equal(out, out2)
+    finally:
+        A.asrkf_destroy(ctx)
+
+
+@pytest.mark.parametrize("Hq,Hkv,D,n,walk", [(16, 2, 128, 520, _walks.HALVES), (64, 8, 64, 520, _walks.HALVES),
+                                             (32, 8, 128, 300, _walks.TEAM4)])
+def test_longest_token_stride_in_larger_tiles(Hq, Hkv, D, n, walk):
+    """... in tiles of 64 and 128 keys, k and v slices of one array whose tiles span up to 2 GiB."""
+    import torch
+    assert _walks.walk(Hq, Hkv, D, "bf16", [n]) == walk
+    stride = (16 << 20) // 2
+    A, ctx = _init(1, Hq, Hkv, D, "bf16", n + 2)
+    try:
+        q, k, v = _inputs([n], Hq, Hkv, D, "bf16")
+        far = torch.empty((n - 1) * stride + 2 * Hkv * D, dtype=torch.bfloat16, device="cuda")
+        far = far.as_strided((n, 2 * Hkv, D), (stride, D, 1))
+        far[:, :Hkv] = k
+        far[:, Hkv:] = v
+        out, out2 = torch.empty_like(q), torch.empty_like(q)
+        A.asrkf_prefill_packed(ctx, 0, [0], [n], q, k, v, out)
+        _check(out, *_reference([n], q, k, v), n)
+        A.asrkf_prefill_packed(ctx, 0, [0], [n], q, far[:, :Hkv], far[:, Hkv:], out2)
+        assert torch.equal(out, out2)
+        kb, vb = torch.empty_like(k), torch.empty_like(v)
+        A.asrkf_get_rows(ctx, 0, 0, 0, n, kb, vb)
+        assert torch.equal(kb, k) and torch.equal(vb, v)
     finally:
         A.asrkf_destroy(ctx)
 

@@ -94,3 +94,21 @@ def test_rows_of_256_keep_the_longest_blocks_in_front(lib, lens):
     ends = _greedy([tiles[u] for u in units for _ in range(Hkv)], CUS)
     straight = _greedy([t for t in tiles for _ in range(Hkv)], CUS)
     assert ends <= straight, (ends, straight)
+
+
+@pytest.mark.parametrize("Hq,Hkv,D,dtype", [(64, 32, 64, "bf16"), (64, 8, 128, "bf16"), (64, 8, 256, "bf16"), (64, 16, 64, "f32")])
+def test_the_longest_launch_fits_a_grid(lib, Hq, Hkv, D, dtype):
+    """The threads of a launch with as many tokens as are taken into one, whatever memory would hold:
+    a workgroup for every block of rows and for every 16 tokens' store."""
+    lib.prompt_max_tokens.restype = ctypes.c_int64
+    top = lib.prompt_max_tokens()
+    for lens in ([top], [top // 128] * 128, [top - 127] + [1] * 127):
+        _, _, waves, rows = _choice(lib, Hq, Hkv, D, dtype, lens)
+        blocks = sum(-(-n * (Hq // Hkv) // rows) for n in lens) * Hkv + sum(-(-n // 16) for n in lens)
+        assert blocks * waves * 64 < 1 << 32
+
+
+def test_offsets_within_a_tile(lib):
+    """... of the longest token stride are 32-bit, the last row's end included."""
+    lib.prompt_max_stride.restype = ctypes.c_int64
+    assert (lib.prompt_max_tile() - 1) * lib.prompt_max_stride() + 1024 < 1 << 31
