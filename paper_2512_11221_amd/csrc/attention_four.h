@@ -93,6 +93,7 @@ struct FourStream {
     static constexpr int kTile = R::kTile;
     static constexpr int kC = kTile / (16 * kParts);      // C tiles of a tile
     static constexpr int kPieces = kParts == 4 ? D / 32 : D / 64;     // 16-byte pieces of K per lane
+    static_assert(kPieces == 1 || kPieces == 2 || kPieces == 4, "a lane's scales are one word");
     static constexpr int NL = R::kFourLoads, NB = D / 16;
 
     int lane, t, t1, n, step, rel_abs;
@@ -214,29 +215,19 @@ struct FourStream {
         const int c16 = lane & 15, q4 = lane >> 4;
         const int token = kParts == 4 ? lane : c * 32 + (q4 >> 1) * 16 + c16;
         const int piece0 = kParts == 4 ? 0 : (q4 & 1) * kPieces;
-        uint32_t sc[(kPieces + 3) / 4];
+        uint32_t sc;
         const char* s = k_scales() + token * R::kScales + piece0;
-        if constexpr (kPieces == 1) sc[0] = *reinterpret_cast<const uint8_t*>(s);
-        else if constexpr (kPieces == 2) sc[0] = *reinterpret_cast<const uint16_t*>(s);
-        else if constexpr (kPieces == 4) sc[0] = *reinterpret_cast<const uint32_t*>(s);
-        else {
-            const uintx2 w = *reinterpret_cast<const uintx2*>(s);
-            sc[0] = w[0];
-            sc[1] = w[1];
-        }
-        uint32_t none = 0;                                // nonzero: some scale byte is 255
-#pragma unroll
-        for (int i = 0; i < (kPieces + 3) / 4; ++i) none |= (~sc[i] - 0x01010101u) & sc[i] & 0x80808080u;
+        if constexpr (kPieces == 1) sc = *reinterpret_cast<const uint8_t*>(s);
+        else if constexpr (kPieces == 2) sc = *reinterpret_cast<const uint16_t*>(s);
+        else sc = *reinterpret_cast<const uint32_t*>(s);
+        const uint32_t none = (~sc - 0x01010101u) & sc & 0x80808080u;     // nonzero: some scale byte is 255
         const uint64_t nans = __ballot(none != 0);        // (lanes of the tokens)
-        if (nans && none) {
-#pragma unroll
-            for (int i = 0; i < (kPieces + 3) / 4; ++i) sc[i] = 0x7F7F7F7Fu;
-        }
+        if (nans && none) sc = 0x7F7F7F7Fu;
         floatx4 sum[2] = {};
 #pragma unroll
         for (int e = 0; e < kPieces; ++e) {
             const intx4 x = *reinterpret_cast<const intx4*>(lds + code_at(token, piece0 + e));
-            const float f = scale_value(sc[e / 4] >> e % 4 * 8 & 255u);
+            const float f = scale_value(sc >> e * 8 & 255u);
             if constexpr (D == 256) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
