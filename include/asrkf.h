@@ -99,7 +99,9 @@ typedef struct {
                                 at most 64 q heads, and at most 8 KiB of K per token (32 KV
                                 heads of 128 bf16, 16 of 256 bf16 or of 128 fp32) */
     int32_t head_dim;        /* 64, 128 or 256 (256 with bf16 rows only) */
-    int32_t max_ctx;         /* positions per sequence: prompt + decode steps */
+    int32_t max_ctx;         /* positions per sequence: prompt + decode steps; max_ctx + 1
+                                rounded up to 64 K rows of all KV heads in dtype stay below
+                                2 GiB, also where the cache holds 4 bits */
     int32_t window_K;        /* protected window of most recent positions (Sec. 3.2; paper: 32) */
     float   tau;             /* relevance threshold, strict s_j < tau (paper: 0.5) */
     float   k_soft;          /* Eq. 3 softness k, in [2^-8, 2^16] (paper: 2) */

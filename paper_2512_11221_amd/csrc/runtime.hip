@@ -311,7 +311,8 @@ asrkf_status validate(const asrkf_config* c) {
         const int64_t row = (int64_t)c->n_kv_heads * c->head_dim * (c->dtype == ASRKF_BF16 ? 2 : 4);
         const int64_t cap = ((int64_t)c->max_ctx + 1 + 63) / 64 * 64;
         if (cap * row >= ((int64_t)1 << 31))
-            return fail(ASRKF_EINVAL, "max_ctx too large: one sequence's cache must stay below 2 GiB per layer");
+            return fail(ASRKF_EINVAL, "max_ctx too large: one sequence's K rows of %lld bytes in dtype must stay below 2 GiB per layer%s",
+                        (long long)row, c->kv_bits ? ", also where the cache holds 4 bits" : "");
     }
     return ASRKF_OK;
 }

@@ -1,5 +1,7 @@
 """Checks of the packed prompts and the 4-bit cache that need no GPU: refused
 configurations, the binding's checks, and the 4-bit format's own reference."""
+import os
+
 import numpy as np
 import pytest
 
@@ -14,6 +16,19 @@ def test_configurations_refused(bad):
     with pytest.raises(A.AsrkfError) as e:
         A.asrkf_init(A.make_config(**{**BASE, **bad}))
     assert e.value.code == A._lib.EINVAL
+
+
+@pytest.mark.parametrize("bits", [0, 4])
+def test_the_longest_context_is_counted_in_the_type_of_the_rows_given(bits):
+    """... whatever the cache holds, and the refusal says so: 2^23 positions of 256 bytes."""
+    with pytest.raises(A.AsrkfError) as e:
+        A.asrkf_init(A.make_config(**{**BASE, "max_ctx": (1 << 23) - 1, "kv_bits": bits}))
+    assert e.value.code == A._lib.EINVAL and "256 bytes in dtype" in str(e.value)
+    assert ("4 bits" in str(e.value)) == (bits == 4)
+    with open(os.path.join(os.path.dirname(A.__file__), "..", "include", "asrkf.h")) as f:
+        text = f.read()
+    doc = text[text.index("int32_t max_ctx;"):text.index("int32_t window_K;")]
+    assert "2 GiB" in doc and "4 bits" in doc
 
 
 def test_null_context():
