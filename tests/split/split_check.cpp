@@ -34,6 +34,16 @@ int split_layout(const int32_t* plen, int batch, int t, int n_kv_heads, int row_
 
 int split_tile(int row_bytes) { return tile_tokens(row_bytes); }
 
+// ... of rows held in 4 bits
+int split_layout_four(const int32_t* plen, int batch, int t, int n_kv_heads, int head_dim, int grid, int* launch) {
+    int heads = 0;
+    attention_layout(plen, batch, t, n_kv_heads, four_tile(head_dim), four_room(head_dim), grid, &heads, launch);
+    return heads;
+}
+
+int split_tile_four(int head_dim) { return four_tile(head_dim); }
+int split_room_four(int head_dim) { return room_tiles(four_tile(head_dim), four_room(head_dim)); }
+
 // The pieces as rows of nine ints (range, then Piece in order), at most cap of
 // them; returns their number.  info: live, aligned, groups, cost.
 int split_pieces(const int32_t* n_active, int batch, int n_kv_heads, int heads_per_group, int grid, int tile,
