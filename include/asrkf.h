@@ -216,11 +216,16 @@ asrkf_status asrkf_prefill(asrkf_ctx* ctx, int32_t layer, int32_t seq,
  *             softmax weights to bf16 for the product with v.
  * Without tokens (T = 0) no pointer to them is looked at.
  * The attention is over k and v as given, also where the cache holds 4 bits.  A
- * value of v that is not finite reaches the tokens from its own on.  All
- * pointers 16-byte aligned, in memory of the context's device (EINVAL
+ * value of v that is not finite reaches the tokens from its own on; where all are
+ * finite, so are the outputs (fp32: below v's largest by the rounding of n terms).
+ * The same call gives the same bits again; how the keys' sums are split follows
+ * the launch's prompts as a whole, so that a prompt's outputs may differ in their
+ * rounding from batch to batch.
+ * All pointers 16-byte aligned, in memory of the context's device (EINVAL
  * otherwise, or where they reach past the end of an allocation, or where out
- * overlaps q, k or v).  Only before
- * the first decode step (else ESTATE).  Asynchronous; the host arrays may be
+ * overlaps q, k or v).  Only before the first decode step (else ESTATE).  A call
+ * that is captured into a graph counts as made: the graph is replayed before the
+ * first decode step, and after no reset.  Asynchronous; the host arrays may be
  * reused on return. */
 asrkf_status asrkf_prefill_packed(asrkf_ctx* ctx, int32_t layer, int32_t n_seqs,
                                   const int32_t* seqs, const int32_t* n_tokens,
@@ -233,6 +238,7 @@ asrkf_status asrkf_prefill_packed(asrkf_ctx* ctx, int32_t layer, int32_t n_seqs,
  * the codes stand for, which enter such a cache again unchanged.
  *   k, v: device, [n][n_kv_heads][head_dim] of cfg.dtype, 16-byte aligned (written;
  *         EINVAL where they overlap)
+ * A layer that was not given the prompt has rows without meaning there.
  * ESTATE in spill mode.  Asynchronous. */
 asrkf_status asrkf_get_rows(asrkf_ctx* ctx, int32_t layer, int32_t seq, int32_t first, int32_t n,
                             void* k, void* v, void* stream);

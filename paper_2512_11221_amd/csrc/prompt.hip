@@ -410,8 +410,11 @@ prompt_attention_kernel(PromptArgs a, PromptBatch batch) {
                 }
             }
             if constexpr (BF16) {
-                // the weights as the product takes them; their sums too, so that an output is an
-                // average under the weights it was formed with
+                // The weights as the product takes them, rounded to bf16; their sums too, so that an
+                // output is an average under the weights it was formed with.  Against 64 bits the
+                // outputs are 2.0e-3 to 2.1e-3 off in the 2-norm, 1.6e-3 of it their own rounding to
+                // bf16; a second bf16 part of each weight brings 1.6e-3 and takes 8k tokens of 32/8
+                // heads of 128 from 554 to 747 us, 2500 of 16/2 of 64 from 30 to 39.
                 bf16x8 w;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) w[e] = (__bf16)p[e];

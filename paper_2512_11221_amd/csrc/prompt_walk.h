@@ -51,24 +51,29 @@ constexpr int prompt_waves(bool bf16, int head_dim, int waves, Walk walk) {
     return waves == 8 || row < 256 || (walk == kTeam && row == 256) ? 2 : 1;
 }
 
-// Which walk, by the launch's work: units of 32 rows of a KV head.
+// Which walk, by the launch's work: units of 32 rows of a KV head.  The times are of one
+// run over every walk, in us; heads are query / KV heads, of 128 where not said.
 //  kSplit  with so few units that they leave compute units idle, a unit's keys are split
 //          over four waves.  bf16 rows of 128 up to 256 units (1024 tokens of 8/8 heads:
-//          16.4 us against 22.8 in halves; 512 units, 512 tokens of 32/8: 19.9 against
-//          16.6), rows of 64, two workgroups a CU, up to 1024 (2048 tokens of 16/2: 24.6
-//          against 25.9); fp32 rows, whose products take 16 times as long, up to 1024 (700
-//          tokens of 32/8: 70 against 96 us; 1100: 163 against 148).  Rows of 256 bf16 have
-//          no registers left for it, nor for halves.
+//          18.9, in halves 24.6; 512 units, 512 tokens of 32/8: 21.9 and 17.7), rows of 64,
+//          two workgroups a CU, up to 1024 (2048 tokens of 16/2: 25.6 and 26.6; 2500: 31.8
+//          and 31.5); fp32 rows, whose products take 16 times as long, up to 1024 (700
+//          tokens of 32/8: 72 and 99; 1100: 142 and 153, past the limit; 2000: 383 and
+//          295).  Rows of 256 bf16 have no registers left for it, nor for halves.
 //  kHalves where the launch would wait for the longest workgroup of four waves, alone on its
 //          CU: prompts of 512 tokens or more with that workgroup's tiles 1.2 times the mean of
-//          a CU's (32/8 heads of 128: 1280 tokens 29.1 us, 36.2 with four waves; 1536: 35.9
-//          and 42.3; 2048: 57.8 and 56.6; two prompts of 512: 17.8 and 19.1; of 1024: 39.1
-//          and 34.3; four of 375: 24.0 and 20.8).  fp32 rows, whose products hide the merge,
-//          always (2000 tokens of 32/8: 287 us, 384 with four waves; 4000: 1036 and 1132).
+//          a CU's (32/8 heads: 1024 tokens 27.0, with four waves 31.1; 1280: 31.8 and 39.6;
+//          1536: 37.8 and 45.2; 2048: 59.0 and 58.3; two prompts of 512: 19.1 and 20.5; of
+//          1024: 42.8 and 36.6; four of 375: 25.5 and 22.6).  fp32 rows, whose products hide
+//          the merge, always (2000 tokens of 32/8: 295, with eight waves 501; 4000: 1059
+//          and 1053).
 //  kTeam   four waves until every CU has its eight at least twice over, then eight, which
-//          read a tile once for 256 rows (2048 tokens of 32/8: 62 us with four, 70 with
-//          eight; 4096: 180 and 167, though four prompts of 1024 61 and 70; four prompts of
-//          1000 to 4000, 16/8 heads of 256: 435 and 325).
+//          read a tile once for 256 rows (32/8 heads: 2048 tokens 58.3 with four, 67.9 with
+//          eight; 4096 tokens 181 and 168).  The limit knows the units alone and is not the
+//          best one for every batch: four prompts of 1024, past it, take 64 with four and
+//          70 with eight, and rows of 256, with one workgroup of four waves on a CU, are
+//          faster with eight well below it (16/8 heads: one prompt of 2048 110 and 117, two
+//          142 and 122, five of 700 72 and 50; 1000 to 4000 tokens, past it, 447 and 313).
 inline PromptWalk prompt_walk(bool bf16, int head_dim, int group, int n_kv_heads, const int32_t* len, int n) {
     int64_t units = 0, pairs = 0;
     int longest = 0;

@@ -597,12 +597,15 @@ asrkf_status asrkf_init(const asrkf_config* cfg, asrkf_ctx** out) {
     }
     // Relevance planes.  A list names distinct device rows, so a plane has room for
     // pool_rows entries.  The planes of as many layers are kept as take a 32nd of the
-    // cache (every layer's under Eq. 2, at most a 64th of it, and under the softmax
-    // reading with rows of 128 and four query heads per KV head), or 256 MiB, less than
-    // a thousandth of the device's memory; the verdicts of every rel_layers layers take
-    // a launch of their own, 8 to 16 us (eight layers of 8 x 4k, 64 query heads: 8.67 ms
-    // a request of 32 steps with one launch a step, 9.20 with two).  Where that does
-    // not fit into the device's memory, one layer's do.
+    // cache (of rows in dtype every layer's under Eq. 2, at most a 64th of it, and under
+    // the softmax reading with rows of 128 and four query heads per KV head), or 256 MiB,
+    // less than a thousandth of the device's memory; the verdicts of every rel_layers
+    // layers take a launch of their own, 8 to 16 us (eight layers of 8 x 4k, 64 query
+    // heads: 8.67 ms a request of 32 steps with one launch a step, 9.20 with two).  Of a
+    // cache held in 4 bits, whose planes are as large, a 32nd holds under Eq. 2 every
+    // layer's with rows of 128 and more and half of them with rows of 64, and under the
+    // softmax reading a quarter of what 16-bit rows do.  Where that does not fit into the
+    // device's memory, one layer's do.
     ctx->rel_cap = std::min(ctx->cap, (ctx->pool_rows + 63) / 64 * 64);
     const size_t layer_planes = (size_t)c.batch * ctx->planes * ctx->rel_cap * 4;
     const size_t kept = std::max(2 * pool_bytes / 32, (size_t)256 << 20) / layer_planes;
