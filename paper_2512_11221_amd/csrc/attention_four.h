@@ -23,10 +23,12 @@
 // instruction); K's codes pass through LDS into the rows that the lanes hold, V's
 // values as bf16, 32 tokens at a time, into transposed reads.
 //
-// Dense launches over 8 sequences of 32k, 8 KV heads of 128, four query heads each (285 MB):
-// 79.4 us with repeated columns and the 16-bit rows' layouts, 71.8 with several tokens a
-// tile, 62 to 67 with non-temporal loads of the scales too; the arithmetic alone takes 58, the
-// loads alone 53 to 62, and two waves a SIMD overlap them that far.
+// Dense launches over 8 sequences of 32k, 8 KV heads of 128, four query heads each (285 MB),
+// random scores: 79.4 us with repeated columns and the 16-bit rows' layouts, 71.8 with several
+// tokens a tile, 62 to 69 with non-temporal loads of the scales too (60 with scores that bring
+// few new maxima; one query head 60, eight 71); the arithmetic alone takes 58, the loads alone
+// 53 to 62, and two waves a SIMD overlap them that far.  Rows of 64 (143 MB, four query heads)
+// 43 us, rows of 256 (8 x 16k, 285 MB) 80.
 
 // A group of 32 values as codes, with its scale byte.
 __device__ __forceinline__ void encode_group(const intx4 (&x)[4], intx4& codes, uint32_t& byte) {
