@@ -196,25 +196,23 @@ def _token_stride(name, x):
     return 0
 
 
-def _holds(ctx, name, x, n, kv):
-    """Refuses a tensor of rows [T][heads][dim] with fewer than n tokens, or of another
-    type or head layout than the context's.  The library is given an address: what stands
-    behind the tensor in the same allocation would pass there as its rows."""
-    if n < 1 or not hasattr(x, "data_ptr"):
-        return
+def _holds(ctx, name, x, n, kv, stride=0):
+    """Refuses a tensor of another type than the context's, and one that ends before its n
+    tokens' rows do (stride: as _token_stride has it).  The library is given an address: what
+    stands behind the tensor in the same allocation would pass there as its rows."""
     layout = ctx.layout if type(ctx) is Context else None
-    shape = x.shape
-    have = shape[0] if len(shape) == 3 else n
-    if layout is not None:
-        heads, dim = layout[kv], layout[2]
-        if x.dtype != layout[3]:
-            raise AsrkfError(EINVAL, f"{name} is {x.dtype}, the context {layout[3]}")
-        if len(shape) != 3:
-            have = x.numel() // (heads * dim)
-        elif shape[1] != heads or shape[2] != dim:
-            raise AsrkfError(EINVAL, f"{name}: tokens of {shape[1]} x {shape[2]}, the context's have {heads} heads of {dim}")
-    if have < n:
-        raise AsrkfError(EINVAL, f"{name} holds {have} of {n} tokens")
+    if layout is None or n < 1 or not hasattr(x, "data_ptr"):
+        return
+    if x.dtype != layout[3]:
+        raise AsrkfError(EINVAL, f"{name} is {x.dtype}, the context {layout[3]}")
+    row = layout[kv] * layout[2]
+    if stride:
+        shape = x.shape
+        have = (shape[0] - 1) * stride + shape[1] * shape[2]
+    else:
+        have = x.numel()
+    if have < (n - 1) * (stride or row) + row:
+        raise AsrkfError(EINVAL, f"{name} is smaller than {n} tokens of {row} values")
 
 
 def _dense(ctx, name, x, n, kv):
@@ -227,24 +225,24 @@ def _dense(ctx, name, x, n, kv):
 
 
 def asrkf_prefill_packed(ctx, layer, seqs, n_tokens, q, k, v, out, stream=None):
-    """seqs, n_tokens: Python sequences of ints of the same length.  Tensors of three
-    dimensions are [tokens][heads][dim]; all hold at least the lengths' sum of tokens."""
+    """seqs, n_tokens: Python sequences of ints of the same length.  q, k, v and out are of the
+    context's type and hold at least the lengths' sum of tokens."""
     n = len(seqs)
     if len(n_tokens) != n:
         raise ValueError(f"{n} sequences, {len(n_tokens)} lengths")
     a, b = array.array("i", seqs), array.array("i", n_tokens)
     total = sum(b)
-    strides = _token_stride("q", q), _token_stride("k", k), _token_stride("v", v)
+    sq, sk, sv = _token_stride("q", q), _token_stride("k", k), _token_stride("v", v)
     _dense(ctx, "out", out, total, 0)
-    _holds(ctx, "q", q, total, 0)
-    _holds(ctx, "k", k, total, 1)
-    _holds(ctx, "v", v, total, 1)
-    _check(load().asrkf_prefill_packed(ctx, layer, n, a.buffer_info()[0], b.buffer_info()[0], _ptr(q), strides[0], _ptr(k),
-                                       strides[1], _ptr(v), strides[2], _ptr(out), _stream(stream)))
+    _holds(ctx, "q", q, total, 0, sq)
+    _holds(ctx, "k", k, total, 1, sk)
+    _holds(ctx, "v", v, total, 1, sv)
+    _check(load().asrkf_prefill_packed(ctx, layer, n, a.buffer_info()[0], b.buffer_info()[0], _ptr(q), sq, _ptr(k), sk,
+                                       _ptr(v), sv, _ptr(out), _stream(stream)))
 
 
 def asrkf_get_rows(ctx, layer, seq, first, n, k, v, stream=None):
-    """k, v: tensors of at least n tokens."""
+    """k, v: tensors of the context's type and at least n tokens."""
     _dense(ctx, "k", k, n, 1)
     _dense(ctx, "v", v, n, 1)
     _check(load().asrkf_get_rows(ctx, layer, seq, first, n, _ptr(k), _ptr(v), _stream(stream)))

@@ -95,8 +95,9 @@ def _context():
 
 
 def test_binding_refuses_tensors_that_hold_too_little(monkeypatch):
-    """A tensor with fewer tokens than the lengths' sum, or of another type or head layout, lies in an
-    allocation that may go on behind it: the library would take its neighbour's bytes for rows."""
+    """A tensor that ends before the rows of the lengths' sum, or of another type, lies in an allocation
+    that may go on behind it: the library would take its neighbour's bytes for rows.  Every other
+    view of the same rows is taken as before."""
     import torch
     monkeypatch.setattr(A._lib, "load", _NoLibrary)
     ctx = _context()
@@ -109,25 +110,27 @@ def test_binding_refuses_tensors_that_hold_too_little(monkeypatch):
 
     fused = rows(12, 12)
     taken = [dict(), dict(q=None, out=None), dict(lens=(3, 4)), dict(k=k.view(-1), v=k.view(12, 128)),
-             dict(q=fused[:, :8], k=fused[:, 8:10], v=fused[:, 10:]), dict(lens=(0,), q=None, k=None, v=None, out=None),
-             dict(lens=(0, 0), k=rows(0, 2)), dict(lens=(-3, 2))]      # (the library's to refuse)
+             dict(q=q.view(1, 12, 512), k=k.view(1, 12, 2, 64)), dict(q=fused[:, :8], k=fused[:, 8:10], v=fused[:, 10:]),
+             dict(q=fused), dict(lens=(0,), q=None, k=None, v=None, out=None), dict(lens=(0, 0), k=rows(0, 2)),
+             dict(lens=(-3, 2)), dict(ctx=int(ctx), q=rows(11, 8))]    # (the library's to refuse; a bare handle)
     for kw in taken:
         with pytest.raises(_Called):
             call(**kw)
     wide = torch.float32
     for name, h in (("q", 8), ("k", 2), ("v", 2), ("out", 8)):
-        for bad in (rows(11, h), rows(12, h, t=wide), rows(12, h).view(torch.int16), rows(12, h, 32), rows(24, h // 2),
-                    rows(12, 64, h), rows(12, h).view(-1)[:-1], rows(11, h).view(11, -1)):
+        for bad in (rows(11, h), rows(12, h, t=wide), rows(12, h).view(torch.int16), rows(12, h, 32), rows(12, h).half(),
+                    rows(12, h).view(-1)[:-1], rows(11, h).view(11, -1), rows(1, h), rows(0, h)):
             with pytest.raises(A.AsrkfError) as e:
                 call(**{name: bad})
             assert e.value.code == A._lib.EINVAL and str(e.value).split(": ")[1].startswith(name), e.value
-    for bad in (dict(q=rows(11, 8)), dict(v=rows(11, 2))):             # a bare handle knows no layout
+    for bad in (fused[:11, :8], fused[:, 5:12]):                       # slices of a fused projection
         with pytest.raises(A.AsrkfError):
-            call(ctx=int(ctx), **bad)
+            call(q=bad)
 
-    with pytest.raises(_Called):
-        A.asrkf_get_rows(ctx, 0, 0, 3, 12, k, k.clone(), stream=0)
-    for bad in (rows(11, 2), rows(12, 2, t=wide), rows(12, 8), rows(12, 2).view(-1)[:-1]):
+    for k12 in (k, k.view(-1), rows(13, 2)):
+        with pytest.raises(_Called):
+            A.asrkf_get_rows(ctx, 0, 0, 3, 12, k12, k.clone(), stream=0)
+    for bad in (rows(11, 2), rows(12, 2, t=wide), rows(12, 2).view(-1)[:-1], rows(0, 2)):
         for a, b in ((bad, k), (k, bad)):
             with pytest.raises(A.AsrkfError) as e:
                 A.asrkf_get_rows(ctx, 0, 0, 0, 12, a, b, stream=0)
