@@ -254,7 +254,9 @@ asrkf_status asrkf_get_rows(asrkf_ctx* ctx, int32_t layer, int32_t seq, int32_t 
  *   q:     device, [batch][n_q_heads][head_dim] of cfg.dtype
  *   k_new: device, [batch][n_kv_heads][head_dim] of cfg.dtype
  *   v_new: device, same layout as k_new
- *   out:   device, [batch][n_q_heads][head_dim] float32 (written)
+ *   out:   device, [batch][n_q_heads][head_dim] float32 (written).  The weighted
+ *          sums are divided at their end: finite as long as the largest |v| times
+ *          the attended tokens is a float
  * Layers must come in order 0 .. n_layers-1 within a step (else ESTATE);
  * ECAPACITY when a sequence has no room for the new position.  Asynchronous. */
 asrkf_status asrkf_decode_step(asrkf_ctx* ctx, int32_t layer, const void* q,
