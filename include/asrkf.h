@@ -30,7 +30,8 @@
  *    shared by all calls).  Calls marked "waits" synchronize only the
  *    context's own streams, not the whole device.
  *  - Graph capture (resident mode): after the first decode step, a whole step
- *    (decode_step of every layer, then restore) may be captured on a stream
+ *    (decode_step of every layer, then restore, with the calls of
+ *    drafted tokens that belong to it) may be captured on a stream
  *    into a HIP graph and replayed; the kernels take the step index from the
  *    context's device counter, so each replay runs the next step.  A captured
  *    call queues nothing until the graph is replayed.  The host learns of
@@ -176,6 +177,37 @@ typedef struct {
 
 typedef struct asrkf_ctx asrkf_ctx;
 
+/* Rotary positions: of a head's first `dim` values every pair (a, b) becomes
+ * magnitude * (a cos x - b sin x, b cos x + a sin x) at the angle x = position *
+ * f_i of its pair i = 0 .. dim/2-1; the other values stay.  Without scaling
+ * f_i = base^(-2 i / dim). */
+typedef enum {
+    ASRKF_ROT_HALVES = 0,  /* values i and i + dim/2 are a pair */
+    ASRKF_ROT_PAIRS = 1    /* values 2 i and 2 i + 1 are */
+} asrkf_rot_layout;
+/* Contexts longer than the original_ctx positions that a model was trained on:
+ * f_i is multiplied by s_i + (1 - s_i) / factor, with s_i cut to 0 .. 1. */
+typedef enum {
+    ASRKF_SCALE_NONE = 0,
+    ASRKF_SCALE_LINEAR = 1,  /* s_i = 0 */
+    ASRKF_SCALE_BANDS = 2,   /* s_i = (r_i - low) / (high - low), r_i = original_ctx f_i / (2 pi)
+                                the pair's turns over the original context */
+    ASRKF_SCALE_RAMP = 3     /* s_i = 1 - (i - p) / (q - p) by pair, from p = the pair of `high`
+                                turns, rounded down and at least 0, to q = that of `low`, rounded
+                                up and at most dim - 1 (where q is not above p the step lies behind
+                                p); the pair of r turns is dim / 2 * log_base(original_ctx / (2 pi r)) */
+} asrkf_rot_scaling;
+typedef struct {
+    int32_t dim;             /* a multiple of 16, at most head_dim */
+    int32_t layout;          /* an asrkf_rot_layout value */
+    int32_t scaling;         /* an asrkf_rot_scaling value */
+    int32_t original_ctx;    /* BANDS and RAMP: >= 1 */
+    double  base;            /* > 1 */
+    double  factor;          /* > 0; not looked at without scaling */
+    double  low, high;       /* BANDS and RAMP: 0 < low < high */
+    double  magnitude;       /* > 0, usually 1 */
+} asrkf_rotary;
+
 /* Allocate the cache and token states of every (layer, sequence): the
  * active cache A, frozen storage F and states S of Algorithm 1 (REQUIRE).
  * cfg: host.  On success *out receives the context.  Errors: EINVAL for a
@@ -281,6 +313,151 @@ asrkf_status asrkf_decode_step(asrkf_ctx* ctx, int32_t layer, const void* q,
 asrkf_status asrkf_decode_step_static(asrkf_ctx* ctx, int32_t layer, const void* q,
                                       const void* k_new, const void* v_new, float* out,
                                       void* stream);
+
+/* Host-only helper: the frequencies f_i (radians per position) of a rotary
+ * setting for heads of head_dim values.  out: host, dim / 2 entries.  EINVAL for
+ * a setting outside the documented ranges. */
+asrkf_status asrkf_rotary_table(const asrkf_rotary* r, int32_t head_dim, double* out);
+
+/* The rotary setting of the context's later asrkf_rotate calls (also after a
+ * reset; captured calls keep the one they were captured with).  r: host.
+ * Host-side. */
+asrkf_status asrkf_set_rotary(asrkf_ctx* ctx, const asrkf_rotary* r);
+
+/* Rows of queries and keys turned by their positions, for the calls that take
+ * them: the library stores K and takes q as given.
+ *   n_rows:       tokens, 0 .. 2^28
+ *   rows_per_seq: 0: row i stands at position pos[i].  Else n_rows = batch *
+ *                 rows_per_seq, and row i, of sequence i / rows_per_seq, stands
+ *                 pos[i] positions behind the token that the present step
+ *                 appends (between two steps: that the next one will), a
+ *                 position that the device knows: in a replayed graph it moves with the
+ *                 steps.  The step's own token has pos 0, a drafted token behind
+ *                 it 1 + its depth.
+ *   pos:          device, [n_rows], or NULL with rows_per_seq for all 0
+ *   q, k:         device, [n_rows][n_q_heads or n_kv_heads][head_dim] of
+ *                 cfg.dtype; either may be NULL with its output
+ *   q_out, k_out: device, the same shapes (written); equal to q, k with the same
+ *                 stride to turn in place
+ *   strides:      elements from one row to the next, 0 for dense rows; else at
+ *                 least a token's row, a multiple of 16 bytes and at most 16 MiB
+ *   inverse:      not 0: the rotation undone (by -x, magnitude 1 / magnitude)
+ * Angles are formed in 64 bits, sine and cosine rounded to fp32, the products
+ * and their sum are fp32 operations, rounded once to cfg.dtype.  All rows 16-byte
+ * aligned, in memory of the context's device (EINVAL otherwise, or where they
+ * reach past the end of an allocation, or where an output overlaps anything but its
+ * own rows).  ESTATE before asrkf_set_rotary.  Asynchronous. */
+asrkf_status asrkf_rotate(asrkf_ctx* ctx, int32_t n_rows, int32_t rows_per_seq, const int32_t* pos,
+                          const void* q, int64_t q_stride, void* q_out, int64_t q_out_stride,
+                          const void* k, int64_t k_stride, void* k_out, int64_t k_out_stride,
+                          int32_t inverse, void* stream);
+
+/* Speculative decoding.  A draft model guesses tokens behind a sequence's last one, as
+ * a tree of at most 64 nodes a sequence (a chain is one): node i has the parent
+ * parents[i] < i, or -1, the root, for a guess of the next token.  The target model
+ * takes the last token and all nodes in one pass:
+ *
+ *     for every layer:  asrkf_decode_step     (the last token)
+ *                       asrkf_attend_drafts   (the nodes)
+ *     asrkf_restore, asrkf_verify_drafts, asrkf_accept_drafts
+ *
+ * The freeze schedule sees the last token of each round: drafted tokens read the
+ * active cache and change no state; accepted ones enter it like prompt tokens
+ * (counts 0, active), and are scored from the next step on. */
+
+/* Room for drafts of up to max_nodes (1 .. 64) nodes a sequence, which the calls
+ * below need; a later call may ask for more.  EINVAL in spill mode.  ESTATE during
+ * capture, and for more room once a call was captured.  Waits for all queued work of
+ * the context. */
+asrkf_status asrkf_reserve_drafts(asrkf_ctx* ctx, int32_t max_nodes);
+
+/* Host-only helper: what the n (1 .. 64) nodes of a tree see and how deep they stand.
+ *   parents: host, [n]
+ *   sees:    host, [n] receives bit j of node i where j is i or an ancestor (may be
+ *            NULL)
+ *   depth:   host, [n] receives 0 for children of the root (may be NULL)
+ * EINVAL for a parent that is neither -1 nor a node before its child. */
+asrkf_status asrkf_tree_masks(int32_t n, const int32_t* parents, uint64_t* sees, int32_t* depth);
+
+/* Attention of every sequence's drafted nodes in one layer: a node attends to the
+ * sequence's active cache (with the step's own token once decode_step of this layer
+ * was called in it) and to the nodes that its mask names (Eq. 1 over both).
+ *   n_nodes:  nodes a sequence that the arrays are laid out for, 1 .. the room
+ *   count:    device, [batch] nodes of each sequence, cut to 0 .. n_nodes; NULL:
+ *             n_nodes each.  Nodes behind them are not read, and their rows of out
+ *             stay as they are.
+ *   sees:     device, [batch][n_nodes] bit j: node j is attended.  Any mask will do (its
+ *             own bit is not implied; bits from count on are not looked at).
+ *   q:        device, [batch][n_nodes][n_q_heads][head_dim] of cfg.dtype
+ *   k, v:     device, [batch][n_nodes][n_kv_heads][head_dim], also where the cache
+ *             holds 4 bits
+ *   q_stride, k_stride, v_stride: elements from one node to the next (sequences
+ *             follow each other at n_nodes of them), as for asrkf_prefill_packed
+ *   out:      device, [batch][n_nodes][n_q_heads][head_dim] of cfg.dtype, dense
+ *             (written).  A node that sees nothing, or only scores of -inf, gets
+ *             zeros.  Sums and softmax statistics are held in fp32; bf16 contexts
+ *             round the softmax weights to bf16 for the product with v.
+ * A value of a node's v that is not finite reaches the nodes that see it, and no
+ * others.  The same call gives the same bits again.  Pointers 16-byte aligned (sees 8,
+ * count 4), in memory of the context's device (EINVAL otherwise, or where they reach
+ * past the end of an allocation, or where out overlaps another).  ESTATE before
+ * the first decode step.  Asynchronous. */
+asrkf_status asrkf_attend_drafts(asrkf_ctx* ctx, int32_t layer, int32_t n_nodes, const int32_t* count,
+                                 const uint64_t* sees, const void* q, int64_t q_stride, const void* k,
+                                 int64_t k_stride, const void* v, int64_t v_stride, void* out, void* stream);
+
+/* Which drafted tokens the target model keeps, from given random numbers.  A walk
+ * from the root looks at the nodes in their order, at those whose parent is the
+ * last one kept.  With p = softmax(logits / temperature) behind that one and w = p
+ * at first, W = sum w, node i with token x is kept where u[i] q(x) W < w(x).
+ * Without draft probabilities q(x) = 1, and where a node is not kept w(x) becomes 0;
+ * with them q is the parent's row and w becomes max(w / W - q, 0) (or stays where
+ * that is 0 everywhere).  The next token is the first whose running sum of w passes
+ * u[n_nodes] W.  A next token then has the target's distribution, whatever
+ * the drafts are (with q: where siblings were drawn from it independently).
+ *   count, parents: device, as above; a parent that is neither -1 nor a node
+ *                before makes the node unreachable
+ *   tokens:      device, [batch][n_nodes]; one outside the vocabulary is not kept
+ *   root_logits: device, [batch][vocab] float32, behind the sequences' last tokens
+ *                (asrkf_restore takes the same)
+ *   logits:      device, [batch][n_nodes][vocab] float32, behind every node
+ *   probs:       device, [batch][n_nodes][vocab] float32 or NULL: row 0 the draft
+ *                model's distribution of the root's children, row 1 + i that of node i's
+ *   temperature: 0: greedy, a node is kept where its token has the largest logit (the
+ *                lowest among equals), the next token is that of the largest; probs
+ *                must be NULL and u is not read.  Else at least 1e-6.
+ *   u:           device, [batch][n_nodes + 1] float32 in [0, 1)
+ *   path:        device, [batch][n_nodes] (written): the nodes kept, from the root
+ *                on, then -1
+ *   n_path:      device, [batch] (written): how many
+ *   next:        device, [batch] (written): the next token.  -1 where the logits
+ *                behind the last node kept hold a NaN, +inf, or nothing above -inf: no child
+ *                of such a row is kept.
+ * Exponentials and sums are 64-bit.  EINVAL where an array reaches past the end of an
+ * allocation or an output overlaps another array.  Asynchronous. */
+asrkf_status asrkf_verify_drafts(asrkf_ctx* ctx, int32_t n_nodes, const int32_t* count, const int32_t* tokens,
+                                 const int32_t* parents, const float* root_logits, const float* logits,
+                                 const float* probs, float temperature, const float* u, int32_t* path,
+                                 int32_t* n_path, int32_t* next, void* stream);
+
+/* Append nodes to their sequences, in every layer: K and V of node path[b][j]
+ * become position n_t + j of sequence b, j < n_path[b], with counts 0 and active
+ * from the next step on.  No step passes: timers and counts of other tokens stay.
+ *   path, n_path: device, as asrkf_verify_drafts leaves them; an entry outside 0 ..
+ *                 n_nodes-1 ends its path
+ *   k, v:         device, [n_layers][batch][n_nodes][n_kv_heads][head_dim] of
+ *                 cfg.dtype, 16-byte aligned; k_stride, v_stride: elements from one node to
+ *                 the next, as above; k_layer_stride, v_layer_stride: from one
+ *                 layer to the next, 0 for dense ones
+ * The host learns how many were accepted at its next waiting call (as of replayed
+ * steps); until then it counts every node, and a call that would then find no room
+ * waits and looks.  ECAPACITY where a sequence has no room for n_nodes; a replayed
+ * call without room appends nothing to that sequence, and the next waiting call
+ * returns ECAPACITY.  ESTATE before the first decode step and within a step.
+ * Asynchronous. */
+asrkf_status asrkf_accept_drafts(asrkf_ctx* ctx, int32_t n_nodes, const int32_t* path, const int32_t* n_path,
+                                 const void* k, int64_t k_stride, int64_t k_layer_stride, const void* v,
+                                 int64_t v_stride, int64_t v_layer_stride, void* stream);
 
 /* End the step: entropy of each sequence's next-token distribution and the
  * recovery ladder (Sec. 3.6), the step's freeze schedule (c_j += 1 and the

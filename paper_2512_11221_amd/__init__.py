@@ -5,6 +5,9 @@ The HIP kernels and the C ABI live in libasrkf.so (csrc/, include/asrkf.h);
 """
 from ._lib import (AUTO, SR, WR, FR, NONE, BF16, F32, AsrkfError, load,  # noqa: F401
                    REL_ABS, REL_SOFTMAX, SCOPE_LAYER, SCOPE_TOKEN, CAND_OUTSIDE, CAND_INSIDE,
+                   ROT_HALVES, ROT_PAIRS, SCALE_NONE, SCALE_LINEAR, SCALE_BANDS, SCALE_RAMP,
+                   make_rotary, asrkf_rotary_table, asrkf_set_rotary, asrkf_rotate, asrkf_reserve_drafts,
+                   asrkf_tree_masks, asrkf_attend_drafts, asrkf_verify_drafts, asrkf_accept_drafts,
                    make_config, asrkf_init, asrkf_prefill, asrkf_prefill_packed, asrkf_get_rows,
                    asrkf_decode_step,
                    asrkf_decode_step_static, asrkf_restore, asrkf_stats, asrkf_stats_reset, asrkf_set_timing, asrkf_timing_series, asrkf_reset,

@@ -21,6 +21,8 @@ AUTO, SR, WR, FR, NONE = 0, 1, 2, 3, 4
 REL_ABS, REL_SOFTMAX = 0, 1
 SCOPE_LAYER, SCOPE_TOKEN = 0, 1
 CAND_OUTSIDE, CAND_INSIDE = 0, 1
+ROT_HALVES, ROT_PAIRS = 0, 1
+SCALE_NONE, SCALE_LINEAR, SCALE_BANDS, SCALE_RAMP = 0, 1, 2, 3
 _STATUS = {EINVAL: "EINVAL", ENOMEM: "ENOMEM", EHIP: "EHIP", ESTATE: "ESTATE",
            ECAPACITY: "ECAPACITY"}
 
@@ -58,6 +60,14 @@ class asrkf_stats_t(ctypes.Structure):
         return d
 
 
+class asrkf_rotary(ctypes.Structure):
+    _fields_ = [
+        ("dim", ctypes.c_int32), ("layout", ctypes.c_int32), ("scaling", ctypes.c_int32), ("original_ctx", ctypes.c_int32),
+        ("base", ctypes.c_double), ("factor", ctypes.c_double), ("low", ctypes.c_double), ("high", ctypes.c_double),
+        ("magnitude", ctypes.c_double),
+    ]
+
+
 class AsrkfError(RuntimeError):
     def __init__(self, code, msg):
         super().__init__(f"{_STATUS.get(code, code)}: {msg}")
@@ -90,6 +100,14 @@ def load():
         "asrkf_decode_step": ([P, I32, P, P, P, P, P], I32),
         "asrkf_decode_step_static": ([P, I32, P, P, P, P, P], I32),
         "asrkf_restore": ([P, P, I32, P], I32),
+        "asrkf_rotary_table": ([ctypes.POINTER(asrkf_rotary), I32, P], I32),
+        "asrkf_set_rotary": ([P, ctypes.POINTER(asrkf_rotary)], I32),
+        "asrkf_rotate": ([P, I32, I32, P, P, I64, P, I64, P, I64, P, I64, I32, P], I32),
+        "asrkf_reserve_drafts": ([P, I32], I32),
+        "asrkf_tree_masks": ([I32, P, P, P], I32),
+        "asrkf_attend_drafts": ([P, I32, I32, P, P, P, I64, P, I64, P, I64, P, P], I32),
+        "asrkf_verify_drafts": ([P, I32, P, P, P, P, P, P, F, P, P, P, P, P], I32),
+        "asrkf_accept_drafts": ([P, I32, P, P, P, I64, I64, P, I64, I64, P], I32),
         "asrkf_stats": ([P, ctypes.POINTER(asrkf_stats_t)], I32),
         "asrkf_stats_reset": ([P], I32),
         "asrkf_set_timing": ([P, I32], I32),
@@ -165,6 +183,7 @@ def make_config(n_layers, batch, n_q_heads, n_kv_heads, head_dim, max_ctx, windo
 class Context(int):
     """The handle of a context, with the layout that tensors are checked against."""
     layout = None                # q heads, KV heads, head dim, torch type
+    sizes = None                 # layers, sequences, vocabulary
 
 
 def asrkf_init(cfg):
@@ -173,6 +192,7 @@ def asrkf_init(cfg):
     _check(load().asrkf_init(ctypes.byref(cfg), ctypes.byref(h)))
     ctx = Context(h.value)
     ctx.layout = (cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim, torch.bfloat16 if cfg.dtype == BF16 else torch.float32)
+    ctx.sizes = (cfg.n_layers, cfg.batch, cfg.vocab)
     return ctx
 
 
@@ -260,6 +280,173 @@ def asrkf_decode_step_static(ctx, layer, q, k_new, v_new, out, stream=None):
 
 def asrkf_restore(ctx, logits, mode=AUTO, stream=None):
     _check(load().asrkf_restore(ctx, _ptr(logits), mode, _stream(stream)))
+
+
+def make_rotary(dim, base=10000.0, layout="halves", scaling="none", factor=1.0, original_ctx=0, low=1.0, high=32.0, magnitude=1.0):
+    return asrkf_rotary(dim, _enum("layout", layout, {"halves": ROT_HALVES, "pairs": ROT_PAIRS}),
+                        _enum("scaling", scaling, {"none": SCALE_NONE, "linear": SCALE_LINEAR, "bands": SCALE_BANDS,
+                                                   "ramp": SCALE_RAMP}), original_ctx, base, factor, low, high, magnitude)
+
+
+def asrkf_rotary_table(head_dim, dim, **setting):
+    """The frequencies of make_rotary(dim, **setting) as a numpy float64 array."""
+    import numpy as np
+    out = np.zeros(max(1, dim // 2), np.float64)
+    _check(load().asrkf_rotary_table(ctypes.byref(make_rotary(dim, **setting)), head_dim, out.ctypes.data))
+    return out
+
+
+def asrkf_set_rotary(ctx, dim, base=10000.0, **setting):
+    _check(load().asrkf_set_rotary(ctx, ctypes.byref(make_rotary(dim, base, **setting))))
+
+
+def _rows(ctx, name, x, kv, n=None):
+    """Rows [..., heads, dim] of the context's type, heads and head dim as its query (kv 0) or KV
+    heads (1): their number and the elements from one to the next.  The dimensions before the heads
+    have to be evenly spaced."""
+    stride, shape = x.stride(), x.shape
+    layout = ctx.layout if type(ctx) is Context else None
+    if layout is not None:
+        if x.dtype != layout[3]:
+            raise AsrkfError(EINVAL, f"{name} is {x.dtype}, the context {layout[3]}")
+        if len(shape) < 3 or shape[-2] != layout[kv] or shape[-1] != layout[2]:
+            raise AsrkfError(EINVAL, f"{name} must be [..., {layout[kv]}, {layout[2]}], not {tuple(shape)}")
+    elif len(shape) < 3:
+        raise AsrkfError(EINVAL, f"{name} must be [..., heads, dim]")
+    rows = math.prod(shape[:-2])
+    if n is not None and rows != n:
+        raise AsrkfError(EINVAL, f"{name} has {rows} rows, not {n}")
+    if rows == 0:
+        return rows, 0
+    if stride[-1] != 1 or (shape[-2] > 1 and stride[-2] != shape[-1]):
+        raise ValueError(f"{name}: the heads of a token must be dense rows")
+    step, size = 0, 1                # of the last dimension that has more than one row; rows behind it
+    for d in range(len(shape) - 3, -1, -1):
+        if shape[d] == 1:
+            continue
+        if step == 0:
+            step = stride[d]
+            if step < shape[-2] * shape[-1]:
+                raise ValueError(f"{name}: tokens overlap")
+        elif stride[d] != step * size:
+            raise ValueError(f"{name}: tokens must be evenly spaced")
+        size *= shape[d]
+    return rows, step
+
+
+def _array(name, x, dtype, shape, optional=False):
+    """A dense tensor of that type and shape."""
+    if x is None and optional:
+        return
+    if not hasattr(x, "data_ptr"):
+        return
+    if x.dtype != dtype:
+        raise AsrkfError(EINVAL, f"{name} is {x.dtype}, not {dtype}")
+    if tuple(x.shape) != tuple(shape):
+        raise AsrkfError(EINVAL, f"{name} is {tuple(x.shape)}, not {tuple(shape)}")
+    if not x.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+
+
+def asrkf_rotate(ctx, pos, q, q_out, k, k_out, rows_per_seq=0, inverse=False, stream=None):
+    """q, q_out [..., q heads, dim], k, k_out [..., KV heads, dim]: as many rows each, evenly spaced; pos:
+    an int32 tensor of as many entries (or None with rows_per_seq)."""
+    import torch
+    n, strides = None, []
+    for name, x, y, kv in (("q", q, q_out, 0), ("k", k, k_out, 1)):
+        if (x is None) != (y is None):
+            raise ValueError(f"{name} and its output go together")
+        for what, t in ((name, x), (f"{name}_out", y)):
+            if t is None:
+                strides.append(0)
+                continue
+            n, step = _rows(ctx, what, t, kv, n)
+            strides.append(step)
+    if n is None:
+        raise ValueError("neither q nor k")
+    if pos is not None and hasattr(pos, "data_ptr"):
+        _array("pos", pos.reshape(-1) if pos.is_contiguous() else pos, torch.int32, (n,))
+    _check(load().asrkf_rotate(ctx, n, rows_per_seq, _ptr(pos), _ptr(q), strides[0], _ptr(q_out), strides[1], _ptr(k), strides[2],
+                               _ptr(k_out), strides[3], 1 if inverse else 0, _stream(stream)))
+
+
+def asrkf_reserve_drafts(ctx, max_nodes):
+    _check(load().asrkf_reserve_drafts(ctx, max_nodes))
+
+
+def asrkf_tree_masks(parents):
+    """(sees, depth) of a tree's nodes as numpy arrays, uint64 and int32."""
+    import numpy as np
+    n = len(parents)
+    p = np.asarray(parents, np.int32)
+    sees, depth = np.zeros(max(1, n), np.uint64), np.zeros(max(1, n), np.int32)
+    _check(load().asrkf_tree_masks(n, p.ctypes.data, sees.ctypes.data, depth.ctypes.data))
+    return sees[:n], depth[:n]
+
+
+def _tree_sizes(ctx, name, x, nodes_dim):
+    """(batch, nodes) of a call, the nodes from a tensor's shape."""
+    if len(x.shape) <= nodes_dim:
+        raise AsrkfError(EINVAL, f"{name} has no dimension for the nodes")
+    batch = ctx.sizes[1] if type(ctx) is Context else x.shape[nodes_dim - 1]
+    if x.shape[nodes_dim - 1] != batch:
+        raise AsrkfError(EINVAL, f"{name} has {x.shape[nodes_dim - 1]} sequences, the context {batch}")
+    return batch, x.shape[nodes_dim]
+
+
+def asrkf_attend_drafts(ctx, layer, sees, q, k, v, out, count=None, stream=None):
+    """q, out [batch, nodes, q heads, dim], k, v [batch, nodes, KV heads, dim]; sees [batch, nodes], int64 or uint64
+    (the bits count); count [batch], int32, or None."""
+    import torch
+    B, N = _tree_sizes(ctx, "q", q, 1)
+    (_, sq), (_, sk), (_, sv) = _rows(ctx, "q", q, 0, B * N), _rows(ctx, "k", k, 1, B * N), _rows(ctx, "v", v, 1, B * N)
+    _rows(ctx, "out", out, 0, B * N)
+    if not out.is_contiguous():
+        raise ValueError("out must be contiguous")
+    _array("sees", sees, torch.uint64 if sees.dtype == torch.uint64 else torch.int64, (B, N))
+    _array("count", count, torch.int32, (B,), optional=True)
+    _check(load().asrkf_attend_drafts(ctx, layer, N, _ptr(count), _ptr(sees), _ptr(q), sq, _ptr(k), sk, _ptr(v), sv, _ptr(out),
+                                      _stream(stream)))
+
+
+def asrkf_verify_drafts(ctx, tokens, parents, root_logits, logits, u, path, n_path, next, probs=None, temperature=1.0, count=None,
+                        stream=None):
+    """tokens, parents, path [batch, nodes], n_path, next, count [batch], int32; root_logits [batch, vocab], logits and
+    probs [batch, nodes, vocab], u [batch, nodes + 1], float32."""
+    import torch
+    B, N = _tree_sizes(ctx, "tokens", tokens, 1)
+    V = ctx.sizes[2] if type(ctx) is Context else root_logits.shape[-1]
+    i32, f32 = torch.int32, torch.float32
+    for name, x, t, shape, optional in (("tokens", tokens, i32, (B, N), False), ("parents", parents, i32, (B, N), False),
+                                        ("path", path, i32, (B, N), False), ("n_path", n_path, i32, (B,), False),
+                                        ("next", next, i32, (B,), False), ("count", count, i32, (B,), True),
+                                        ("root_logits", root_logits, f32, (B, V), False), ("logits", logits, f32, (B, N, V), False),
+                                        ("probs", probs, f32, (B, N, V), True), ("u", u, f32, (B, N + 1), True)):
+        _array(name, x, t, shape, optional)
+    _check(load().asrkf_verify_drafts(ctx, N, _ptr(count), _ptr(tokens), _ptr(parents), _ptr(root_logits), _ptr(logits), _ptr(probs),
+                                      temperature, _ptr(u), _ptr(path), _ptr(n_path), _ptr(next), _stream(stream)))
+
+
+def asrkf_accept_drafts(ctx, path, n_path, k, v, stream=None):
+    """path [batch, nodes], n_path [batch], int32; k, v [layers, batch, nodes, KV heads, dim] (a context of one layer: also
+    without the first dimension)."""
+    import torch
+    B, N = _tree_sizes(ctx, "path", path, 1)
+    L = ctx.sizes[0] if type(ctx) is Context else (k.shape[0] if len(k.shape) > 4 else 1)
+    _array("path", path, torch.int32, (B, N))
+    _array("n_path", n_path, torch.int32, (B,))
+    strides = []
+    for name, x in (("k", k), ("v", v)):
+        if len(x.shape) == 4:
+            x = x[None]
+        if len(x.shape) != 5 or x.shape[0] != L or x.shape[1] != B or x.shape[2] != N:
+            raise AsrkfError(EINVAL, f"{name} must be [{L}, {B}, {N}, KV heads, dim], not {tuple(x.shape)}")
+        _, step = _rows(ctx, name, x[0], 1)
+        strides += [step, x.stride()[0] if L > 1 else 0]
+        if L > 1 and strides[-1] < 1:
+            raise ValueError(f"{name}: layers overlap")
+    _check(load().asrkf_accept_drafts(ctx, N, _ptr(path), _ptr(n_path), _ptr(k), strides[0], strides[1], _ptr(v), strides[2],
+                                      strides[3], _stream(stream)))
 
 
 def asrkf_stats(ctx):

@@ -1,0 +1,790 @@
+// Drafted tokens: their attention over the active cache, and accepted ones' rows into it.
+//
+// Attention, for node i of sequence b's drafts and query head h,
+//   o[i,h] = sum_j softmax_j(q[i,h] . k_j / sqrt(D)) v_j,
+// j over the sequence's active list (Eq. 1's set) and over the nodes that sees[i] names.  Every
+// row sees the whole list, so a (sequence, KV head) pair's query rows, node by node and head
+// by head, are one matrix that the list's K and V rows pass by once: row r is head r % G of
+// node r / G.
+//
+// A tile holds 32 or 64 keys.  The pair's nodes are its first tiles, with a bit per key and
+// row; the list's tiles follow, rows gathered by their positions and, of a cache held in 4 bits,
+// turned into bf16 on the way to LDS.  Products and softmax are as for prompts: scores
+// transposed, S^T = K Q^T with the query row in the lane, O^T = V^T P^T, whose operands are
+// the scores' registers and V's transposed LDS reads.
+//
+// The tiles of all pairs are dealt to a fixed number of workgroups from the counts on the
+// device (attention_split.h).  A pair that several workgroups share leaves one partial each, and
+// the one that arrives last folds them in order.
+#include <type_traits>
+
+#include "attention_split.h"
+#include "kernels.h"
+#include "rows.h"
+#include "tiles.h"
+
+namespace asrkf {
+namespace {
+
+constexpr int kStreamPolicy = 2;              // non-temporal: rows that one workgroup reads
+constexpr int kAgentScope = 16;               // partials: past the XCD's own L2
+constexpr int kNowhere = (int)0x80000000;     // past every buffer's range: reads as zeros
+// What a piece costs a workgroup beside its rows, in tiles.
+constexpr int kDraftPieceCost = 2;
+// As for prompts: the rescaling of O waits until a row's maximum has grown by 2^kLazy.
+constexpr float kLazy = 8.f;
+
+__device__ __forceinline__ int wave_uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+template <int ROWS, int D, int RW, int KW>
+struct Tile {
+    static constexpr bool kFour = ROWS == kRowsFour, kBF16 = ROWS != kRowsF32;
+    static constexpr bool kSplit = RW == 1;               // every wave has a tile of its own
+    static constexpr int kWaves = RW * KW, kThreads = kWaves * 64;
+    static constexpr int kRows = 32 * RW;                 // query rows of a workgroup
+    static constexpr int kElem = kBF16 ? 2 : 4;
+    static constexpr int kRow = D * kElem;                // bytes of a row of one head, in LDS
+    static constexpr int kKeys = KW > 1 || kRow > 256 ? 32 : 64;      // keys of a wave's tile
+    static constexpr int kStep = KW * kKeys;              // ... of the workgroup's
+    static constexpr int kTileKeys = kSplit ? kKeys : kStep;          // ... of a tile in LDS
+    static constexpr int kKB = kKeys / 32;                // score blocks of 32 keys
+    static constexpr int kLoaders = kSplit ? 64 : kThreads;
+    // LDS row strides: 16 rows of a 16-byte piece (K), and 4 rows of 64 bytes (V, bf16) or
+    // rows 4 apart of 128 bytes (V, fp32), meet no bank twice
+    static constexpr int kKStride = kRow + 16;
+    static constexpr int kVStride = kRow + (kBF16 ? 64 : 32);
+    static constexpr int kKBuffer = kTileKeys * kKStride, kVBuffer = kTileKeys * kVStride;
+    static constexpr int kBuffers = kSplit ? 1 : 2;
+    static constexpr int kTiles = kBuffers * (kKBuffer + kVBuffer);   // of the workgroup, or of a wave
+    static constexpr int kLds = kTiles * (kSplit ? kWaves : 1);
+    static constexpr int kPieces = kRow / 16;             // 16-byte pieces of a row in LDS
+    static constexpr int kNodeLoads = kTileKeys * kPieces / kLoaders; // of a tile of nodes, per thread
+    // pieces of a row in the cache: 16 bytes each, 32 codes of 4 bits with one scale
+    static constexpr int kPoolRow = kFour ? D / 2 : kRow;
+    static constexpr int kPoolPieces = kPoolRow / 16;
+    static constexpr int kPoolTotal = kTileKeys * kPoolPieces;
+    static constexpr int kLoads = (kPoolTotal + kLoaders - 1) / kLoaders;
+    static constexpr int kQRegs = kBF16 ? D / 16 : D / 8; // 16-byte pieces of q per lane
+    static constexpr int kState = D + 4;                  // floats of a row of a wave's state
+    static constexpr int kPerSimd = kRow <= 256 || kWaves == 8 ? 2 : 1;
+    static_assert(kNodeLoads * kLoaders == kTileKeys * kPieces, "whole pieces per thread");
+    static_assert(kTileKeys <= 64, "a lane per key's list entry");
+    static_assert(kSplit || KW == 1 || RW * 64 * (D / 2 + 2) * 4 <= kLds, "the states of half the waves fit the tiles");
+    static_assert(!kSplit || 32 * kState * 4 <= kTiles, "a wave's state fits its tile");
+};
+
+// The tiles dealt to the workgroups.  Batches of up to 64 sequences are planned by every wave
+// for itself, one sequence per lane; larger ones by wave 0 into LDS: [B + 1] offsets, then [B]
+// tiles.
+struct Deal : Split {
+    int tiles, units, off;          // of the lane's sequence (up to 64 sequences)
+    const int32_t* lds;
+    int B;
+
+    // the sequence that owns unit x
+    __device__ __forceinline__ int find(int x) const {
+        if (B <= 64) return __popcll(__ballot((int)(threadIdx.x & 63) < B && off + units <= x));
+        int lo = 0, hi = B;                       // the first b with lds[b + 1] > x
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (wave_uniform(lds[mid + 1]) <= x) lo = mid + 1; else hi = mid;
+        }
+        return lo;
+    }
+    __device__ __forceinline__ int offset(int b) const {
+        return B <= 64 ? __builtin_amdgcn_readlane(off, b) : wave_uniform(lds[b]);
+    }
+    __device__ __forceinline__ int count(int b) const {
+        return B <= 64 ? __builtin_amdgcn_readlane(tiles, b) : wave_uniform(lds[B + 1 + b]);
+    }
+};
+
+__device__ __forceinline__ int nodes_of(const DraftArgs& a, int b) {
+    return a.count ? min(max(a.count[b], 0), a.N) : a.N;
+}
+__device__ __forceinline__ int listed(const DraftArgs& a, int b) { return max(a.n_active[b] - a.list_tail, 0); }
+
+template <int STEP>
+__device__ __forceinline__ Deal make_deal(const DraftArgs& a, int32_t* lds) {
+    Deal p;
+    p.init(1, a.Hkv * a.row_blocks, 1, a.grid);
+    p.cost = kDraftPieceCost;
+    p.B = a.B;
+    p.lds = lds;
+    const int lane = threadIdx.x & 63;
+    auto tiles = [&](int b) __attribute__((always_inline)) {
+        const int c = nodes_of(a, b), n = listed(a, b);
+        return c == 0 ? 0 : (n + STEP - 1) / STEP + (c + STEP - 1) / STEP;
+    };
+    auto total_of = [&](int& sum, int& top, int& filled) __attribute__((always_inline)) {
+        for (int o = 1; o < 64; o <<= 1) {
+            sum += __shfl_xor(sum, o);
+            top = max(top, __shfl_xor(top, o));
+            filled += __shfl_xor(filled, o);
+        }
+    };
+    auto before = [&](int x) __attribute__((always_inline)) {     // inclusive sum over the lanes
+        for (int o = 1; o < 64; o <<= 1) {
+            const int y = __shfl_up(x, o);
+            if (lane >= o) x += y;
+        }
+        return x;
+    };
+    if (a.B <= 64) {
+        p.tiles = lane < a.B ? tiles(lane) : 0;
+        int sum = p.tiles, top = p.tiles, filled = p.tiles > 0;
+        total_of(sum, top, filled);
+        p.choose(wave_uniform(sum), wave_uniform(top), wave_uniform(filled));
+        p.units = p.units_of(p.tiles);
+        const int incl = before(p.units);
+        p.off = incl - p.units;
+        p.ranges(__builtin_amdgcn_readlane(incl, 63));
+        return p;
+    }
+    __shared__ int summary[2];
+    if (threadIdx.x < 64) {
+        const int per = (a.B + 63) / 64, b0 = min(a.B, lane * per), b1 = min(a.B, b0 + per);
+        int sum = 0, top = 0, filled = 0;
+        for (int b = b0; b < b1; ++b) {
+            const int t = tiles(b);
+            lds[a.B + 1 + b] = t;
+            sum += t;
+            top = max(top, t);
+            filled += t > 0;
+        }
+        total_of(sum, top, filled);
+        p.choose(wave_uniform(sum), wave_uniform(top), wave_uniform(filled));
+        int mine = 0;
+        for (int b = b0; b < b1; ++b) mine += p.units_of(lds[a.B + 1 + b]);
+        const int incl = before(mine);
+        int run = incl - mine;
+        for (int b = b0; b < b1; ++b) {
+            lds[b] = run;
+            run += p.units_of(lds[a.B + 1 + b]);
+        }
+        if (lane == 63) {
+            lds[a.B] = incl;
+            summary[0] = p.share;
+            summary[1] = p.aligned ? 1 : 0;
+        }
+    }
+    __syncthreads();
+    p.share = wave_uniform(summary[0]);
+    p.aligned = wave_uniform(summary[1]) != 0;
+    p.ranges(wave_uniform(lds[a.B]));
+    return p;
+}
+
+// The weight of a state whose reference is m, in one whose reference is M.
+__device__ __forceinline__ float weight(float m, float M, float scale_log2) {
+    return m == M ? 1.f : __builtin_amdgcn_exp2f((m - (M == -INFINITY ? 0.f : M)) * scale_log2);
+}
+
+template <int ROWS, int D, int RW, int KW>
+__global__ void __launch_bounds__((Tile<ROWS, D, RW, KW>::kThreads), (Tile<ROWS, D, RW, KW>::kPerSimd))
+draft_kernel(DraftArgs a) {
+    using T = Tile<ROWS, D, RW, KW>;
+    constexpr bool BF16 = T::kBF16, FOUR = T::kFour;
+    constexpr int KB = T::kKB, NQ = T::kQRegs, NL = T::kLoads, DB = D / 32;
+    __shared__ __align__(16) char lds[T::kLds];
+    __shared__ float ml_lds[T::kSplit ? T::kWaves * 2 * 32 : 1];
+    __shared__ int infinite_lds, last_arrival;
+    extern __shared__ __align__(16) int32_t deal_lds[];           // more than 64 sequences
+
+    const int wave = wave_uniform(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
+    const int loader = T::kSplit ? lane : threadIdx.x;    // among those that load a tile
+    const int row_wave = wave % RW;
+    const int key0 = T::kSplit ? 0 : wave / RW * T::kKeys;        // the wave's keys within a tile in LDS
+    char* tiles_lds = T::kSplit ? lds + wave * T::kTiles : lds;
+    const int G = a.Hq / a.Hkv, group_shift = __ffs(G) - 1;
+
+    const Deal deal = make_deal<T::kStep>(a, deal_lds);
+    for (int wi = blockIdx.x; wi < deal.live; wi += gridDim.x) {
+    const int w = deal.range_of(wi);
+    int x, x_end;
+    deal.range(w, x, x_end);
+    x = wave_uniform(x);
+    x_end = wave_uniform(x_end);
+    Piece pc;
+    while (next_piece(deal, deal, w, x, x_end, pc)) {
+        const int b = wave_uniform(pc.b), gi = wave_uniform(pc.group);
+        const int t0 = wave_uniform(pc.t0), t1 = wave_uniform(pc.t1);
+        const int n_parts = wave_uniform(pc.n_parts), part = wave_uniform(pc.part);
+        const int kvh = gi / a.row_blocks, r0 = gi % a.row_blocks * T::kRows;
+        const int n = wave_uniform(listed(a, b)), nodes = wave_uniform(nodes_of(a, b));
+        const int live_rows = (nodes << group_shift) - r0;        // of the block, at least
+        if (live_rows <= 0) continue;             // (every workgroup of the pair does)
+        const int node_tiles = (nodes + T::kStep - 1) / T::kStep;
+        const int headroom = 33 - __builtin_clz(n + nodes);
+
+        const size_t pair = (size_t)b * a.Hkv + kvh;
+        const auto rk = buffer(a.kpool + pair * a.pool_rows * T::kPoolRow, a.pool_rows * T::kPoolRow);
+        const auto rv = buffer(a.vpool + pair * a.pool_rows * T::kPoolRow, a.pool_rows * T::kPoolRow);
+        const auto rks = buffer(FOUR ? a.kscale + pair * a.pool_rows * (D / kScaleGroup) : nullptr, FOUR ? a.pool_rows * (D / kScaleGroup) : 0);
+        const auto rvs = buffer(FOUR ? a.vscale + pair * a.pool_rows * (D / kScaleGroup) : nullptr, FOUR ? a.pool_rows * (D / kScaleGroup) : 0);
+        const auto rl = buffer(a.list + (size_t)b * a.cap, n * 4);
+        const char* kn = a.k + (size_t)b * a.N * a.k_stride + kvh * T::kRow;
+        const char* vn = a.v + (size_t)b * a.N * a.v_stride + kvh * T::kRow;
+
+        const int wr0 = r0 + row_wave * 32;
+        const bool idle = row_wave * 32 >= live_rows;     // no row of the wave is written
+        const int row = wr0 + col;                        // the lane's query row
+        const int node = min(row >> group_shift, nodes - 1);      // rows past the end repeat the last node's
+        intx4 q[NQ];
+        {
+            const char* p = a.q + ((size_t)b * a.N + node) * a.q_stride + (kvh * G + (row & (G - 1))) * T::kRow;
+#pragma unroll
+            for (int i = 0; i < NQ; ++i)
+                q[i] = *reinterpret_cast<const intx4*>(p + (BF16 ? i * 32 + half * 16 : half * (T::kRow / 2) + i * 16));
+        }
+        const uint64_t sees = a.sees[(size_t)b * a.N + node] & (nodes >= 64 ? ~0ull : (1ull << nodes) - 1ull);
+
+        // ---- the list's tiles: an entry per lane, then the rows ----
+        int entry = 0;
+        intx4 kx[NL], vx[NL];
+        uint32_t ks[FOUR ? NL : 1], vs[FOUR ? NL : 1];
+        // tile j of the wave (split) or of the workgroup
+        auto request_entries = [&](int j) __attribute__((always_inline)) {
+            const int at = j * T::kTileKeys + (lane & (T::kTileKeys - 1));
+            entry = __builtin_amdgcn_raw_buffer_load_b32(rl, at < n ? at * 4 : kNowhere, 0, 0);
+            entry = at < n ? entry : -1;
+        };
+        auto request = [&]() __attribute__((always_inline)) {
+#pragma unroll
+            for (int u = 0; u < NL; ++u) {
+                const int i = loader + u * T::kLoaders;
+                const int p = __shfl(entry, i / T::kPoolPieces & (T::kTileKeys - 1));
+                const bool in = p >= 0 && (T::kPoolTotal % T::kLoaders == 0 || i < T::kPoolTotal);
+                const int off = in ? p * T::kPoolRow + i % T::kPoolPieces * 16 : kNowhere;
+                kx[u] = __builtin_bit_cast(intx4, __builtin_amdgcn_raw_buffer_load_b128(rk, off, 0, kStreamPolicy));
+                vx[u] = __builtin_bit_cast(intx4, __builtin_amdgcn_raw_buffer_load_b128(rv, off, 0, kStreamPolicy));
+                if constexpr (FOUR) {
+                    const int so = in ? p * (D / kScaleGroup) + i % T::kPoolPieces : kNowhere;
+                    ks[u] = __builtin_amdgcn_raw_buffer_load_b8(rks, so, 0, 0);
+                    vs[u] = __builtin_amdgcn_raw_buffer_load_b8(rvs, so, 0, 0);
+                }
+            }
+        };
+        auto keep = [&](int buf) __attribute__((always_inline)) {
+            char* kt = tiles_lds + buf * T::kKBuffer;
+            char* vt = tiles_lds + T::kBuffers * T::kKBuffer + buf * T::kVBuffer;
+#pragma unroll
+            for (int u = 0; u < NL; ++u) {
+                const int i = loader + u * T::kLoaders;
+                if (T::kPoolTotal % T::kLoaders != 0 && i >= T::kPoolTotal) continue;
+                const int key = i / T::kPoolPieces, piece = i % T::kPoolPieces;
+                if constexpr (FOUR) {
+                    const float kf = scale_value(ks[u]), vf = scale_value(vs[u]);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        const uint32_t kc = (uint32_t)kx[u][c], vc = (uint32_t)vx[u][c];
+                        *reinterpret_cast<uintx4*>(kt + key * T::kKStride + piece * 64 + c * 16) =
+                            uintx4{decode2<0>(kc, kf), decode2<1>(kc, kf), decode2<2>(kc, kf), decode2<3>(kc, kf)};
+                        *reinterpret_cast<uintx4*>(vt + key * T::kVStride + piece * 64 + c * 16) =
+                            uintx4{decode2<0>(vc, vf), decode2<1>(vc, vf), decode2<2>(vc, vf), decode2<3>(vc, vf)};
+                    }
+                } else {
+                    *reinterpret_cast<intx4*>(kt + key * T::kKStride + piece * 16) = kx[u];
+                    *reinterpret_cast<intx4*>(vt + key * T::kVStride + piece * 16) = vx[u];
+                }
+            }
+        };
+        // nodes from .. of a tile into LDS, zeros past the last; whether some value of V was not
+        // finite (it is left out there: a weight of zero must not meet it)
+        auto keep_nodes = [&](int from) __attribute__((always_inline)) {
+            bool bad = false;
+#pragma unroll 4
+            for (int u = 0; u < T::kNodeLoads; ++u) {
+                const int i = loader + u * T::kLoaders, key = i / T::kPieces, piece = i % T::kPieces;
+                intx4 k = {0, 0, 0, 0}, v = {0, 0, 0, 0};
+                if (from + key < nodes) {
+                    k = *reinterpret_cast<const intx4*>(kn + (size_t)(from + key) * a.k_stride + piece * 16);
+                    v = *reinterpret_cast<const intx4*>(vn + (size_t)(from + key) * a.v_stride + piece * 16);
+                }
+                v = finite_part<BF16>(v, bad);
+                *reinterpret_cast<intx4*>(tiles_lds + key * T::kKStride + piece * 16) = k;
+                *reinterpret_cast<intx4*>(tiles_lds + T::kBuffers * T::kKBuffer + key * T::kVStride + piece * 16) = v;
+            }
+            return bad;
+        };
+
+        float m = -INFINITY, l = 0.f;                     // of the lane's row (l: the lane's own keys)
+        floatx16 acc[DB];
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[d][i] = 0.f;
+
+        // the wave's tile in buffer buf; visible: bit j where the lane's row sees key j
+        auto tile = [&](int buf, bool masked, uint64_t visible) __attribute__((always_inline)) {
+            const char* kt = tiles_lds + buf * T::kKBuffer + key0 * T::kKStride;
+            const char* vt = tiles_lds + T::kBuffers * T::kKBuffer + buf * T::kVBuffer + key0 * T::kVStride;
+            floatx16 s[KB];
+#pragma unroll
+            for (int i = 0; i < NQ; ++i)
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb) {
+                    const intx4 kr = *reinterpret_cast<const intx4*>(
+                        kt + (kb * 32 + col) * T::kKStride + (BF16 ? i * 32 + half * 16 : half * (T::kRow / 2) + i * 16));
+                    if (i == 0)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) s[kb][e] = 0.f;
+                    if constexpr (BF16) {
+                        s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kr),
+                                                                        __builtin_bit_cast(bf16x8, q[i]), s[kb], 0, 0, 0);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            s[kb] = __builtin_amdgcn_mfma_f32_32x32x2f32(__int_as_float(kr[e]), __int_as_float(q[i][e]), s[kb], 0, 0, 0);
+                    }
+                }
+            // key of value i in block kb: 32 kb + 8 (i / 4) + 4 half + i % 4
+            if (masked) {
+                const uint64_t mine = visible >> (half * 4);
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb) {
+                    const uint32_t word = (uint32_t)(mine >> (kb * 32));
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[kb][i] = word >> (i / 4 * 8 + i % 4) & 1 ? s[kb][i] : -INFINITY;
+                }
+            }
+            float top = s[0][0];
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) top = fmaxf(top, s[kb][i]);
+            if (__any(top > m + a.lazy)) {
+                const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+                const float mn = fmaxf(m, fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1])));
+                const float sc = m < mn ? __builtin_amdgcn_exp2f((m - mn) * a.scale_log2) : 1.f;
+                m = mn;
+                l *= sc;
+#pragma unroll
+                for (int d = 0; d < DB; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) acc[d][i] *= sc;
+            }
+            const float bias = -(m == -INFINITY ? 0.f : m * a.scale_log2) - (BF16 ? kLazy + headroom : kLazy);
+            // V's transposed reads (bf16): 4 keys of 16 dims per 16 lanes
+            const char* vb = vt + (half * 4 + (lane & 15) / 4) * T::kVStride + (lane >> 4 & 1) * 32 + (lane & 3) * 8;
+            unroll<KB * 2>([&](auto GROUP) __attribute__((always_inline)) {      // of 16 keys
+                constexpr int g = decltype(GROUP)::value;
+                float p[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    p[e] = __builtin_amdgcn_exp2f(fmaf(s[g / 2][g % 2 * 8 + e], a.scale_log2, bias));
+                    if constexpr (!BF16) {
+                        p[e] *= __uint_as_float((127 - headroom) << 23);
+                        l += p[e];
+                    }
+                }
+                if constexpr (BF16) {
+                    // weights rounded to bf16 as the product takes them, and their sums of the rounded
+                    // ones: an output is an average under the weights it was formed with
+                    bf16x8 pw;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) pw[e] = (__bf16)p[e];
+#pragma unroll
+                    for (int e = 0; e < 8; e += 2)
+                        l = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{pw[e], pw[e + 1]}, bf16x2{(__bf16)1.f, (__bf16)1.f}, l, false);
+#pragma unroll
+                    for (int d = 0; d < DB; ++d) {
+                        const char* at = vb + g * 16 * T::kVStride + d * 64;
+                        const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4)at);
+                        const shortx4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4)(at + 8 * T::kVStride));
+                        const bf16x8 v = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+                        acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pw, acc[d], 0, 0, 0);
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const char* at = vt + (g * 16 + e / 4 * 8 + half * 4 + e % 4) * T::kVStride + col * 4;
+#pragma unroll
+                        for (int d = 0; d < DB; ++d)
+                            acc[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(*reinterpret_cast<const float*>(at + d * 128),
+                                                                          p[e], acc[d], 0, 0, 0);
+                    }
+                }
+            });
+        };
+        auto list_tile = [&](int buf, int from) __attribute__((always_inline)) {
+            const int left = n - from;
+            if (left > 0 && !idle) tile(buf, left < T::kKeys, left >= 64 ? ~0ull : (1ull << left) - 1ull);
+        };
+        auto node_tile = [&](int from, bool infinite) __attribute__((always_inline)) {
+            if (from >= nodes || idle) return;
+            tile(0, true, sees >> from);
+            if (infinite) {
+                // values that are not finite, from memory, to the rows that see their node
+                for (int key = from; key < min(nodes, from + T::kKeys); ++key) {
+                    const char* at = vn + (size_t)key * a.v_stride + half * 4 * T::kElem;
+#pragma unroll
+                    for (int d = 0; d < DB; ++d)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const char* e = at + (d * 32 + i / 4 * 8 + i % 4) * T::kElem;
+                            float v;
+                            if constexpr (BF16) v = (float)*reinterpret_cast<const __bf16*>(e);
+                            else v = *reinterpret_cast<const float*>(e);
+                            if ((sees >> key & 1) && !(fabsf(v) < INFINITY)) acc[d][i] += v;
+                        }
+                }
+            }
+        };
+
+        // list tiles [l0, l1) of the workgroup's steps; those of nodes come first
+        const int l0 = max(t0, node_tiles) - node_tiles, l1 = t1 - node_tiles;
+        if constexpr (T::kSplit) {
+            request_entries(l0 * KW + wave);
+            request();
+            request_entries((l0 + 1) * KW + wave);
+            for (int j = t0; j < min(t1, node_tiles); ++j) {
+                const bool infinite = __any(keep_nodes(j * T::kStep + wave * T::kKeys));
+                __builtin_amdgcn_wave_barrier();
+                node_tile(j * T::kStep + wave * T::kKeys, infinite);
+                __builtin_amdgcn_wave_barrier();
+            }
+            for (int j = l0; j < l1; ++j) {
+                keep(0);
+                __builtin_amdgcn_wave_barrier();
+                request();
+                request_entries((j + 2) * KW + wave);
+                list_tile(0, (j * KW + wave) * T::kKeys);
+                __builtin_amdgcn_wave_barrier();
+            }
+        } else {
+            request_entries(l0);
+            request();
+            request_entries(l0 + 1);
+            for (int j = t0; j < min(t1, node_tiles); ++j) {
+                if (threadIdx.x == 0) infinite_lds = 0;
+                __syncthreads();
+                if (keep_nodes(j * T::kStep)) infinite_lds = 1;
+                __syncthreads();
+                node_tile(j * T::kStep + key0, infinite_lds != 0);
+                __syncthreads();
+            }
+            if (l0 < l1) {
+                keep(l0 & 1);
+                request();
+                request_entries(l0 + 2);
+            }
+            for (int j = l0; j < l1; ++j) {
+                __syncthreads();                          // tile j is in place, tile j - 1 has been read
+                if (j + 1 < l1) {
+                    keep((j + 1) & 1);
+                    request();
+                    request_entries(j + 3);
+                }
+                list_tile(j & 1, j * T::kStep + key0);
+            }
+        }
+
+        // ---- the waves' states together, and the outputs or the partial ----
+        {
+            const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
+            l = __uint_as_float(y[0]) + __uint_as_float(y[1]);
+        }
+        const int first_slot = deal.aligned ? wave_uniform(pc.slot) - part : 2 * (w - part);
+        auto slot_of = [&](int k) __attribute__((always_inline)) {
+            return deal.aligned ? first_slot + k : first_slot + (k ? 2 * k : 1);
+        };
+        float* my_acc = a.part_acc + (size_t)slot_of(part) * T::kRows * D;
+        float* my_ml = a.part_ml + (size_t)slot_of(part) * 2 * T::kRows;
+        // four dims of row r of the block, with the row's sum
+        auto write = [&](int r, int quad, floatx4 o, float sum) __attribute__((always_inline)) {
+            if (r >= live_rows) return;
+            const float inv = sum == 0.f ? 0.f : 1.f / sum;       // nothing seen: zeros
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] *= inv;
+            const int at = r0 + r;
+            char* to = a.out + (((size_t)b * a.N + (at >> group_shift)) * a.Hq + kvh * G + (at & (G - 1))) * T::kRow + quad * 4 * T::kElem;
+            if constexpr (BF16) {
+                typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+                *reinterpret_cast<bf16x4*>(to) = __builtin_convertvector(o, bf16x4);
+            } else {
+                *reinterpret_cast<floatx4*>(to) = o;
+            }
+        };
+        const auto ra = buffer(my_acc, T::kRows * D * 4), rm = buffer(my_ml, 2 * T::kRows * 4);
+        auto finish = [&](int r, int quad, floatx4 o, float mx, float sum) __attribute__((always_inline)) {
+            if (n_parts == 1) {
+                write(r, quad, o, sum);
+                return;
+            }
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(uintx4, o), ra, (quad * T::kRows + r) * 16, 0, kAgentScope);
+            if (quad == 0) {
+                __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(mx), rm, r * 4, 0, kAgentScope);
+                __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(sum), rm, (T::kRows + r) * 4, 0, kAgentScope);
+            }
+        };
+        __syncthreads();                                  // every wave has read its tiles
+        if constexpr (T::kSplit) {
+            float* state = reinterpret_cast<float*>(tiles_lds);
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    *reinterpret_cast<floatx4*>(state + col * T::kState + d * 32 + i * 8 + half * 4) =
+                        floatx4{acc[d][i * 4], acc[d][i * 4 + 1], acc[d][i * 4 + 2], acc[d][i * 4 + 3]};
+            if (half == 0) {
+                ml_lds[wave * 64 + col] = m;
+                ml_lds[wave * 64 + 32 + col] = l;
+            }
+            __syncthreads();
+            for (int e = threadIdx.x; e < 32 * (D / 4); e += T::kThreads) {
+                const int r = e & 31, quad = e >> 5;
+                float M = -INFINITY, L = 0.f;
+#pragma unroll
+                for (int k = 0; k < KW; ++k) M = fmaxf(M, ml_lds[k * 64 + r]);
+                floatx4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int k = 0; k < KW; ++k) {
+                    const float f = weight(ml_lds[k * 64 + r], M, a.scale_log2);
+                    const floatx4 v = *reinterpret_cast<const floatx4*>(lds + k * T::kTiles + (r * T::kState + quad * 4) * 4);
+                    L = fmaf(f, ml_lds[k * 64 + 32 + r], L);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[i] = fmaf(f, v[i], o[i]);
+                }
+                finish(r, quad, o, M, L);
+            }
+        } else {
+            if constexpr (KW == 2) {
+                // the second halves' states, value by value in the same lanes
+                float* state = reinterpret_cast<float*>(lds) + row_wave * 64 * (D / 2 + 2) + lane;
+                if (key0) {
+#pragma unroll
+                    for (int d = 0; d < DB; ++d)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) state[(d * 16 + i) * 64] = acc[d][i];
+                    state[D / 2 * 64] = m;
+                    state[(D / 2 + 1) * 64] = l;
+                }
+                __syncthreads();
+                if (!key0) {
+                    const float m2 = state[D / 2 * 64], M = fmaxf(m, m2);
+                    const float f = weight(m, M, a.scale_log2), f2 = weight(m2, M, a.scale_log2);
+                    l = l * f + state[(D / 2 + 1) * 64] * f2;
+                    m = M;
+#pragma unroll
+                    for (int d = 0; d < DB; ++d)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) acc[d][i] = fmaf(state[(d * 16 + i) * 64], f2, acc[d][i] * f);
+                }
+            }
+            if (!key0) {
+#pragma unroll
+                for (int d = 0; d < DB; ++d)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)           // dims 32 d + 8 i + 4 half ..
+                        finish(row_wave * 32 + col, d * 8 + i * 2 + half,
+                               floatx4{acc[d][i * 4], acc[d][i * 4 + 1], acc[d][i * 4 + 2], acc[d][i * 4 + 3]}, m, l);
+            }
+        }
+        if (n_parts > 1) {
+            // the device-scope stores of every thread have completed before the ticket is
+            // taken, so no cache-wide write-back is needed
+            __builtin_amdgcn_s_waitcnt(0);
+            __syncthreads();
+            int* ticket = a.ticket + (size_t)b * a.Hkv * a.row_blocks + gi;
+            if (threadIdx.x == 0)
+                last_arrival = __hip_atomic_fetch_add(ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == n_parts - 1;
+            __syncthreads();
+            if (last_arrival) {
+                const int rows = min(T::kRows, live_rows);
+                for (int e = threadIdx.x; e < T::kRows * (D / 4); e += T::kThreads) {
+                    const int r = e % T::kRows, quad = e / T::kRows;
+                    if (r >= rows) continue;
+                    float M = -INFINITY, L = 0.f;
+                    floatx4 o = {0.f, 0.f, 0.f, 0.f};
+                    constexpr int kPass = 4;              // partials in flight
+                    for (int k0 = 0; k0 < n_parts; k0 += kPass) {
+                        float pm[kPass], pl[kPass];
+                        floatx4 po[kPass];
+#pragma unroll
+                        for (int u = 0; u < kPass; ++u) {
+                            const int slot = slot_of(min(k0 + u, n_parts - 1));
+                            const auto fa = buffer(a.part_acc + (size_t)slot * T::kRows * D, T::kRows * D * 4);
+                            const auto fm = buffer(a.part_ml + (size_t)slot * 2 * T::kRows, 2 * T::kRows * 4);
+                            pm[u] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(fm, r * 4, 0, kAgentScope));
+                            pl[u] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(fm, (T::kRows + r) * 4, 0, kAgentScope));
+                            po[u] = __builtin_bit_cast(floatx4, __builtin_amdgcn_raw_buffer_load_b128(fa, e * 16, 0, kAgentScope));
+                        }
+                        float Mn = M;
+#pragma unroll
+                        for (int u = 0; u < kPass; ++u)
+                            if (k0 + u < n_parts) Mn = fmaxf(Mn, pm[u]);
+                        const float f0 = weight(M, Mn, a.scale_log2);
+                        L *= f0;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) o[i] *= f0;
+#pragma unroll
+                        for (int u = 0; u < kPass; ++u) {
+                            if (k0 + u >= n_parts) continue;
+                            const float f = weight(pm[u], Mn, a.scale_log2);
+                            L = fmaf(f, pl[u], L);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) o[i] = fmaf(f, po[u][i], o[i]);
+                        }
+                        M = Mn;
+                    }
+                    write(r, quad, o, L);
+                }
+                if (threadIdx.x == 0) *ticket = 0;        // ready for the next launch
+            }
+        }
+        __syncthreads();                                  // the states have been read: tiles may be rewritten
+    }
+    }
+}
+
+struct DraftLaunch {
+    int blocks;
+    hipStream_t stream;
+    int* occupancy;                 // non-null: report it instead
+};
+
+template <int ROWS, int D, int RW, int KW>
+hipError_t launch_walk(const DraftArgs& args, const DraftLaunch& l) {
+    using T = Tile<ROWS, D, RW, KW>;
+    auto kernel = draft_kernel<ROWS, D, RW, KW>;
+    if (l.occupancy) return hipOccupancyMaxActiveBlocksPerMultiprocessor(l.occupancy, kernel, T::kThreads, 0);
+    DraftArgs a = args;
+    a.row_blocks = (a.N * (a.Hq / a.Hkv) + T::kRows - 1) / T::kRows;
+    const size_t lds = a.B > 64 ? (size_t)(2 * a.B + 1) * 4 : 0;
+    hipLaunchKernelGGL(kernel, dim3(l.blocks), dim3(T::kThreads), lds, l.stream, a);
+    return hipGetLastError();
+}
+
+template <int ROWS, int D>
+hipError_t launch_rows(const DraftArgs& a, int rows, const DraftLaunch& l) {
+    switch (rows) {
+        case 32: return launch_walk<ROWS, D, 1, 4>(a, l);
+        case 64: return launch_walk<ROWS, D, 2, 2>(a, l);
+        case 128: return launch_walk<ROWS, D, 4, 1>(a, l);
+        case 256: return launch_walk<ROWS, D, 8, 1>(a, l);
+    }
+    return hipErrorInvalidValue;
+}
+
+hipError_t dispatch(const DraftArgs& a, int rows_kind, int head_dim, int rows, const DraftLaunch& l) {
+    if (rows_kind == kRowsBF16) {
+        if (head_dim == 64) return launch_rows<kRowsBF16, 64>(a, rows, l);
+        if (head_dim == 128) return launch_rows<kRowsBF16, 128>(a, rows, l);
+        if (head_dim == 256) return launch_rows<kRowsBF16, 256>(a, rows, l);
+    } else if (rows_kind == kRowsFour) {
+        if (head_dim == 64) return launch_rows<kRowsFour, 64>(a, rows, l);
+        if (head_dim == 128) return launch_rows<kRowsFour, 128>(a, rows, l);
+        if (head_dim == 256) return launch_rows<kRowsFour, 256>(a, rows, l);
+    } else {
+        if (head_dim == 64) return launch_rows<kRowsF32, 64>(a, rows, l);
+        if (head_dim == 128) return launch_rows<kRowsF32, 128>(a, rows, l);
+    }
+    return hipErrorInvalidValue;
+}
+
+// ---- accepted nodes ----
+
+constexpr int kAcceptThreads = 256;
+
+// A workgroup copies the rows of one (layer, sequence); the last to finish extends every
+// sequence's lists and lengths, which all of them have read by then.
+template <bool FOUR>
+__global__ void __launch_bounds__(kAcceptThreads)
+accept_kernel(AcceptArgs a) {
+    __shared__ int path[kMaxDrafts];
+    __shared__ int last;
+    const int b = blockIdx.x, layer = blockIdx.y;
+    const int t = *a.t_dev;
+    // nodes taken: up to the first entry that names none, and none where the room is short
+    auto taken = [&](int seq, int n) __attribute__((always_inline)) {
+        int take = min(max(a.n_path[seq], 0), a.N);
+        for (int i = 0; i < take; ++i)
+            if ((uint32_t)a.path[(size_t)seq * a.N + i] >= (uint32_t)a.N) take = i;
+        return n + take > a.max_ctx ? -1 : take;
+    };
+    const int n = a.plen[b] + t;
+    const int take = max(taken(b, n), 0);
+    if ((int)threadIdx.x < take) path[threadIdx.x] = a.path[(size_t)b * a.N + threadIdx.x];
+    __syncthreads();
+    const int per_head = a.head_bytes / 16, per_token = per_head * a.Hkv;     // powers of two
+    const int head_shift = __ffs(per_head) - 1, token_shift = __ffs(per_token) - 1;
+    const int pool_bytes = FOUR ? a.head_bytes / 4 : a.head_bytes;
+    const char* k = a.k + (size_t)layer * a.k_layer + (size_t)b * a.N * a.k_stride;
+    const char* v = a.v + (size_t)layer * a.v_layer + (size_t)b * a.N * a.v_stride;
+    const size_t row0 = ((size_t)layer * a.B + b) * a.Hkv * a.pool_rows + n;
+    for (int u = threadIdx.x; u < take << token_shift; u += kAcceptThreads) {
+        const int i = u >> token_shift, e = u & (per_token - 1);
+        const int g = e >> head_shift, p = e & (per_head - 1);
+        const uintx4 x = *reinterpret_cast<const uintx4*>(k + (size_t)path[i] * a.k_stride + e * 16);
+        const uintx4 y = *reinterpret_cast<const uintx4*>(v + (size_t)path[i] * a.v_stride + e * 16);
+        const size_t row = row0 + (size_t)g * a.pool_rows + i, at = row * pool_bytes;
+        if constexpr (FOUR) {
+            const bool of_64 = per_head == 8;
+            uint32_t ks, vs;
+            *reinterpret_cast<uint32_t*>(a.kpool + at + p * 4) = round8(x, of_64, ks);
+            *reinterpret_cast<uint32_t*>(a.vpool + at + p * 4) = round8(y, of_64, vs);
+            const size_t to = (row * per_head + p) / 4;           // the first of the lanes' groups
+            if (of_64 && p == 0) {
+                *reinterpret_cast<uint16_t*>(a.kscale + to) = (uint16_t)ks;
+                *reinterpret_cast<uint16_t*>(a.vscale + to) = (uint16_t)vs;
+            } else if (!of_64 && p % 16 == 0) {
+                *reinterpret_cast<uint32_t*>(a.kscale + to) = ks;
+                *reinterpret_cast<uint32_t*>(a.vscale + to) = vs;
+            }
+        } else {
+            *reinterpret_cast<uintx4*>(a.kpool + at + p * 16) = x;
+            *reinterpret_cast<uintx4*>(a.vpool + at + p * 16) = y;
+        }
+    }
+    __syncthreads();                              // n and take have been read by every thread
+    if (threadIdx.x == 0)
+        last = __hip_atomic_fetch_add(a.ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (int)(gridDim.x * gridDim.y) - 1;
+    __syncthreads();
+    if (!last) return;
+    unsigned long long more = 0;
+    for (int i = threadIdx.x; i < a.states * a.B; i += kAcceptThreads) {
+        const int seq = i % a.B, len = a.plen[seq] + t, grow = taken(seq, len);
+        if (grow < 0) a.flags[1] = 1;
+        if (grow <= 0) continue;
+        const int na = a.n_active[i];             // the last entry is the next token's position, len
+        for (int j = 1; j <= grow; ++j) a.list[(size_t)i * a.cap + na - 1 + j] = len + j;
+        a.n_active[i] = na + grow;
+        more += grow;
+    }
+    if (more) atomicAdd(a.listed_total, more);
+    __syncthreads();                              // every list has been extended from the old lengths
+    for (int seq = threadIdx.x; seq < a.B; seq += kAcceptThreads) {
+        const int grow = taken(seq, a.plen[seq] + t);
+        if (grow > 0) a.plen[seq] += grow;
+    }
+    if (threadIdx.x == 0) *a.ticket = 0;          // ready for the next launch
+}
+
+}  // namespace
+
+int draft_rows(int n, int group) {
+    const int rows = n * group;
+    return rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
+}
+
+hipError_t draft_occupancy(int rows_kind, int head_dim, int rows, int* blocks_per_cu) {
+    return dispatch(DraftArgs{}, rows_kind, head_dim, rows, DraftLaunch{0, nullptr, blocks_per_cu});
+}
+
+hipError_t launch_drafts(const DraftArgs& args, int rows_kind, int head_dim, int blocks, hipStream_t s) {
+    DraftArgs a = args;
+    a.scale_log2 = (float)(1.4426950408889634 / __builtin_sqrt((double)head_dim));
+    a.lazy = kLazy / a.scale_log2;
+    return dispatch(a, rows_kind, head_dim, draft_rows(a.N, a.Hq / a.Hkv), DraftLaunch{blocks, s, nullptr});
+}
+
+hipError_t launch_accept(const AcceptArgs& a, hipStream_t s) {
+    const dim3 grid(a.B, a.L);
+    if (a.four) hipLaunchKernelGGL(accept_kernel<true>, grid, dim3(kAcceptThreads), 0, s, a);
+    else hipLaunchKernelGGL(accept_kernel<false>, grid, dim3(kAcceptThreads), 0, s, a);
+    return hipGetLastError();
+}
+
+}  // namespace asrkf

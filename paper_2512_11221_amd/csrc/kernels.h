@@ -238,6 +238,103 @@ struct RowsArgs {
     int32_t head_bytes;       // one token, one KV head, of k and v
 };
 
+// Rotary positions (rotate.hip): rows of queries and keys turned by their positions.
+constexpr int kMaxPairs = 128;
+struct RotateArgs {
+    const char* x[2];         // [n][heads][D], rows x_stride bytes apart (16-byte aligned, as the strides)
+    char* y[2];               // the same, y_stride apart; may be x
+    int64_t x_stride[2], y_stride[2];
+    int32_t heads[2];         // 0: no such rows
+    const int32_t* pos;       // [n], or null: all 0
+    const int32_t* plen;      // rows_per_seq > 0: row i's position is plen[i / rows_per_seq] + *t_dev +
+    const int32_t* t_dev;     //   t_offset + pos[i]; else pos[i]
+    int32_t t_offset, rows_per_seq;
+    int32_t n, D, pairs;      // pairs of values that are turned, the first of a head
+    int32_t in_pairs;         // 0: value i goes with i + pairs, 1: 2 i with 2 i + 1
+    int32_t rows_per_block;   // set for the launch
+    uint32_t head_magic;      // ceil(2^32 / (heads of both))
+    double magnitude;
+    double turns[kMaxPairs];  // turns per position of each pair, negative for the inverse
+};
+
+// Drafted tokens (draft.hip, verify.hip): at most kMaxDrafts to a sequence, one bit each.
+constexpr int kMaxDrafts = 64;
+struct DraftArgs {
+    const char* q;            // [B][N][Hq][D], tokens q_stride bytes apart
+    const char* k;            // [B][N][Hkv][D]
+    const char* v;
+    char* out;                // [B][N][Hq][D], dense
+    int64_t q_stride, k_stride, v_stride;
+    const uint64_t* sees;     // [B][N] bit j: node j is attended
+    const int32_t* count;     // [B] nodes of each sequence, or null: N
+    const char* kpool;        // layer base, as AttnArgs
+    const char* vpool;
+    const uint8_t* kscale;
+    const uint8_t* vscale;
+    const int32_t* list;      // layer base, [B][cap]
+    const int32_t* n_active;  // layer base, [B]
+    int32_t list_tail;        // entries at a list's end whose rows are not written: 0 or 1
+    float* part_acc;          // [slots][D / 4][rows][4] of the pairs that several workgroups share
+    float* part_ml;           // [slots][2][rows]
+    int32_t* ticket;          // [B][pairs of a sequence], zero between launches
+    int32_t B, N, cap, Hq, Hkv, pool_rows;
+    int32_t grid;             // workgroups the work is dealt to
+    int32_t row_blocks;       // blocks of query rows of a (sequence, KV head) (set for the launch)
+    float scale_log2, lazy;
+};
+// Accepted nodes' rows of every layer into the cache, and the sequences grown by them.
+struct AcceptArgs {
+    const char* k;            // [L][B][N][Hkv][D], layers and tokens so many bytes apart
+    const char* v;
+    int64_t k_stride, v_stride, k_layer, v_layer;
+    const int32_t* path;      // [B][N] nodes, in order
+    const int32_t* n_path;    // [B]
+    char* kpool;              // [L][B][Hkv][pool_rows][row of the cache]
+    char* vpool;
+    uint8_t* kscale;
+    uint8_t* vscale;
+    int32_t* plen;            // [B] grown
+    const int32_t* t_dev;
+    int32_t* list;            // [states][B][cap] extended
+    int32_t* n_active;
+    unsigned long long* listed_total;
+    int32_t* flags;           // [1]: a sequence would pass max_ctx
+    int32_t* ticket;          // zero between launches
+    int32_t L, B, N, Hkv, pool_rows, head_bytes, four, cap, states, max_ctx;
+};
+// Verification of drafted tokens (verify.hip).
+constexpr int kVerifySplitMax = 64;
+struct VerifyPart {           // of a row of logits: sum of e^((x - m) / T), maximum, its lowest index
+    double S;
+    float m;
+    int32_t at;               // -1: a NaN, an infinity, or nothing above -inf
+};
+struct VerifyEnd {            // where a sequence's walk has ended
+    double scale, c;          // weights are max(e^((x - m) / T) scale - c q, 0)
+    double c_before;          // c where that leaves nothing, or -1
+    float m;
+    int32_t row;              // 0 the root's, 1 + i node i's; -1: nothing to draw from
+    uint64_t rejected;        // nodes whose tokens weigh 0
+};
+struct VerifyArgs {
+    const int32_t* tokens;    // [B][N]
+    const int32_t* parents;   // [B][N]
+    const int32_t* count;     // [B] or null
+    const float* root;        // [B][V]
+    const float* logits;      // [B][N][V]
+    const float* probs;       // [B][N][V] or null
+    const float* u;           // [B][N + 1]
+    int32_t* path;            // [B][N] (written)
+    int32_t* n_path;          // [B]
+    int32_t* next;            // [B]
+    VerifyPart* part;         // [B][N + 1][split]
+    VerifyEnd* end;           // [B]
+    double* sums;             // [B][split]
+    int32_t* ticket;          // [B], zero between launches
+    int32_t B, N, V, split;
+    double inv_t;             // log2(e) / temperature; 0: greedy
+};
+
 // Row copies between the device cache and the host store (spill mode).
 struct XferArgs {
     char* kpool;              // [L][B][Hkv][pool_rows][row_bytes / Hkv]
@@ -299,5 +396,15 @@ hipError_t launch_prefill(const PrefillArgs& a, hipStream_t s);
 hipError_t launch_prompt_store(const PromptArgs& a, const PromptBatch& b, hipStream_t s);
 hipError_t launch_prompt_attention(const PromptArgs& a, const PromptBatch& b, int bf16, int head_dim, hipStream_t s);
 hipError_t launch_get_rows(const RowsArgs& a, bool four, hipStream_t s);
+hipError_t launch_rotate(const RotateArgs& a, int bf16, hipStream_t s);
+// Query rows of a workgroup that attends drafts of n nodes, and workgroups of that kind
+// that a CU holds.
+int draft_rows(int n, int group);
+hipError_t draft_occupancy(int rows_kind, int head_dim, int rows, int* blocks_per_cu);
+hipError_t launch_drafts(const DraftArgs& a, int rows_kind, int head_dim, int blocks, hipStream_t s);
+hipError_t launch_accept(const AcceptArgs& a, hipStream_t s);
+// Workgroups of a row of logits.
+int verify_split(int rows, int V);
+hipError_t launch_verify(const VerifyArgs& a, hipStream_t s);
 
 }  // namespace asrkf

@@ -21,34 +21,10 @@
 
 #include "kernels.h"
 #include "rows.h"
+#include "tiles.h"
 
 namespace asrkf {
 namespace {
-
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef float floatx4 __attribute__((ext_vector_type(4)));
-typedef float floatx16 __attribute__((ext_vector_type(16)));
-typedef int intx4 __attribute__((ext_vector_type(4)));
-typedef unsigned uintx4 __attribute__((ext_vector_type(4)));
-typedef short shortx4 __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) shortx4* lds_shortx4;
-
-constexpr int kBufferFlags = 0x00020000;      // raw buffer, 32-bit data
-
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const void* p, int bytes) {
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), (short)0, bytes, kBufferFlags);
-}
-__device__ __forceinline__ intx4 load16(__amdgpu_buffer_rsrc_t r, int off) {
-    return __builtin_bit_cast(intx4, __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0));
-}
-
-template <int N, typename F>
-__device__ __forceinline__ void unroll(F f) {
-    if constexpr (N > 0) {
-        unroll<N - 1>(f);
-        f(std::integral_constant<int, N - 1>{});
-    }
-}
 
 // The sequence of the batch whose units (given by their first ones) hold unit x: one
 // round trip to the table, a sequence per lane.
@@ -64,25 +40,6 @@ __device__ __forceinline__ int find_sequence(const int32_t* first, int n, int x)
 // ---- the rows into the cache ----
 
 constexpr int kStoreThreads = 256;
-
-// Eight values of a row, whose group's others the lane's three neighbours hold, as
-// codes, and (lanes at the start of a row's 16, or of rows of 64 values at the start of
-// its 8) the scale bytes of those lanes' groups.
-__device__ __forceinline__ uint32_t round8(uintx4 x, bool rows_of_64, uint32_t& scales) {
-    uint32_t top = max_magnitude(max_magnitude(x[0], x[1]), max_magnitude(x[2], x[3]));
-    top = max(top & 0xFFFFu, top >> 16);
-    top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0xB1, 0xF, 0xF, false));   // quad_perm [1,0,3,2]
-    top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0x4E, 0xF, 0xF, false));   // quad_perm [2,3,0,1]
-    const uint32_t byte = scale_byte(top);
-    scales = byte << (threadIdx.x / 4 & (rows_of_64 ? 1 : 3)) * 8;
-    if (rows_of_64) {
-        scales |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)scales, 0x141, 0xF, 0xF, false);     // row_half_mirror
-    } else {
-        scales |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)scales, 0x124, 0xF, 0xF, false);     // row_ror 4
-        scales |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)scales, 0x128, 0xF, 0xF, false);     // row_ror 8
-    }
-    return encode8(x[0], x[1], x[2], x[3], scale_value(byte));
-}
 
 // Packed rows [T][Hkv][D] into the head-major cache, a workgroup per kPromptStoreTokens
 // tokens of a sequence.  A thread takes 16 bytes of K and of V at a time, several in
@@ -222,24 +179,6 @@ struct Tile {
     static_assert(!kHalved || kRowWaves * 64 * (D / 2 + 2) * 4 <= kLds, "the states of half the waves fit the tiles");
     static_assert(!kSplits || 32 * kState * 4 <= kTiles, "a wave's state fits its tile");
 };
-
-// x with 0 in the place of infinities and NaNs; bad says whether there were any
-template <bool BF16>
-__device__ __forceinline__ intx4 finite_part(intx4 x, bool& bad) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if constexpr (BF16) {
-            const bool lo = (x[i] & 0x7F80) == 0x7F80, hi = (x[i] & 0x7F800000) == 0x7F800000;
-            bad |= lo || hi;
-            x[i] &= (lo ? 0 : 0xFFFF) | (hi ? 0 : (int)0xFFFF0000);
-        } else {
-            const bool is = (x[i] & 0x7F800000) == 0x7F800000;
-            bad |= is;
-            x[i] = is ? 0 : x[i];
-        }
-    }
-    return x;
-}
 
 // The rescaling of O waits until a row's maximum has grown by 2^kLazy; weights are
 // 2^(x - m - kLazy - b) with 2^b >= twice the keys that a workgroup's rows see, so that no

@@ -27,6 +27,7 @@ constexpr int kScaleGroup = 32;
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef unsigned short ushortx2 __attribute__((ext_vector_type(2)));
+typedef unsigned uintx4 __attribute__((ext_vector_type(4)));
 
 // the larger magnitudes of two pairs of bf16, as bits
 __device__ __forceinline__ uint32_t max_magnitude(uint32_t a, uint32_t b) {
@@ -57,6 +58,25 @@ __device__ __forceinline__ uint32_t encode8(uint32_t a, uint32_t b, uint32_t c, 
 template <int SEL>
 __device__ __forceinline__ uint32_t decode2(uint32_t codes, float scale) {
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, SEL));
+}
+
+// Eight values of a row, whose group's others the lane's three neighbours hold, as
+// codes, and (lanes at the start of a row's 16, or of rows of 64 values at the start of
+// its 8) the scale bytes of those lanes' groups.
+__device__ __forceinline__ uint32_t round8(uintx4 x, bool rows_of_64, uint32_t& scales) {
+    uint32_t top = max_magnitude(max_magnitude(x[0], x[1]), max_magnitude(x[2], x[3]));
+    top = max(top & 0xFFFFu, top >> 16);
+    top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0xB1, 0xF, 0xF, false));   // quad_perm [1,0,3,2]
+    top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0x4E, 0xF, 0xF, false));   // quad_perm [2,3,0,1]
+    const uint32_t byte = scale_byte(top);
+    scales = byte << (threadIdx.x / 4 & (rows_of_64 ? 1 : 3)) * 8;
+    if (rows_of_64) {
+        scales |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)scales, 0x141, 0xF, 0xF, false);     // row_half_mirror
+    } else {
+        scales |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)scales, 0x124, 0xF, 0xF, false);     // row_ror 4
+        scales |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)scales, 0x128, 0xF, 0xF, false);     // row_ror 8
+    }
+    return encode8(x[0], x[1], x[2], x[3], scale_value(byte));
 }
 
 }  // namespace asrkf

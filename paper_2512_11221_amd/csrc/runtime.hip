@@ -20,6 +20,8 @@
 // a host-store flag, the device row of every listed position, a stack of
 // free rows and the out/in copy lists; and a pinned host store
 // [L][B][cap][Hkv][D] for K and V, written once per token.
+// Drafted tokens (asrkf_reserve_drafts): one workspace with the attention's partials, the
+// parts of the logits' rows, and the tickets.
 #include <math.h>
 #include <stdarg.h>
 #include <stdio.h>
@@ -203,6 +205,25 @@ struct asrkf_ctx {
     int side_delay_us = 0;              // test hook: side stream waits before its copies
     int device = 0;
     void* static_scratch = nullptr;     // this device's address of the static partials array
+
+    // rotary positions and drafted tokens
+    bool rotary = false;
+    RotateArgs rotate{};                // pairs, layout, turns and magnitude
+    int draft_nodes = 0;                // nodes of a sequence that there is room for
+    int draft_grid[4] = {0, 0, 0, 0};   // attention workgroups resident at once, by 32, 64, 128, 256 rows
+    int cus = 0;
+    void* draft_space = nullptr;        // one allocation:
+    int32_t* draft_ticket = nullptr;    // [B][Hkv][2] (zero between launches)
+    int32_t* accept_ticket = nullptr;
+    int32_t* verify_ticket = nullptr;   // [B]
+    VerifyPart* verify_part = nullptr;  // [B][nodes + 1][kVerifySplitMax]
+    VerifyEnd* verify_end = nullptr;    // [B]
+    double* verify_sums = nullptr;      // [B][kVerifySplitMax]
+    float* draft_acc = nullptr;
+    float* draft_ml = nullptr;
+    bool accepted = false;              // asrkf_accept_drafts was called: the lengths grow on the device,
+    bool accept_captured = false;       // by a graph's replays too
+    std::vector<int32_t> plen_most;     // ... and are at most these (plen_host: as last read back)
 };
 
 namespace {
@@ -250,7 +271,7 @@ void free_all(asrkf_ctx* ctx) {
     void* ptrs[] = {ctx->kpool, ctx->vpool, ctx->kscale, ctx->vscale, ctx->unfreeze, ctx->count, ctx->flag, ctx->list, ctx->small,
                     ctx->part_acc, ctx->rel, ctx->rel_sum, ctx->row_of, ctx->on_host, ctx->list_row, ctx->last_row,
                     ctx->row_owner, ctx->pop_buf, ctx->out_pos, ctx->out_row, ctx->in_pos, ctx->in_row,
-                    ctx->hmask, ctx->hlast, ctx->seg_count};
+                    ctx->hmask, ctx->hlast, ctx->seg_count, ctx->draft_space};
     for (void* p : ptrs) if (p) (void)hipFree(p);
     void* host[] = {ctx->khost, ctx->vhost, ctx->flags_host};
     for (void* p : host) if (p) (void)hipHostFree(p);
@@ -458,6 +479,7 @@ asrkf_status asrkf_init(const asrkf_config* cfg, asrkf_ctx** out) {
     ctx->row_bytes = (size_t)c.n_kv_heads * (ctx->four ? c.head_dim / 2 : c.head_dim * ctx->esz);
     ctx->scale_bytes = ctx->four ? (size_t)c.n_kv_heads * c.head_dim / kScaleGroup : 0;
     ctx->plen_host.assign(c.batch, 0);
+    ctx->plen_most.assign(c.batch, 0);
     ctx->prefilled.assign(c.batch, 0);
 
     hipError_t e = hipGetDevice(&ctx->device);
@@ -489,6 +511,7 @@ asrkf_status asrkf_init(const asrkf_config* cfg, asrkf_ctx** out) {
             return fail(ASRKF_EINVAL, "attention workgroup does not fit on a CU for this shape");
         }
         ctx->grid = per_cu * prop.multiProcessorCount;
+        ctx->cus = prop.multiProcessorCount;
     }
     ctx->planes = c.relevance == ASRKF_REL_SOFTMAX ? c.n_q_heads : c.n_kv_heads;
     ctx->dur_len = c.max_ctx + 2;
@@ -683,7 +706,7 @@ asrkf_status asrkf_prefill(asrkf_ctx* ctx, int32_t layer, int32_t seq, const voi
         one.seq[0] = seq;
         HIP_OK(ctx, launch_prompt_store(p, one, s));
         ctx->prefilled[seq] = 1;
-        ctx->plen_host[seq] = n_tokens;
+        ctx->plen_host[seq] = ctx->plen_most[seq] = n_tokens;
         mark_queued(ctx, s, capturing(s));
         return ASRKF_OK;
     }
@@ -713,7 +736,7 @@ asrkf_status asrkf_prefill(asrkf_ctx* ctx, int32_t layer, int32_t seq, const voi
     }
     HIP_OK(ctx, launch_prefill(p, s));
     ctx->prefilled[seq] = 1;
-    ctx->plen_host[seq] = n_tokens;
+    ctx->plen_host[seq] = ctx->plen_most[seq] = n_tokens;
     mark_queued(ctx, s, capturing(s));
     return ASRKF_OK;
 }
@@ -806,7 +829,7 @@ asrkf_status asrkf_prefill_packed(asrkf_ctx* ctx, int32_t layer, int32_t n_seqs,
     }
     for (int i = 0; i < n_seqs; ++i) {
         ctx->prefilled[seqs[i]] = 1;
-        ctx->plen_host[seqs[i]] = n_tokens[i];
+        ctx->plen_host[seqs[i]] = ctx->plen_most[seqs[i]] = n_tokens[i];
     }
     mark_queued(ctx, s, capturing(s));
     return ASRKF_OK;
@@ -994,6 +1017,41 @@ asrkf_status check_overflow(asrkf_ctx* ctx, bool synced) {
 
 namespace {
 
+// Everything the context queued: its calls are ordered on last_stream (a call
+// on a new stream waits for the previous one), except the spill-mode copies
+// on the side stream, which the next decode_step waits for.
+// Steps replayed from a captured graph advance only the device's step
+// counter: after the wait the host adopts it (the counter counts steps
+// started, so a step in progress is not yet complete).
+asrkf_status sync_ctx(asrkf_ctx* ctx) {
+    if (!ctx->captured) {
+        // the status block comes back behind the queued work: one wait for both
+        HIP_OK(ctx, hipMemcpyAsync(&ctx->status_host, ctx->status, sizeof(Status), hipMemcpyDeviceToHost, ctx->last_stream));
+        HIP_OK(ctx, hipStreamSynchronize(ctx->last_stream));
+    } else {
+        // last_stream may be the stream of the capture, where the replays do not run: the
+        // blocking copy is ordered after the default stream and every stream that follows it
+        HIP_OK(ctx, hipStreamSynchronize(ctx->last_stream));
+        HIP_OK(ctx, hipMemcpy(&ctx->status_host, ctx->status, sizeof(Status), hipMemcpyDeviceToHost));
+    }
+    if (ctx->side) HIP_OK(ctx, hipStreamSynchronize(ctx->side));
+    const int completed = ctx->status_host.t - (ctx->next_layer != 0 ? 1 : 0);
+    if (completed > ctx->t) ctx->t = completed;
+    if (ctx->accepted && ctx->lists_ready) {      // the lengths grow on the device
+        HIP_OK(ctx, hipMemcpy(ctx->plen_host.data(), ctx->plen, ctx->plen_host.size() * 4, hipMemcpyDeviceToHost));
+        ctx->plen_most = ctx->plen_host;
+    }
+    return ASRKF_OK;
+}
+
+// The lengths as the device has them, where the host knows only how far accepted drafts may have
+// taken them.  Waits.
+asrkf_status learn_lengths(asrkf_ctx* ctx) {
+    if (!ctx->accepted) return ASRKF_OK;
+    asrkf_status st = sync_ctx(ctx);
+    return st == ASRKF_OK ? check_overflow(ctx, true) : st;
+}
+
 // The verdicts of the layers before layer_end whose planes are kept, and with e
 // the entropy monitors.
 hipError_t launch_verdicts(const asrkf_ctx* ctx, int layer_end, const EntropyArgs* e, hipStream_t s) {
@@ -1043,12 +1101,17 @@ asrkf_status decode_step_impl(asrkf_ctx* ctx, int32_t layer, const void* q, cons
     if (!q || !k_new || !v_new || !out) return fail(ASRKF_EINVAL, "null argument");
     if (!aligned16(q) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(out))
         return fail(ASRKF_EINVAL, "q, k_new, v_new and out must be 16-byte aligned");
-    const int t = ctx->t + 1;
-    for (int b = 0; b < c.batch; ++b)
-        if (ctx->plen_host[b] + t > c.max_ctx)
-            return fail(ASRKF_ECAPACITY, "sequence %d would exceed max_ctx=%d", b, c.max_ctx);
     hipStream_t s = static_cast<hipStream_t>(stream);
     const bool capture = capturing(s);
+    for (int b = 0; b < c.batch; ++b) {
+        if (ctx->plen_most[b] + ctx->t + 1 > c.max_ctx && layer == 0 && !capture) {
+            st = learn_lengths(ctx);      // accepted drafts may have been fewer
+            if (st != ASRKF_OK) return st;
+        }
+        if (ctx->plen_most[b] + ctx->t + 1 > c.max_ctx)
+            return fail(ASRKF_ECAPACITY, "sequence %d would exceed max_ctx=%d", b, c.max_ctx);
+    }
+    const int t = ctx->t + 1;
     if (capture && (ctx->spill || !ctx->lists_ready))
         return fail(ASRKF_ESTATE, ctx->spill ? "spill-mode steps cannot be captured in a graph"
                                              : "capture a step only after the first decode step");
@@ -1058,10 +1121,10 @@ asrkf_status decode_step_impl(asrkf_ctx* ctx, int32_t layer, const void* q, cons
     mark_queued(ctx, s, capture);
     if (layer == 0) {
         if (ctx->four)
-            attention_layout(ctx->plen_host.data(), c.batch, t, c.n_kv_heads, four_tile(c.head_dim), four_room(c.head_dim), ctx->grid,
+            attention_layout(ctx->plen_most.data(), c.batch, t, c.n_kv_heads, four_tile(c.head_dim), four_room(c.head_dim), ctx->grid,
                              &ctx->heads_per_group, &ctx->launch);
         else
-            attention_layout(ctx->plen_host.data(), c.batch, t, c.n_kv_heads, (int)(c.head_dim * ctx->esz), ctx->grid,
+            attention_layout(ctx->plen_most.data(), c.batch, t, c.n_kv_heads, (int)(c.head_dim * ctx->esz), ctx->grid,
                              &ctx->heads_per_group, &ctx->launch);
         if (capture) ctx->launch = ctx->grid;    // replayed at later, longer steps
     }
@@ -1208,29 +1271,6 @@ asrkf_status asrkf_restore(asrkf_ctx* ctx, const float* logits, int32_t mode, vo
 
 namespace {
 
-// Everything the context queued: its calls are ordered on last_stream (a call
-// on a new stream waits for the previous one), except the spill-mode copies
-// on the side stream, which the next decode_step waits for.
-// Steps replayed from a captured graph advance only the device's step
-// counter: after the wait the host adopts it (the counter counts steps
-// started, so a step in progress is not yet complete).
-asrkf_status sync_ctx(asrkf_ctx* ctx) {
-    if (!ctx->captured) {
-        // the status block comes back behind the queued work: one wait for both
-        HIP_OK(ctx, hipMemcpyAsync(&ctx->status_host, ctx->status, sizeof(Status), hipMemcpyDeviceToHost, ctx->last_stream));
-        HIP_OK(ctx, hipStreamSynchronize(ctx->last_stream));
-    } else {
-        // last_stream may be the stream of the capture, where the replays do not run: the
-        // blocking copy is ordered after the default stream and every stream that follows it
-        HIP_OK(ctx, hipStreamSynchronize(ctx->last_stream));
-        HIP_OK(ctx, hipMemcpy(&ctx->status_host, ctx->status, sizeof(Status), hipMemcpyDeviceToHost));
-    }
-    if (ctx->side) HIP_OK(ctx, hipStreamSynchronize(ctx->side));
-    const int completed = ctx->status_host.t - (ctx->next_layer != 0 ? 1 : 0);
-    if (completed > ctx->t) ctx->t = completed;
-    return ASRKF_OK;
-}
-
 asrkf_status collect_timing(asrkf_ctx* ctx) {
     for (auto& ev : ctx->ev_used) {
         float ms = 0.f;
@@ -1247,6 +1287,472 @@ asrkf_status collect_timing(asrkf_ctx* ctx) {
 }  // namespace
 
 extern "C" {
+
+// ---- rotary positions ----
+
+asrkf_status asrkf_rotary_table(const asrkf_rotary* r, int32_t head_dim, double* out) {
+    if (!r || !out) return fail(ASRKF_EINVAL, "null argument");
+    if (r->dim < 16 || r->dim % 16 || r->dim > head_dim || head_dim > 2 * kMaxPairs)
+        return fail(ASRKF_EINVAL, "rotary dim must be a multiple of 16 up to head_dim = %d", head_dim);
+    if (!(r->base > 1.0) || isinf(r->base)) return fail(ASRKF_EINVAL, "rotary base must be finite and above 1");
+    if (r->layout != ASRKF_ROT_HALVES && r->layout != ASRKF_ROT_PAIRS) return fail(ASRKF_EINVAL, "unknown rotary layout");
+    if (r->scaling < ASRKF_SCALE_NONE || r->scaling > ASRKF_SCALE_RAMP) return fail(ASRKF_EINVAL, "unknown rotary scaling");
+    if (!(r->magnitude > 0.0) || isinf(r->magnitude)) return fail(ASRKF_EINVAL, "rotary magnitude must be finite and above 0");
+    if (r->scaling != ASRKF_SCALE_NONE && (!(r->factor > 0.0) || isinf(r->factor)))
+        return fail(ASRKF_EINVAL, "rotary factor must be finite and above 0");
+    const bool by_turns = r->scaling == ASRKF_SCALE_BANDS || r->scaling == ASRKF_SCALE_RAMP;
+    if (by_turns && (r->original_ctx < 1 || !(r->low > 0.0) || !(r->high > r->low) || isinf(r->high)))
+        return fail(ASRKF_EINVAL, "bands and ramp need original_ctx >= 1 and 0 < low < high");
+    const double two_pi = 6.283185307179586476925;
+    const int pairs = r->dim / 2;
+    double from = 0.0, to = 0.0;
+    if (r->scaling == ASRKF_SCALE_RAMP) {
+        const auto pair_of = [&](double turns) { return pairs * log(r->original_ctx / (turns * two_pi)) / log(r->base); };
+        from = std::max(floor(pair_of(r->high)), 0.0);
+        to = std::min(ceil(pair_of(r->low)), (double)(r->dim - 1));
+    }
+    for (int i = 0; i < pairs; ++i) {
+        double f = pow(r->base, -2.0 * i / r->dim);
+        if (r->scaling == ASRKF_SCALE_LINEAR) {
+            f /= r->factor;
+        } else if (by_turns) {
+            double keep = r->scaling == ASRKF_SCALE_BANDS
+                              ? (r->original_ctx * f / two_pi - r->low) / (r->high - r->low)
+                              : 1.0 - (i - from) / (to > from ? to - from : 0.001);
+            keep = std::min(std::max(keep, 0.0), 1.0);
+            f *= keep + (1.0 - keep) / r->factor;
+        }
+        out[i] = f;
+    }
+    return ASRKF_OK;
+}
+
+asrkf_status asrkf_set_rotary(asrkf_ctx* ctx, const asrkf_rotary* r) {
+    asrkf_status st = check_ctx(ctx);
+    if (st != ASRKF_OK) return st;
+    double f[kMaxPairs];
+    st = asrkf_rotary_table(r, ctx->cfg.head_dim, f);
+    if (st != ASRKF_OK) return st;
+    ctx->rotary = true;
+    ctx->rotate.pairs = r->dim / 2;
+    ctx->rotate.in_pairs = r->layout == ASRKF_ROT_PAIRS ? 1 : 0;
+    ctx->rotate.magnitude = r->magnitude;
+    for (int i = 0; i < r->dim / 2; ++i) ctx->rotate.turns[i] = f[i] / 6.283185307179586476925;
+    return ASRKF_OK;
+}
+
+asrkf_status asrkf_rotate(asrkf_ctx* ctx, int32_t n_rows, int32_t rows_per_seq, const int32_t* pos, const void* q,
+                          int64_t q_stride, void* q_out, int64_t q_out_stride, const void* k, int64_t k_stride,
+                          void* k_out, int64_t k_out_stride, int32_t inverse, void* stream) {
+    TraceRange range("asrkf_rotate");
+    asrkf_status st = check_ctx(ctx);
+    if (st != ASRKF_OK) return st;
+    const asrkf_config& c = ctx->cfg;
+    if (!ctx->rotary) return fail(ASRKF_ESTATE, "asrkf_set_rotary comes first");
+    if (n_rows < 0 || n_rows > (1 << 28)) return fail(ASRKF_EINVAL, "n_rows must be in 0..2^28");
+    if (rows_per_seq < 0 || (rows_per_seq > 0 && (int64_t)rows_per_seq * c.batch != n_rows))
+        return fail(ASRKF_EINVAL, "n_rows must be rows_per_seq for every one of the %d sequences", c.batch);
+    if (rows_per_seq == 0 && !pos && n_rows > 0) return fail(ASRKF_EINVAL, "null positions");
+    if (!q != !q_out || !k != !k_out) return fail(ASRKF_EINVAL, "rows and their outputs go together");
+    if (!q && !k) return fail(ASRKF_EINVAL, "neither q nor k");
+    st = on_device(ctx);
+    if (st != ASRKF_OK) return st;
+    RotateArgs a = ctx->rotate;
+    const struct { const char* name; const void* x; int64_t xs; void* y; int64_t ys; int heads; } both[2] = {
+        {"q", q, q_stride, q_out, q_out_stride, c.n_q_heads}, {"k", k, k_stride, k_out, k_out_stride, c.n_kv_heads}};
+    struct Span { const void* p; size_t bytes; };
+    Span from[2] = {}, to[2] = {};
+    for (int i = 0; i < 2; ++i) {
+        const auto& r = both[i];
+        if (!r.x) continue;
+        const int64_t row = (int64_t)r.heads * c.head_dim * ctx->esz;
+        int64_t bytes[2];
+        for (int o = 0; o < 2; ++o) {
+            const int64_t stride = o ? r.ys : r.xs;
+            if (stride < 0 || stride > kMaxTokenStride) return fail(ASRKF_EINVAL, "%s: row stride out of range", r.name);
+            bytes[o] = stride ? stride * (int64_t)ctx->esz : row;
+            if (bytes[o] < row || bytes[o] % 16 || bytes[o] > kMaxTokenStride)
+                return fail(ASRKF_EINVAL, "%s: the row stride must be a multiple of 16 bytes from a token's row up to 16 MiB", r.name);
+            const void* p = o ? r.y : r.x;
+            if (n_rows == 0) continue;
+            if (!aligned16(p)) return fail(ASRKF_EINVAL, "%s and its output must be 16-byte aligned", r.name);
+            const size_t size = (size_t)(n_rows - 1) * bytes[o] + row;
+            bool inside;
+            if (!kernel_readable(ctx, p, size, &inside))
+                return fail(ASRKF_EINVAL, "%s and its output must be in memory of the context's device", r.name);
+            if (!inside) return fail(ASRKF_EINVAL, "%s or its output is smaller than %d rows", r.name, n_rows);
+            (o ? to : from)[i] = Span{p, size};
+        }
+        a.x[i] = static_cast<const char*>(r.x);
+        a.y[i] = static_cast<char*>(r.y);
+        a.x_stride[i] = bytes[0];
+        a.y_stride[i] = bytes[1];
+        a.heads[i] = r.heads;
+    }
+    if (n_rows == 0) return ASRKF_OK;
+    // Rows may be turned in place.  Else an output may share no memory with what is read or
+    // written beside it; interleaved slices of one buffer (equal strides) are told apart by row.
+    const auto apart = [&](const void* p, int64_t ps, size_t prow, size_t pn, const void* z, int64_t zs, size_t zrow, size_t zn) {
+        if (!overlap(p, pn, z, zn)) return true;
+        if (ps != zs) return false;
+        const int64_t d = (int64_t)(reinterpret_cast<uintptr_t>(z) - reinterpret_cast<uintptr_t>(p)) % ps, at = d < 0 ? d + ps : d;
+        return at >= (int64_t)prow && at + (int64_t)zrow <= ps;
+    };
+    for (int i = 0; i < 2; ++i) {
+        if (!to[i].p) continue;
+        const size_t row_i = (size_t)a.heads[i] * c.head_dim * ctx->esz;
+        for (int j = 0; j < 2; ++j) {
+            if (!from[j].p) continue;
+            const size_t row_j = (size_t)a.heads[j] * c.head_dim * ctx->esz;
+            const bool in_place = i == j && to[i].p == from[i].p && a.x_stride[i] == a.y_stride[i];
+            if (!in_place && !apart(to[i].p, a.y_stride[i], row_i, to[i].bytes, from[j].p, a.x_stride[j], row_j, from[j].bytes))
+                return fail(ASRKF_EINVAL, "%s's output overlaps %s", both[i].name, both[j].name);
+            if (i < j && to[j].p && !apart(to[i].p, a.y_stride[i], row_i, to[i].bytes, to[j].p, a.y_stride[j], row_j, to[j].bytes))
+                return fail(ASRKF_EINVAL, "the outputs overlap");
+        }
+    }
+    bool inside;
+    if (pos) {
+        if (reinterpret_cast<uintptr_t>(pos) & 3) return fail(ASRKF_EINVAL, "positions must be 4-byte aligned");
+        if (!kernel_readable(ctx, pos, (size_t)n_rows * 4, &inside) || !inside)
+            return fail(ASRKF_EINVAL, "positions must be %d int32 in memory of the context's device", n_rows);
+        for (const Span& x : to)
+            if (x.p && overlap(x.p, x.bytes, pos, (size_t)n_rows * 4)) return fail(ASRKF_EINVAL, "an output overlaps the positions");
+    }
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    HIP_OK(ctx, follow_last_stream(ctx, s));
+    mark_queued(ctx, s, capturing(s));
+    a.pos = pos;
+    a.plen = ctx->plen;
+    a.t_dev = ctx->t_dev;
+    a.t_offset = ctx->next_layer > 0 ? -1 : 0;    // the step's first launch has advanced the counter
+    a.rows_per_seq = rows_per_seq;
+    a.n = n_rows;
+    a.D = c.head_dim;
+    if (inverse) {
+        a.magnitude = 1.0 / a.magnitude;
+        for (int i = 0; i < a.pairs; ++i) a.turns[i] = -a.turns[i];
+    }
+    HIP_OK(ctx, launch_rotate(a, c.dtype == ASRKF_BF16, s));
+    return ASRKF_OK;
+}
+
+// ---- drafted tokens ----
+
+asrkf_status asrkf_tree_masks(int32_t n, const int32_t* parents, uint64_t* sees, int32_t* depth) {
+    if (n < 1 || n > kMaxDrafts || !parents) return fail(ASRKF_EINVAL, "n must be in 1..%d, parents given", kMaxDrafts);
+    uint64_t m[kMaxDrafts];
+    int32_t d[kMaxDrafts];
+    for (int i = 0; i < n; ++i) {
+        const int p = parents[i];
+        if (p < -1 || p >= i) return fail(ASRKF_EINVAL, "node %d: parent %d must be -1 or a node before it", i, p);
+        m[i] = (p >= 0 ? m[p] : 0) | (uint64_t)1 << i;
+        d[i] = p >= 0 ? d[p] + 1 : 0;
+    }
+    if (sees) memcpy(sees, m, n * sizeof m[0]);
+    if (depth) memcpy(depth, d, n * sizeof d[0]);
+    return ASRKF_OK;
+}
+
+asrkf_status asrkf_reserve_drafts(asrkf_ctx* ctx, int32_t max_nodes) {
+    asrkf_status st = check_ctx(ctx);
+    if (st != ASRKF_OK) return st;
+    const asrkf_config& c = ctx->cfg;
+    if (max_nodes < 1 || max_nodes > kMaxDrafts) return fail(ASRKF_EINVAL, "max_nodes must be in 1..%d", kMaxDrafts);
+    if (ctx->spill) return fail(ASRKF_EINVAL, "drafted tokens are not combined with spill mode");
+    if (max_nodes <= ctx->draft_nodes) return ASRKF_OK;
+    if (ctx->queued && capturing(ctx->last_stream)) return fail(ASRKF_ESTATE, "reserve while the context's stream is being captured");
+    if (ctx->captured && ctx->draft_nodes > 0)
+        return fail(ASRKF_ESTATE, "captured calls hold the room for %d nodes", ctx->draft_nodes);
+    st = on_device(ctx);
+    if (st != ASRKF_OK) return st;
+    st = sync_ctx(ctx);
+    if (st != ASRKF_OK) return st;
+    // partials: two slots of every attention workgroup, by the kind of workgroup
+    size_t acc = 0, ml = 0;
+    for (int i = 0, rows = 32; i < 4; ++i, rows *= 2) {
+        if (rows > draft_rows(max_nodes, ctx->group)) break;
+        int per_cu = 0;
+        HIP_OK(ctx, draft_occupancy(row_kind(ctx), c.head_dim, rows, &per_cu));
+        if (per_cu < 1) return fail(ASRKF_EINVAL, "draft attention workgroup does not fit on a CU for this shape");
+        ctx->draft_grid[i] = per_cu * ctx->cus;
+        acc = std::max(acc, (size_t)2 * ctx->draft_grid[i] * rows * c.head_dim * 4);
+        ml = std::max(ml, (size_t)2 * ctx->draft_grid[i] * rows * 2 * 4);
+    }
+    const size_t B = (size_t)c.batch;
+    void* parts[8] = {};
+    const size_t bytes[8] = {B * c.n_kv_heads * 2 * 4, 4, B * 4, B * (max_nodes + 1) * kVerifySplitMax * sizeof(VerifyPart),
+                             B * sizeof(VerifyEnd), B * kVerifySplitMax * 8, acc, ml};
+    size_t total = 0;
+    for (size_t x : bytes) total += (x + 255) / 256 * 256;
+    void* space = nullptr;
+    st = dev_alloc(ctx, &space, total);
+    if (st != ASRKF_OK) return st;
+    size_t at = 0, cleared = 0;
+    for (int i = 0; i < 8; ++i) {
+        parts[i] = static_cast<char*>(space) + at;
+        at += (bytes[i] + 255) / 256 * 256;
+        if (i == 2) cleared = at;                  // the tickets
+    }
+    ClearArgs z{};
+    z.n = 1;
+    z.p[0] = space;
+    z.words[0] = cleared / 4;
+    hipError_t e = launch_clear(z, nullptr);
+    if (e == hipSuccess) e = hipStreamSynchronize(nullptr);
+    if (e != hipSuccess) {
+        (void)hipFree(space);
+        return hip_fail(ctx, e, "clearing the tickets");
+    }
+    if (ctx->draft_space) (void)hipFree(ctx->draft_space);
+    ctx->draft_space = space;
+    ctx->draft_ticket = static_cast<int32_t*>(parts[0]);
+    ctx->accept_ticket = static_cast<int32_t*>(parts[1]);
+    ctx->verify_ticket = static_cast<int32_t*>(parts[2]);
+    ctx->verify_part = static_cast<VerifyPart*>(parts[3]);
+    ctx->verify_end = static_cast<VerifyEnd*>(parts[4]);
+    ctx->verify_sums = static_cast<double*>(parts[5]);
+    ctx->draft_acc = static_cast<float*>(parts[6]);
+    ctx->draft_ml = static_cast<float*>(parts[7]);
+    ctx->draft_nodes = max_nodes;
+    return ASRKF_OK;
+}
+
+}  // extern "C"
+
+namespace {
+
+asrkf_status check_drafts(const asrkf_ctx* ctx, int n_nodes) {
+    if (ctx->draft_nodes == 0) return fail(ASRKF_ESTATE, "asrkf_reserve_drafts comes first");
+    if (n_nodes < 1 || n_nodes > ctx->draft_nodes)
+        return fail(ASRKF_EINVAL, "n_nodes must be in 1..%d, the room reserved", ctx->draft_nodes);
+    return on_device(ctx);
+}
+
+// An array of the caller's that a kernel reads or writes: aligned to its elements, and inside
+// its allocation.
+asrkf_status check_array(const asrkf_ctx* ctx, const char* name, const void* p, size_t bytes, size_t align) {
+    if (!p) return fail(ASRKF_EINVAL, "null %s", name);
+    if (reinterpret_cast<uintptr_t>(p) % align) return fail(ASRKF_EINVAL, "%s must be %zu-byte aligned", name, align);
+    bool inside;
+    if (!kernel_readable(ctx, p, bytes, &inside)) return fail(ASRKF_EINVAL, "%s must be in memory of the context's device", name);
+    if (!inside) return fail(ASRKF_EINVAL, "%s is smaller than %zu bytes", name, bytes);
+    return ASRKF_OK;
+}
+
+// A token stride in elements (0: dense rows of `heads` heads) in bytes.
+asrkf_status token_stride(const asrkf_ctx* ctx, const char* name, int64_t stride, int heads, int64_t* bytes) {
+    const int64_t row = (int64_t)heads * ctx->cfg.head_dim * ctx->esz;
+    if (stride < 0 || stride > kMaxTokenStride) return fail(ASRKF_EINVAL, "%s: token stride out of range", name);
+    *bytes = stride ? stride * (int64_t)ctx->esz : row;
+    if (*bytes < row || *bytes % 16 || *bytes > kMaxTokenStride)
+        return fail(ASRKF_EINVAL, "%s: the token stride must be a multiple of 16 bytes from a token's row up to 16 MiB", name);
+    return ASRKF_OK;
+}
+
+#define CHECK(expr)                          \
+    do {                                     \
+        st = (expr);                         \
+        if (st != ASRKF_OK) return st;       \
+    } while (0)
+
+}  // namespace
+
+extern "C" {
+
+asrkf_status asrkf_attend_drafts(asrkf_ctx* ctx, int32_t layer, int32_t n_nodes, const int32_t* count,
+                                 const uint64_t* sees, const void* q, int64_t q_stride, const void* k,
+                                 int64_t k_stride, const void* v, int64_t v_stride, void* out, void* stream) {
+    TraceRange range("asrkf_attend_drafts");
+    asrkf_status st = check_ctx(ctx);
+    if (st != ASRKF_OK) return st;
+    const asrkf_config& c = ctx->cfg;
+    CHECK(check_drafts(ctx, n_nodes));
+    if (layer < 0 || layer >= c.n_layers) return fail(ASRKF_EINVAL, "layer out of range");
+    if (!ctx->lists_ready) return fail(ASRKF_ESTATE, "drafts attend from the first decode step on");
+    DraftArgs a{};
+    const size_t tokens = (size_t)c.batch * n_nodes;
+    CHECK(token_stride(ctx, "q", q_stride, c.n_q_heads, &a.q_stride));
+    CHECK(token_stride(ctx, "k", k_stride, c.n_kv_heads, &a.k_stride));
+    CHECK(token_stride(ctx, "v", v_stride, c.n_kv_heads, &a.v_stride));
+    const size_t head = c.head_dim * ctx->esz;
+    const size_t out_bytes = tokens * c.n_q_heads * head;
+    const struct { const char* name; const void* p; size_t bytes, align; } arrays[] = {
+        {"q", q, (tokens - 1) * a.q_stride + c.n_q_heads * head, 16},
+        {"k", k, (tokens - 1) * a.k_stride + c.n_kv_heads * head, 16},
+        {"v", v, (tokens - 1) * a.v_stride + c.n_kv_heads * head, 16},
+        {"sees", sees, tokens * 8, 8},
+        {"count", count, (size_t)c.batch * 4, 4}};
+    CHECK(check_array(ctx, "out", out, out_bytes, 16));
+    for (const auto& x : arrays) {
+        if (x.p == count && !count) continue;     // optional
+        CHECK(check_array(ctx, x.name, x.p, x.bytes, x.align));
+        if (overlap(x.p, x.bytes, out, out_bytes)) return fail(ASRKF_EINVAL, "out overlaps %s", x.name);
+    }
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const bool capture = capturing(s);
+    HIP_OK(ctx, follow_last_stream(ctx, s));
+    mark_queued(ctx, s, capture);
+    const PromptArgs p = prompt_args(ctx, layer);
+    const size_t st0 = ctx->token_scope ? 0 : (size_t)layer * c.batch;
+    a.q = static_cast<const char*>(q);
+    a.k = static_cast<const char*>(k);
+    a.v = static_cast<const char*>(v);
+    a.out = static_cast<char*>(out);
+    a.sees = sees;
+    a.count = count;
+    a.kpool = p.kpool;
+    a.vpool = p.vpool;
+    a.kscale = p.kscale;
+    a.vscale = p.vscale;
+    a.list = ctx->list + st0 * ctx->cap;
+    a.n_active = ctx->n_active + st0;
+    a.list_tail = ctx->next_layer > layer ? 0 : 1;     // the step's own token, once it is in the cache
+    a.part_acc = ctx->draft_acc;
+    a.part_ml = ctx->draft_ml;
+    a.ticket = ctx->draft_ticket;
+    a.B = c.batch;
+    a.N = n_nodes;
+    a.cap = ctx->cap;
+    a.Hq = c.n_q_heads;
+    a.Hkv = c.n_kv_heads;
+    a.pool_rows = ctx->pool_rows;
+    const int rows = draft_rows(n_nodes, ctx->group);
+    a.grid = ctx->draft_grid[rows == 32 ? 0 : rows == 64 ? 1 : rows == 128 ? 2 : 3];
+    HIP_OK(ctx, launch_drafts(a, row_kind(ctx), c.head_dim, a.grid, s));
+    return ASRKF_OK;
+}
+
+asrkf_status asrkf_verify_drafts(asrkf_ctx* ctx, int32_t n_nodes, const int32_t* count, const int32_t* tokens,
+                                 const int32_t* parents, const float* root_logits, const float* logits,
+                                 const float* probs, float temperature, const float* u, int32_t* path,
+                                 int32_t* n_path, int32_t* next, void* stream) {
+    TraceRange range("asrkf_verify_drafts");
+    asrkf_status st = check_ctx(ctx);
+    if (st != ASRKF_OK) return st;
+    const asrkf_config& c = ctx->cfg;
+    CHECK(check_drafts(ctx, n_nodes));
+    if (!(temperature >= 0.f) || isinf(temperature) || (temperature > 0.f && temperature < 1e-6f))
+        return fail(ASRKF_EINVAL, "temperature must be 0 or finite and at least 1e-6");
+    if (probs && temperature == 0.f) return fail(ASRKF_EINVAL, "draft probabilities have no part in greedy decoding");
+    const size_t B = (size_t)c.batch, nodes = B * n_nodes, row = (size_t)c.vocab * 4;
+    const struct { const char* name; const void* p; size_t bytes; bool written, optional; } arrays[] = {
+        {"path", path, nodes * 4, true, false},
+        {"n_path", n_path, B * 4, true, false},
+        {"next", next, B * 4, true, false},
+        {"count", count, B * 4, false, true},
+        {"tokens", tokens, nodes * 4, false, false},
+        {"parents", parents, nodes * 4, false, false},
+        {"root_logits", root_logits, B * row, false, false},
+        {"logits", logits, nodes * row, false, false},
+        {"probs", probs, nodes * row, false, true},
+        {"u", u, (nodes + B) * 4, false, temperature == 0.f}};
+    for (const auto& x : arrays) {
+        if (!x.p && x.optional) continue;
+        CHECK(check_array(ctx, x.name, x.p, x.bytes, 4));
+        for (const auto& y : arrays)
+            if (&x != &y && y.written && y.p && overlap(x.p, x.bytes, y.p, y.bytes))
+                return fail(ASRKF_EINVAL, "%s overlaps %s", y.name, x.name);
+    }
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    HIP_OK(ctx, follow_last_stream(ctx, s));
+    mark_queued(ctx, s, capturing(s));
+    VerifyArgs a{};
+    a.tokens = tokens;
+    a.parents = parents;
+    a.count = count;
+    a.root = root_logits;
+    a.logits = logits;
+    a.probs = probs;
+    a.u = u;
+    a.path = path;
+    a.n_path = n_path;
+    a.next = next;
+    a.part = ctx->verify_part;
+    a.end = ctx->verify_end;
+    a.sums = ctx->verify_sums;
+    a.ticket = ctx->verify_ticket;
+    a.B = c.batch;
+    a.N = n_nodes;
+    a.V = c.vocab;
+    a.split = verify_split(c.batch * (n_nodes + 1), c.vocab);
+    a.inv_t = temperature == 0.f ? 0.0 : 1.4426950408889634073599 / (double)temperature;
+    HIP_OK(ctx, launch_verify(a, s));
+    return ASRKF_OK;
+}
+
+asrkf_status asrkf_accept_drafts(asrkf_ctx* ctx, int32_t n_nodes, const int32_t* path, const int32_t* n_path,
+                                 const void* k, int64_t k_stride, int64_t k_layer_stride, const void* v,
+                                 int64_t v_stride, int64_t v_layer_stride, void* stream) {
+    TraceRange range("asrkf_accept_drafts");
+    asrkf_status st = check_ctx(ctx);
+    if (st != ASRKF_OK) return st;
+    const asrkf_config& c = ctx->cfg;
+    CHECK(check_drafts(ctx, n_nodes));
+    if (!ctx->lists_ready || ctx->next_layer != 0)
+        return fail(ASRKF_ESTATE, "drafts are accepted between two steps: after asrkf_restore, before the next decode_step");
+    AcceptArgs a{};
+    const size_t tokens = (size_t)c.batch * n_nodes;
+    CHECK(token_stride(ctx, "k", k_stride, c.n_kv_heads, &a.k_stride));
+    CHECK(token_stride(ctx, "v", v_stride, c.n_kv_heads, &a.v_stride));
+    const size_t row = (size_t)c.n_kv_heads * c.head_dim * ctx->esz;
+    const struct { const char* name; const void* p; int64_t stride, layer, *out; } rows[] = {
+        {"k", k, a.k_stride, k_layer_stride, &a.k_layer}, {"v", v, a.v_stride, v_layer_stride, &a.v_layer}};
+    for (const auto& x : rows) {
+        const size_t one = (tokens - 1) * x.stride + row;          // a layer's
+        const int64_t dense = (int64_t)tokens * x.stride;
+        if (x.layer < 0 || x.layer > ((int64_t)1 << 40)) return fail(ASRKF_EINVAL, "%s: layer stride out of range", x.name);
+        *x.out = x.layer ? x.layer * (int64_t)ctx->esz : dense;
+        if (*x.out % 16) return fail(ASRKF_EINVAL, "%s: the layer stride must be a multiple of 16 bytes", x.name);
+        CHECK(check_array(ctx, x.name, x.p, (size_t)(c.n_layers - 1) * *x.out + one, 16));
+    }
+    CHECK(check_array(ctx, "path", path, tokens * 4, 4));
+    CHECK(check_array(ctx, "n_path", n_path, (size_t)c.batch * 4, 4));
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const bool capture = capturing(s);
+    for (int b = 0; b < c.batch; ++b) {
+        if (ctx->plen_most[b] + ctx->t + n_nodes > c.max_ctx && !capture) CHECK(learn_lengths(ctx));
+        if (ctx->plen_most[b] + ctx->t + n_nodes > c.max_ctx)
+            return fail(ASRKF_ECAPACITY, "sequence %d has no room for %d nodes (max_ctx=%d)", b, n_nodes, c.max_ctx);
+    }
+    HIP_OK(ctx, follow_last_stream(ctx, s));
+    mark_queued(ctx, s, capture);
+    const PromptArgs p = prompt_args(ctx, 0);
+    a.k = static_cast<const char*>(k);
+    a.v = static_cast<const char*>(v);
+    a.path = path;
+    a.n_path = n_path;
+    a.kpool = p.kpool;
+    a.vpool = p.vpool;
+    a.kscale = p.kscale;
+    a.vscale = p.vscale;
+    a.plen = ctx->plen;
+    a.t_dev = ctx->t_dev;
+    a.list = ctx->list;
+    a.n_active = ctx->n_active;
+    a.listed_total = ctx->counters;
+    a.flags = ctx->flags;
+    a.ticket = ctx->accept_ticket;
+    a.L = c.n_layers;
+    a.B = c.batch;
+    a.N = n_nodes;
+    a.Hkv = c.n_kv_heads;
+    a.pool_rows = ctx->pool_rows;
+    a.head_bytes = p.head_bytes;
+    a.four = p.four;
+    a.cap = ctx->cap;
+    a.states = ctx->state_layers;
+    a.max_ctx = c.max_ctx;
+    HIP_OK(ctx, launch_accept(a, s));
+    ctx->accepted = true;
+    if (capture) ctx->accept_captured = true;
+    // a captured call grows the sequences at every replay, which the host learns of like the steps
+    if (!capture)
+        for (int b = 0; b < c.batch; ++b) ctx->plen_most[b] += n_nodes;
+    return ASRKF_OK;
+}
+
+#undef CHECK
 
 asrkf_status asrkf_stats(asrkf_ctx* ctx, asrkf_stats_t* out) {
     asrkf_status st = check_ctx(ctx);
@@ -1441,6 +1947,8 @@ asrkf_status asrkf_reset(asrkf_ctx* ctx) {
     HIP_OK(ctx, hipStreamSynchronize(s));
     if (ctx->flags_host) ctx->flags_host[0] = ctx->flags_host[1] = 0;
     ctx->plen_host.assign(c.batch, 0);
+    ctx->plen_most.assign(c.batch, 0);
+    ctx->accepted = ctx->accept_captured;
     ctx->prefilled.assign(c.batch, 0);
     ctx->t = 0;
     ctx->next_layer = 0;
