@@ -309,12 +309,11 @@ struct VerifyPart {           // of a row of logits: sum of e^((x - m) / T), max
     float m;
     int32_t at;               // -1: a NaN, an infinity, or nothing above -inf
 };
-struct VerifyEnd {            // where a sequence's walk has ended
+struct VerifyEnd {            // where a sequence's walk has ended, where a rejection with draft probabilities is the end
     double scale, c;          // weights are max(e^((x - m) / T) scale - c q, 0)
     double c_before;          // c where that leaves nothing, or -1
     float m;
-    int32_t row;              // 0 the root's, 1 + i node i's; -1: nothing to draw from
-    uint64_t rejected;        // nodes whose tokens weigh 0
+    int32_t row;              // 0 the root's, 1 + i node i's; -1: the next token is known
 };
 struct VerifyArgs {
     const int32_t* tokens;    // [B][N]
@@ -331,7 +330,8 @@ struct VerifyArgs {
     VerifyEnd* end;           // [B]
     double* sums;             // [B][split]
     int32_t* ticket;          // [B], zero between launches
-    int32_t B, N, V, split;
+    int32_t B, N, V;
+    int32_t split, part_len;  // parts of a row, and their length (set for the launch)
     double inv_t;             // log2(e) / temperature; 0: greedy
 };
 
@@ -403,8 +403,6 @@ int draft_rows(int n, int group);
 hipError_t draft_occupancy(int rows_kind, int head_dim, int rows, int* blocks_per_cu);
 hipError_t launch_drafts(const DraftArgs& a, int rows_kind, int head_dim, int blocks, hipStream_t s);
 hipError_t launch_accept(const AcceptArgs& a, hipStream_t s);
-// Workgroups of a row of logits.
-int verify_split(int rows, int V);
 hipError_t launch_verify(const VerifyArgs& a, hipStream_t s);
 
 }  // namespace asrkf

@@ -1635,6 +1635,7 @@ asrkf_status asrkf_verify_drafts(asrkf_ctx* ctx, int32_t n_nodes, const int32_t*
     if (!(temperature >= 0.f) || isinf(temperature) || (temperature > 0.f && temperature < 1e-6f))
         return fail(ASRKF_EINVAL, "temperature must be 0 or finite and at least 1e-6");
     if (probs && temperature == 0.f) return fail(ASRKF_EINVAL, "draft probabilities have no part in greedy decoding");
+    if (c.vocab > (1 << 30)) return fail(ASRKF_EINVAL, "vocab must be at most 2^30");
     const size_t B = (size_t)c.batch, nodes = B * n_nodes, row = (size_t)c.vocab * 4;
     const struct { const char* name; const void* p; size_t bytes; bool written, optional; } arrays[] = {
         {"path", path, nodes * 4, true, false},
@@ -1675,7 +1676,6 @@ asrkf_status asrkf_verify_drafts(asrkf_ctx* ctx, int32_t n_nodes, const int32_t*
     a.B = c.batch;
     a.N = n_nodes;
     a.V = c.vocab;
-    a.split = verify_split(c.batch * (n_nodes + 1), c.vocab);
     a.inv_t = temperature == 0.f ? 0.0 : 1.4426950408889634073599 / (double)temperature;
     HIP_OK(ctx, launch_verify(a, s));
     return ASRKF_OK;

@@ -15,9 +15,10 @@
 // Accepted or not, and which token: decisions on sums over a vocabulary whose neighbours lie 10^-6
 // apart.  Exponentials and sums are 64-bit, so that they do not hang on the order of summation.
 //
-// Three launches: the sums of every row of logits in parts (bound by the bytes, or by the
-// exponentials); the walk, a workgroup to a sequence; the draw, parts of the last row's weights,
-// the part that holds the drawn point searched by the workgroup that arrives last.
+// Launches: the sums of every row of logits, in parts of at most 64 to a row, and the walk, a workgroup to a
+// sequence, which also draws the next token: the parts' sums say which part holds the drawn point, and
+// only that one is read again.  Where the walk ends behind a rejection with draft probabilities the
+// weights are other ones, whose sums a third launch forms.
 #include "kernels.h"
 #include "tiles.h"
 
@@ -56,21 +57,12 @@ __device__ __forceinline__ double shfl_up(double x, int o) {
     return __longlong_as_double(((unsigned long long)hi << 32) | lo);
 }
 
-// Two parts of a row as one.  A part without a logit has m = -inf, S = 0, at = kNone.
+__device__ __forceinline__ double wave_sum(double x) {
+    for (int o = 1; o < 64; o <<= 1) x += shfl_xor(x, o);
+    return x;
+}
+
 constexpr int kNone = 0x7FFFFFFF;
-__device__ __forceinline__ VerifyPart merge(const VerifyPart& a, const VerifyPart& b, double inv_t) {
-    VerifyPart r;
-    if (a.at < 0 || b.at < 0) return VerifyPart{0.0, 0.f, -1};
-    r.m = fmaxf(a.m, b.m);
-    r.at = a.m > b.m ? a.at : b.m > a.m ? b.at : min(a.at, b.at);
-    // (a part at the maximum keeps its sum; -inf - -inf is not formed)
-    r.S = (a.m == r.m ? a.S : a.S * exp2_64(((double)a.m - r.m) * inv_t)) +
-          (b.m == r.m ? b.S : b.S * exp2_64(((double)b.m - r.m) * inv_t));
-    return r;
-}
-__device__ __forceinline__ VerifyPart from_lane(const VerifyPart& a, int o) {
-    return VerifyPart{shfl_xor(a.S, o), __shfl_xor(a.m, o), __shfl_xor(a.at, o)};
-}
 
 __device__ __forceinline__ int nodes_of(const VerifyArgs& a, int b) {
     return a.count ? min(max(a.count[b], 0), a.N) : a.N;
@@ -79,90 +71,227 @@ __device__ __forceinline__ int nodes_of(const VerifyArgs& a, int b) {
 __device__ __forceinline__ const float* row_of(const VerifyArgs& a, int b, int row) {
     return row == 0 ? a.root + (size_t)b * a.V : a.logits + ((size_t)b * a.N + row - 1) * a.V;
 }
+__device__ __forceinline__ const float* draft_row(const VerifyArgs& a, int b, int row) {
+    return a.probs + ((size_t)b * a.N + row) * a.V;
+}
 
-// The logits [i0, i1) of a row that part sp of a.split takes; parts start 16-byte aligned but for the first.
-struct Range { int head, i0, i1; };
-__device__ __forceinline__ Range part_range(const float* x, int V, int sp, int split) {
-    const int head = min(V, (int)((16 - (reinterpret_cast<uintptr_t>(x) & 15)) & 15) / 4);
-    const int per = ((V - head) / 4 + split - 1) / split * 4;
-    Range r;
-    r.i0 = sp == 0 ? 0 : min(V, head + sp * per);
-    r.i1 = sp == split - 1 ? V : min(V, head + (sp + 1) * per);
-    r.head = sp == 0 ? head : 0;
+// Four values from any address, `fill` past the end.
+__device__ __forceinline__ floatx4 load4(const float* x, int i, int end, float fill) {
+    typedef float loose4 __attribute__((ext_vector_type(4), aligned(4)));
+    floatx4 r = {fill, fill, fill, fill};
+    if (i + 3 < end) {
+        const loose4 v = *reinterpret_cast<const loose4*>(x + i);
+        r = floatx4{v[0], v[1], v[2], v[3]};
+    } else {
+#pragma unroll
+        for (int e = 0; e < 3; ++e)
+            if (i + e < end) r[e] = x[i + e];
+    }
     return r;
 }
 
 // ---- the sums of every row ----
 
+// A workgroup's part: its maximum first, over the values it holds in registers, then the sum with one
+// exponential to a value.
 __global__ void __launch_bounds__(kThreads)
 verify_sums_kernel(VerifyArgs a) {
-    __shared__ VerifyPart waves[kThreads / 64];
-    const int sp = blockIdx.x, row = blockIdx.y, b = blockIdx.z;
+    constexpr int kWaves = kThreads / 64, kQuads = 4;
+    __shared__ float top_lds[2][kWaves];
+    __shared__ int at_lds[2][kWaves];
+    __shared__ double sum_lds[kWaves];
+    const int sp = blockIdx.x, row = blockIdx.y, b = blockIdx.z, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     if (row > nodes_of(a, b)) return;
     const float* x = row_of(a, b, row);
-    const Range r = part_range(x, a.V, sp, a.split);
-    VerifyPart acc{0.0, -INFINITY, kNone};
-    auto take = [&](const float (&v)[16], int n, auto at) __attribute__((always_inline)) {
+    const int i0 = sp * a.part_len, i1 = min(a.V, i0 + a.part_len);
+    float m = -INFINITY;
+    int at = kNone;
+    double S = 0.0;                               // the thread's own values, against m
+    bool bad = false;
+    for (int j = i0, turn = 0; j < i1; j += kThreads * kQuads * 4, ++turn) {
+        floatx4 v[kQuads];
+#pragma unroll
+        for (int u = 0; u < kQuads; ++u) v[u] = load4(x, j + (u * kThreads + threadIdx.x) * 4, i1, -INFINITY);
         float top = -INFINITY;
         int where = kNone;
-        bool bad = false;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            if (i >= n) continue;
-            bad |= !(v[i] < INFINITY);
-            if (v[i] > top) {                     // the first of equals
-                top = v[i];
-                where = at(i);
+        for (int u = 0; u < kQuads; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                bad |= !(v[u][e] < INFINITY);
+                if (v[u][e] > top) {              // the first of equals
+                    top = v[u][e];
+                    where = j + (u * kThreads + (int)threadIdx.x) * 4 + e;
+                }
             }
+        for (int o = 1; o < 64; o <<= 1) {
+            const float y = __shfl_xor(top, o);
+            const int z = __shfl_xor(where, o);
+            where = y > top ? z : y == top ? min(where, z) : where;
+            top = fmaxf(top, y);
         }
-        if (bad || acc.at < 0) {
-            acc.at = -1;
-            return;
+        if (lane == 0) {
+            top_lds[turn & 1][wave] = top;
+            at_lds[turn & 1][wave] = where;
         }
-        if (top == -INFINITY) return;             // nothing of weight
-        double S = 0.0;
-        if (a.inv_t != 0.0) {
+        __syncthreads();
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-                if (i < n) S += v[i] == -INFINITY ? 0.0 : exp2_64(((double)v[i] - top) * a.inv_t);
+        for (int w = 0; w < kWaves; ++w) {
+            const float y = top_lds[turn & 1][w];
+            const int z = at_lds[turn & 1][w];
+            where = y > top ? z : y == top ? min(where, z) : where;
+            top = fmaxf(top, y);
         }
-        acc = merge(acc, VerifyPart{S, top, where}, a.inv_t);
-    };
-    const int body0 = r.i0 + r.head, n4 = (r.i1 - body0) / 4;
-    typedef float f4 __attribute__((ext_vector_type(4)));
-    const f4* body = reinterpret_cast<const f4*>(x + body0);
-    for (int i0 = 0; i0 < n4; i0 += 4 * kThreads) {
-        float v[16];
+        if (top > m) {
+            S = m == -INFINITY ? 0.0 : S * exp2_64(((double)m - top) * a.inv_t);
+            m = top;
+            at = where;
+        }
+        if (a.inv_t != 0.0 && m > -INFINITY && m < INFINITY) {
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int i = i0 + u * kThreads + threadIdx.x;
-            const f4 f = i < n4 ? __builtin_nontemporal_load(body + i) : f4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-            v[4 * u] = f.x; v[4 * u + 1] = f.y; v[4 * u + 2] = f.z; v[4 * u + 3] = f.w;
-        }
-        take(v, 16, [&](int i) { return body0 + (i0 + i / 4 * kThreads + (int)threadIdx.x) * 4 + i % 4; });
-    }
-    {   // the few before the first 16-byte boundary and behind the last
-        const int tail0 = body0 + 4 * n4, loose = r.head + r.i1 - tail0;
-        if ((int)threadIdx.x < loose) {
-            const int at = (int)threadIdx.x < r.head ? (int)threadIdx.x : tail0 + (int)threadIdx.x - r.head;
-            float v[16] = {x[at]};
-            take(v, 1, [&](int) { return at; });
+            for (int u = 0; u < kQuads; ++u)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) S += v[u][e] == -INFINITY ? 0.0 : exp2_64(((double)v[u][e] - m) * a.inv_t);
         }
     }
-    for (int o = 1; o < 64; o <<= 1) acc = merge(acc, from_lane(acc, o), a.inv_t);
-    if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = acc;
-    __syncthreads();
+    S = wave_sum(S);
+    if (lane == 0) sum_lds[wave] = S;
+    const bool any_bad = __syncthreads_or(bad);
     if (threadIdx.x == 0) {
-        for (int w = 1; w < kThreads / 64; ++w) acc = merge(acc, waves[w], a.inv_t);
-        a.part[((size_t)b * (a.N + 1) + row) * a.split + sp] = acc;
+        S = 0.0;
+        for (int w = 0; w < kWaves; ++w) S += sum_lds[w];
+        a.part[((size_t)b * (a.N + 1) + row) * a.split + sp] = VerifyPart{S, m, any_bad ? -1 : at};
     }
 }
 
-// ---- the walk ----
+// ---- the walk and the draw ----
 
 // e^((x - m) / T) scale - c q of a token, not below 0
 __device__ __forceinline__ double weight_of(float x, float m, double inv_t, double scale, double c, double q) {
     return fmax(x == -INFINITY ? -c * q : exp2_64(((double)x - m) * inv_t) * scale - c * q, 0.0);
+}
+
+// The weights behind a row, and what a workgroup does with a range of them.
+template <int THREADS>
+struct Weights {
+    static constexpr int kWaves = THREADS / 64;
+    const float* x;
+    const float* q;               // null: c is 0
+    float m;
+    double inv_t, scale, c;
+    const int* gone;              // LDS: tokens without weight
+    int n_gone;
+    double* lds;                  // [kWaves + 1]
+    int* found;                   // LDS, [2]
+
+    __device__ __forceinline__ double of(int v, float xv, float qv) const {
+        double w = weight_of(xv, m, inv_t, scale, c, (double)qv);
+        for (int i = 0; i < n_gone; ++i) w = gone[i] == v ? 0.0 : w;
+        return w;
+    }
+    __device__ __forceinline__ double block_sum(double s) const {
+        s = wave_sum(s);
+        __syncthreads();                          // lds may still be read
+        if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = s;
+        __syncthreads();
+        s = 0.0;
+        for (int w = 0; w < kWaves; ++w) s += lds[w];
+        return s;
+    }
+    // of [i0, i1), in every thread
+    __device__ __forceinline__ double sum(int i0, int i1) const {
+        constexpr int kQuads = 2;
+        double s = 0.0;
+        for (int j = i0; j < i1; j += THREADS * kQuads * 4) {
+            floatx4 xv[kQuads], qv[kQuads];
+#pragma unroll
+            for (int u = 0; u < kQuads; ++u) {
+                const int i = j + (u * THREADS + threadIdx.x) * 4;
+                xv[u] = load4(x, i, i1, -INFINITY);
+                qv[u] = q ? load4(q, i, i1, 0.f) : floatx4{0.f, 0.f, 0.f, 0.f};
+            }
+#pragma unroll
+            for (int u = 0; u < kQuads; ++u)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s += of(j + (u * THREADS + threadIdx.x) * 4 + e, xv[u][e], qv[u][e]);
+        }
+        return block_sum(s);
+    }
+    // The first token of [i0, i1) whose running sum passes point; where rounding leaves none, the last
+    // of any weight; -1 without weights.  In every thread.
+    __device__ __forceinline__ int find(int i0, int i1, double point) const {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        if (threadIdx.x == 0) {
+            found[0] = kNone;
+            found[1] = -1;
+        }
+        // a run of neighbouring tokens per thread, in whole quads
+        const int per = ((i1 - i0 + THREADS - 1) / THREADS + 3) / 4 * 4;
+        const int v0 = min(i1, i0 + (int)threadIdx.x * per), v1 = min(i1, v0 + per);
+        auto quad = [&](int v, double (&w)[4]) __attribute__((always_inline)) {
+            const floatx4 xv = load4(x, v, v1, -INFINITY), qv = q ? load4(q, v, v1, 0.f) : floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = of(v + e, xv[e], qv[e]);
+        };
+        double mine = 0.0, first4[4] = {0.0, 0.0, 0.0, 0.0};
+        if (v0 < v1) quad(v0, first4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) mine += first4[e];
+        for (int v = v0 + 4; v < v1; v += 4) {
+            double w[4];
+            quad(v, w);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) mine += w[e];
+        }
+        double run = mine;
+        for (int o = 1; o < 64; o <<= 1) {
+            const double y = shfl_up(run, o);
+            if (lane >= o) run += y;
+        }
+        __syncthreads();
+        if (lane == 63) lds[wave] = run;
+        __syncthreads();
+        for (int w = 0; w < wave; ++w) run += lds[w];
+        double before = run - mine;
+        int first = kNone, last = -1;
+        for (int v = v0; v < v1; v += 4) {
+            double w[4];
+            if (v == v0) for (int e = 0; e < 4; ++e) w[e] = first4[e];
+            else quad(v, w);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                before += w[e];
+                if (w[e] > 0.0) last = v + e;
+                if (before > point && w[e] > 0.0 && first == kNone) first = v + e;
+            }
+        }
+        if (first != kNone) atomicMin(&found[0], first);
+        if (last >= 0) atomicMax(&found[1], last);
+        __syncthreads();
+        return found[0] != kNone ? found[0] : found[1];
+    }
+};
+
+// The part that holds the point u W, from the parts' sums, one to a lane: the first whose running sum
+// passes it; beyond the end (a random number of 1 and more) the last of any weight; -1 without weights.
+// left: what is still to go within it.
+__device__ __forceinline__ int part_of_point(double s, double u, double& left) {
+    const int lane = threadIdx.x & 63;
+    double run = s;
+    for (int o = 1; o < 64; o <<= 1) {
+        const double y = shfl_up(run, o);
+        if (lane >= o) run += y;
+    }
+    double W = run;                               // the last lane's
+    for (int o = 1; o < 64; o <<= 1) W = fmax(W, shfl_xor(W, o));
+    const double point = u * W;
+    const uint64_t past = __ballot(run > point), some = __ballot(s > 0.0);
+    const int at = past ? __builtin_ctzll(past) : some ? 63 - __builtin_clzll(some) : -1;
+    const double rest = point - (run - s);
+    const unsigned long long bits = __double_as_longlong(rest);
+    const int from = max(at, 0);
+    left = __longlong_as_double(((unsigned long long)(unsigned)__shfl((int)(bits >> 32), from) << 32) | (unsigned)__shfl((int)bits, from));
+    return at;
 }
 
 constexpr int kWalkThreads = 1024;
@@ -170,56 +299,75 @@ constexpr int kWalkThreads = 1024;
 __global__ void __launch_bounds__(kWalkThreads)
 verify_walk_kernel(VerifyArgs a) {
     __shared__ VerifyPart rows[kMaxDrafts + 1];
-    __shared__ double waves[kWalkThreads / 64];
-    __shared__ double mass_lds[kMaxDrafts], q_lds[kMaxDrafts];
-    __shared__ int parent_lds[kMaxDrafts], token_lds[kMaxDrafts];
+    __shared__ double sums[kWalkThreads / 64];
+    __shared__ int gone[kMaxDrafts], found[2];
     const int b = blockIdx.x, nodes = nodes_of(a, b);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    for (int row = wave; row <= nodes; row += blockDim.x / 64) {
+    // a node to a lane, in every wave
+    int parent = -2, token = -1;                  // -2: nobody's child; a token below 0 weighs nothing
+    float u = 0.f;
+    if (lane < nodes) {
+        const int p = a.parents[(size_t)b * a.N + lane], x = a.tokens[(size_t)b * a.N + lane];
+        parent = p >= -1 && p < lane ? p : -2;
+        token = (uint32_t)x < (uint32_t)a.V ? x : -1;
+        if (a.inv_t != 0.0) u = a.u[(size_t)b * (a.N + 1) + lane];
+    }
+    float logit = -INFINITY, q_own = 1.f;
+    if (parent >= -1 && token >= 0 && a.inv_t != 0.0) {
+        logit = row_of(a, b, parent + 1)[token];
+        if (a.probs) q_own = draft_row(a, b, parent + 1)[token];
+    }
+    for (int row = wave; row <= nodes; row += kWalkThreads / 64) {
         VerifyPart p{0.0, -INFINITY, kNone};
         if (lane < a.split) p = a.part[((size_t)b * (a.N + 1) + row) * a.split + lane];
-        for (int o = 1; o < 64; o <<= 1) p = merge(p, from_lane(p, o), a.inv_t);
-        if (lane == 0) rows[row] = VerifyPart{p.S, p.m, p.at == kNone ? -1 : p.at};
-    }
-    __syncthreads();
-    // of every node: p(x) and q(x) behind its parent
-    if ((int)threadIdx.x < nodes) {
-        const int i = threadIdx.x, parent = a.parents[(size_t)b * a.N + i], x = a.tokens[(size_t)b * a.N + i];
-        const bool fits = parent >= -1 && parent < i && (uint32_t)x < (uint32_t)a.V;
-        parent_lds[i] = parent >= -1 && parent < i ? parent : -2;           // -2: nobody's child
-        token_lds[i] = fits ? x : -1 - i;                                   // no token: weighs nothing
-        double mass = 0.0, q = 1.0;
-        if (fits && rows[parent + 1].at >= 0) {
-            const VerifyPart p = rows[parent + 1];
-            if (a.inv_t != 0.0) mass = weight_of(row_of(a, b, parent + 1)[x], p.m, a.inv_t, 1.0 / p.S, 0.0, 0.0);
-            if (a.probs) q = a.probs[((size_t)b * a.N + parent + 1) * a.V + x];
+        float m = p.m;
+        int at = p.at;
+        for (int o = 1; o < 64; o <<= 1) {
+            const float y = __shfl_xor(m, o);
+            const int z = __shfl_xor(at, o);
+            // a part without distribution (-1) takes all
+            at = min(at, z) < 0 ? -1 : y > m ? z : y == m ? min(at, z) : at;
+            m = fmaxf(m, y);
         }
-        mass_lds[i] = mass;
-        q_lds[i] = q;
+        double S = 0.0;
+        if (a.inv_t != 0.0) S = wave_sum(p.m == -INFINITY || at < 0 ? 0.0 : p.S * exp2_64(((double)p.m - m) * a.inv_t));
+        if (lane == 0) rows[row] = VerifyPart{S, m, m == -INFINITY ? -1 : at};
     }
     __syncthreads();
+    double mass = 0.0;                            // p(x) behind the parent
+    if (parent >= -1 && token >= 0 && a.inv_t != 0.0) {
+        const VerifyPart p = rows[parent + 1];
+        if (p.at >= 0) mass = weight_of(logit, p.m, a.inv_t, 1.0 / p.S, 0.0, 0.0);
+    }
+    const double q = q_own;
 
+    auto of_lane = [&](double x, int i) __attribute__((always_inline)) {
+        const unsigned long long bits = __double_as_longlong(x);
+        return __longlong_as_double(((unsigned long long)(unsigned)__builtin_amdgcn_readlane((int)(bits >> 32), i) << 32) |
+                                    (unsigned)__builtin_amdgcn_readlane((int)bits, i));
+    };
     int last = -1, n_path = 0;
     double W = 1.0, c = 0.0, c_before = -1.0;     // w = max(p - c q, 0), W its sum
-    uint64_t rejected = 0;                        // since the last accepted one
-    for (int i = 0; i < nodes; ++i) {             // (the same in every thread)
-        if (parent_lds[i] != last) continue;
+    uint64_t rejected = 0;                        // since the last one kept
+    uint64_t todo = ~0ull;                        // nodes not looked at yet
+    for (;;) {                                    // (the same in every wave)
+        const uint64_t next = __ballot(parent == last) & todo;
+        if (!next) break;
+        const int i = __builtin_ctzll(next);
+        todo = i < 63 ? ~0ull << (i + 1) : 0;
         const VerifyPart p = rows[last + 1];
+        const int x = __builtin_amdgcn_readlane(token, i);
         bool yes = false;
-        if (p.at >= 0 && token_lds[i] >= 0) {
+        if (p.at >= 0 && x >= 0) {
             if (a.inv_t == 0.0) {
-                yes = token_lds[i] == p.at;
+                yes = x == p.at;
             } else {
-                double mass = mass_lds[i];
-                if (a.probs) {
-                    mass = fmax(mass - c * q_lds[i], 0.0);
-                } else {
-                    // a rejected sibling's token weighs nothing
-                    const bool same = lane < i && (rejected >> lane & 1) && token_lds[lane] == token_lds[i];
-                    if (__any(same)) mass = 0.0;
-                }
-                yes = (double)a.u[(size_t)b * (a.N + 1) + i] * q_lds[i] * W < mass;
-                if (!yes && !a.probs) W -= mass;
+                const double qi = of_lane(q, i);
+                double w = of_lane(mass, i);
+                if (a.probs) w = fmax(w - c * qi, 0.0);
+                else if (__ballot(token == x) & rejected) w = 0.0;         // a rejected sibling's token
+                yes = (double)__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(u), i)) * qi * W < w;
+                if (!yes && !a.probs) W -= w;
             }
         }
         if (yes) {
@@ -231,177 +379,113 @@ verify_walk_kernel(VerifyArgs a) {
             rejected = 0;
             continue;
         }
-        rejected |= 1ull << i;
-        if (a.probs && a.inv_t != 0.0 && p.at >= 0) {
-            const double c2 = c + W, scale = 1.0 / p.S;
-            if (!__any(lane > i && lane < nodes && parent_lds[lane] == last)) {
+        if (x >= 0) rejected |= 1ull << i;
+        if (a.probs && p.at >= 0) {
+            const double c2 = c + W;
+            if (!(__ballot(parent == last) & todo)) {
                 c_before = c;                     // nobody asks for the sum: the draw finds it
                 c = c2;
-                continue;
+                break;
             }
-            // the sum of what remains, over the vocabulary
-            const float* x = row_of(a, b, last + 1);
-            const float* q = a.probs + ((size_t)b * a.N + last + 1) * a.V;
-            double sum = 0.0;
-            for (int v = threadIdx.x; v < a.V; v += blockDim.x) sum += weight_of(x[v], p.m, a.inv_t, scale, c2, (double)q[v]);
-            for (int o = 1; o < 64; o <<= 1) sum += shfl_xor(sum, o);
-            __syncthreads();
-            if (lane == 0) waves[wave] = sum;
-            __syncthreads();
-            sum = 0.0;
-            for (int w = 0; w < (int)blockDim.x / 64; ++w) sum += waves[w];
+            const Weights<kWalkThreads> w{row_of(a, b, last + 1), draft_row(a, b, last + 1), p.m, a.inv_t, 1.0 / p.S, c2, gone, 0, sums, found};
+            const double sum = w.sum(0, a.V);
             if (sum > 0.0) {
                 c = c2;
                 W = sum;
             }
         }
     }
-    for (int i = n_path + threadIdx.x; i < a.N; i += blockDim.x) a.path[(size_t)b * a.N + i] = -1;
+    for (int i = n_path + threadIdx.x; i < a.N; i += kWalkThreads) a.path[(size_t)b * a.N + i] = -1;
+    const VerifyPart p = rows[last + 1];
     if (threadIdx.x == 0) {
-        const VerifyPart p = rows[last + 1];
         a.n_path[b] = n_path;
         if (a.inv_t == 0.0 || p.at < 0) a.next[b] = p.at;
-        VerifyEnd e{};
-        e.row = p.at < 0 ? -1 : last + 1;
-        e.m = p.m;
-        e.scale = 1.0 / p.S;
-        e.c = c;
-        e.c_before = c_before;
-        e.rejected = a.probs ? 0 : rejected;
-        a.end[b] = e;
+        if (a.probs) a.end[b] = VerifyEnd{1.0 / p.S, c, c_before, p.m, p.at < 0 || c == 0.0 ? -1 : last + 1};
     }
+    if (a.inv_t == 0.0 || p.at < 0 || c != 0.0) return;
+
+    // the draw from p without the rejected tokens
+    const int n_gone = a.probs ? 0 : __popcll(rejected);
+    if (n_gone && wave == 0 && (rejected >> lane & 1)) gone[__popcll(rejected & ((1ull << lane) - 1ull))] = token;
+    __syncthreads();
+    const Weights<kWalkThreads> w{row_of(a, b, last + 1), nullptr, p.m, a.inv_t, 1.0 / p.S, 0.0, gone, n_gone, sums, found};
+    double s = 0.0;
+    if (lane < a.split) {
+        const VerifyPart mine = a.part[((size_t)b * (a.N + 1) + last + 1) * a.split + lane];
+        if (mine.m > -INFINITY) s = mine.S * exp2_64(((double)mine.m - p.m) * a.inv_t) * w.scale;
+    }
+    uint64_t again = 0;                           // parts that hold a rejected token: summed without it
+    for (int i = 0; i < n_gone; ++i) again |= 1ull << (gone[i] / a.part_len);
+    for (; again; again &= again - 1) {
+        const int sp = __builtin_ctzll(again);
+        const double sum = w.sum(sp * a.part_len, min(a.V, (sp + 1) * a.part_len));
+        if (lane == sp) s = sum;
+    }
+    double left;
+    const int sp = part_of_point(s, (double)a.u[(size_t)b * (a.N + 1) + a.N], left);
+    const int tok = sp < 0 ? -1 : w.find(sp * a.part_len, min(a.V, (sp + 1) * a.part_len), left);
+    if (threadIdx.x == 0) a.next[b] = tok;
 }
 
-// ---- the draw ----
+// ---- the draw from what a rejection has left ----
 
 __global__ void __launch_bounds__(kThreads)
-verify_draw_kernel(VerifyArgs a) {
-    __shared__ double waves[kThreads / 64];
-    __shared__ double base_lds;
-    __shared__ int last_arrival, part_lds, found, last_of_weight;
-    __shared__ int gone[kMaxDrafts];
-    const int sp = blockIdx.x, b = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    VerifyEnd e = a.end[b];
+verify_rest_kernel(VerifyArgs a) {
+    __shared__ double lds[kThreads / 64];
+    __shared__ int last_arrival, found[2];
+    const int sp = blockIdx.x, b = blockIdx.y, lane = threadIdx.x & 63;
+    const VerifyEnd e = a.end[b];
     if (e.row < 0) return;
-    const float* x = row_of(a, b, e.row);
-    const float* q = a.probs && e.c != 0.0 ? a.probs + ((size_t)b * a.N + e.row) * a.V : nullptr;
-    const int n_gone = __popcll(e.rejected);
-    if (threadIdx.x < 64 && (e.rejected >> lane & 1))
-        gone[__popcll(e.rejected & ((1ull << lane) - 1ull))] = a.tokens[(size_t)b * a.N + lane];
-    __syncthreads();
-    auto weight = [&](int v) __attribute__((always_inline)) {
-        double w = weight_of(x[v], e.m, a.inv_t, e.scale, e.c, q ? (double)q[v] : 0.0);
-        for (int i = 0; i < n_gone; ++i) w = gone[i] == v ? 0.0 : w;
-        return w;
-    };
+    Weights<kThreads> w{row_of(a, b, e.row), draft_row(a, b, e.row), e.m, a.inv_t, e.scale, e.c, nullptr, 0, lds, found};
     {
-        const Range r = part_range(x, a.V, sp, a.split);
-        double sum = 0.0;
-        for (int v = r.i0 + threadIdx.x; v < r.i1; v += kThreads) sum += weight(v);
-        for (int o = 1; o < 64; o <<= 1) sum += shfl_xor(sum, o);
-        if (lane == 0) waves[wave] = sum;
-        __syncthreads();
+        const double sum = w.sum(sp * a.part_len, min(a.V, (sp + 1) * a.part_len));
         if (threadIdx.x == 0) {
-            sum = 0.0;
-            for (int w = 0; w < kThreads / 64; ++w) sum += waves[w];
             __hip_atomic_store(a.sums + (size_t)b * a.split + sp, sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             // the store has completed before the ticket is taken
             __builtin_amdgcn_s_waitcnt(0);
             last_arrival = __hip_atomic_fetch_add(a.ticket + b, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == a.split - 1;
+            if (last_arrival) a.ticket[b] = 0;    // ready for the next launch
         }
         __syncthreads();
         if (!last_arrival) return;
     }
-    if (wave == 0) {
-        // the part that holds the drawn point: the first whose running sum passes it
-        const double s = lane < a.split ? __hip_atomic_load(a.sums + (size_t)b * a.split + lane, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0.0;
-        double run = s;
-        for (int o = 1; o < 64; o <<= 1) {
-            const double y = shfl_up(run, o);
-            if (lane >= o) run += y;
-        }
-        double W = run;                           // of the last lane
-        for (int o = 1; o < 64; o <<= 1) W = fmax(W, shfl_xor(W, o));
-        const double point = (double)a.u[(size_t)b * (a.N + 1) + a.N] * W;
-        const uint64_t past = __ballot(run > point), some = __ballot(s > 0.0);
-        // beyond the end (a random number of 1 and more): the last part of any weight
-        const int at = past ? __builtin_ctzll(past) : some ? 63 - __builtin_clzll(some) : -1;
-        if (lane == max(at, 0)) base_lds = point - (run - s);     // still to go within the part
-        if (lane == 0) {
-            part_lds = at;
-            found = kNone;
-            last_of_weight = -1;
-            a.ticket[b] = 0;                      // ready for the next launch
-        }
-    }
-    __syncthreads();
-    if (part_lds < 0 && e.c_before < 0.0) {       // nothing has any weight
-        if (threadIdx.x == 0) a.next[b] = -1;
-        return;
-    }
-    Range r = part_range(x, a.V, max(part_lds, 0), a.split);
-    if (part_lds < 0) {
+    const double u = a.u[(size_t)b * (a.N + 1) + a.N];
+    const double s = lane < a.split ? __hip_atomic_load(a.sums + (size_t)b * a.split + lane, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0.0;
+    double left;
+    const int part = part_of_point(s, u, left);
+    int i0 = part * a.part_len, i1 = min(a.V, (part + 1) * a.part_len);
+    if (part < 0) {
         // nothing is left by the last rejection, which then changes nothing: the whole row with
         // the weights before it
-        e.c = e.c_before;
-        r = Range{0, 0, a.V};
-        double sum = 0.0;
-        for (int v = threadIdx.x; v < a.V; v += kThreads) sum += weight(v);
-        for (int o = 1; o < 64; o <<= 1) sum += shfl_xor(sum, o);
-        if (lane == 0) waves[wave] = sum;
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            sum = 0.0;
-            for (int w = 0; w < kThreads / 64; ++w) sum += waves[w];
-            base_lds = (double)a.u[(size_t)b * (a.N + 1) + a.N] * sum;
-        }
-        __syncthreads();
+        w.c = e.c_before;
+        left = u * w.sum(0, a.V);
+        i0 = 0;
+        i1 = a.V;
     }
-    // the same within the part, a run of neighbouring tokens per thread
-    const int per = (r.i1 - r.i0 + kThreads - 1) / kThreads;
-    const int v0 = min(r.i1, r.i0 + (int)threadIdx.x * per), v1 = min(r.i1, v0 + per);
-    double mine = 0.0;
-    for (int v = v0; v < v1; ++v) mine += weight(v);
-    double run = mine;
-    for (int o = 1; o < 64; o <<= 1) {
-        const double y = shfl_up(run, o);
-        if (lane >= o) run += y;
-    }
-    __syncthreads();
-    if (lane == 63) waves[wave] = run;
-    __syncthreads();
-    for (int w = 0; w < wave; ++w) run += waves[w];
-    double before = run - mine;
-    int first = kNone, last = -1;
-    for (int v = v0; v < v1; ++v) {
-        const double w = weight(v);
-        before += w;
-        if (w > 0.0) last = v;
-        if (before > base_lds && w > 0.0 && first == kNone) first = v;
-    }
-    if (first != kNone) atomicMin(&found, first);
-    if (last >= 0) atomicMax(&last_of_weight, last);
-    __syncthreads();
-    // the parts' sums and these round differently: then it is the part's last token of any weight
-    if (threadIdx.x == 0) a.next[b] = found != kNone ? found : last_of_weight;
+    const int tok = w.find(i0, i1, left);
+    if (threadIdx.x == 0) a.next[b] = tok;
 }
 
 }  // namespace
 
-int verify_split(int rows, int V) {
-    int split = kVerifySplitMax;
-    while (split > 1 && ((int64_t)split * rows > 4096 || split * 1024 > V)) split >>= 1;
-    return split;
+// Parts of 4096 logits, as many as a workgroup's threads hold in registers; longer ones for
+// vocabularies of more than 64 such parts.
+int verify_part_len(int V) {
+    const int most = kVerifySplitMax * 4096;
+    return 4096 * ((V + most - 1) / most);
 }
 
-hipError_t launch_verify(const VerifyArgs& a, hipStream_t s) {
+hipError_t launch_verify(const VerifyArgs& args, hipStream_t s) {
+    VerifyArgs a = args;
+    a.part_len = verify_part_len(a.V);
+    a.split = (a.V + a.part_len - 1) / a.part_len;
     hipLaunchKernelGGL(verify_sums_kernel, dim3(a.split, a.N + 1, a.B), dim3(kThreads), 0, s, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(verify_walk_kernel, dim3(a.B), dim3(a.probs ? kWalkThreads : 256), 0, s, a);
+    hipLaunchKernelGGL(verify_walk_kernel, dim3(a.B), dim3(kWalkThreads), 0, s, a);
     e = hipGetLastError();
-    if (e != hipSuccess || a.inv_t == 0.0) return e;
-    hipLaunchKernelGGL(verify_draw_kernel, dim3(a.split, a.B), dim3(kThreads), 0, s, a);
+    if (e != hipSuccess || !a.probs) return e;
+    hipLaunchKernelGGL(verify_rest_kernel, dim3(a.split, a.B), dim3(kThreads), 0, s, a);
     return hipGetLastError();
 }
 
