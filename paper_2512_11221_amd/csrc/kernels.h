@@ -327,6 +327,7 @@ struct VerifyArgs {
     int32_t* n_path;          // [B]
     int32_t* next;            // [B]
     VerifyPart* part;         // [B][N + 1][split]
+    float2* chance;           // [B][N] a node's logit and the draft's probability behind its parent
     VerifyEnd* end;           // [B]
     double* sums;             // [B][split]
     int32_t* ticket;          // [B], zero between launches

@@ -218,6 +218,7 @@ struct asrkf_ctx {
     int32_t* verify_ticket = nullptr;   // [B]
     VerifyPart* verify_part = nullptr;  // [B][nodes + 1][kVerifySplitMax]
     VerifyEnd* verify_end = nullptr;    // [B]
+    float2* verify_chance = nullptr;    // [B][nodes]
     double* verify_sums = nullptr;      // [B][kVerifySplitMax]
     float* draft_acc = nullptr;
     float* draft_ml = nullptr;
@@ -1480,16 +1481,16 @@ asrkf_status asrkf_reserve_drafts(asrkf_ctx* ctx, int32_t max_nodes) {
         ml = std::max(ml, (size_t)2 * ctx->draft_grid[i] * rows * 2 * 4);
     }
     const size_t B = (size_t)c.batch;
-    void* parts[8] = {};
-    const size_t bytes[8] = {B * c.n_kv_heads * 2 * 4, 4, B * 4, B * (max_nodes + 1) * kVerifySplitMax * sizeof(VerifyPart),
-                             B * sizeof(VerifyEnd), B * kVerifySplitMax * 8, acc, ml};
+    void* parts[9] = {};
+    const size_t bytes[9] = {B * c.n_kv_heads * 2 * 4, 4, B * 4, B * (max_nodes + 1) * kVerifySplitMax * sizeof(VerifyPart),
+                             B * sizeof(VerifyEnd), B * kVerifySplitMax * 8, acc, ml, B * max_nodes * sizeof(float2)};
     size_t total = 0;
     for (size_t x : bytes) total += (x + 255) / 256 * 256;
     void* space = nullptr;
     st = dev_alloc(ctx, &space, total);
     if (st != ASRKF_OK) return st;
     size_t at = 0, cleared = 0;
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < 9; ++i) {
         parts[i] = static_cast<char*>(space) + at;
         at += (bytes[i] + 255) / 256 * 256;
         if (i == 2) cleared = at;                  // the tickets
@@ -1514,6 +1515,7 @@ asrkf_status asrkf_reserve_drafts(asrkf_ctx* ctx, int32_t max_nodes) {
     ctx->verify_sums = static_cast<double*>(parts[5]);
     ctx->draft_acc = static_cast<float*>(parts[6]);
     ctx->draft_ml = static_cast<float*>(parts[7]);
+    ctx->verify_chance = static_cast<float2*>(parts[8]);
     ctx->draft_nodes = max_nodes;
     return ASRKF_OK;
 }
@@ -1671,6 +1673,7 @@ asrkf_status asrkf_verify_drafts(asrkf_ctx* ctx, int32_t n_nodes, const int32_t*
     a.next = next;
     a.part = ctx->verify_part;
     a.end = ctx->verify_end;
+    a.chance = ctx->verify_chance;
     a.sums = ctx->verify_sums;
     a.ticket = ctx->verify_ticket;
     a.B = c.batch;

@@ -27,39 +27,77 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// 2^x for x <= 0, to 3e-15 of it: the nearest integer apart, the exponential's series on |y| <= ln 2 / 2.
+// 2^x for x <= 0: 2^k (1 + f P(f)), k the nearest integer and f = x - k.  P interpolates (2^f - 1) / f at the
+// nine Chebyshev nodes of [-1/2, 1/2], which leaves 3.7e-14 of the result; 2^0 is 1.  Below -1080,
+// and at -infinity, it is 0.
 __device__ __forceinline__ double exp2_64(double x) {
-    x = fmax(x, -1080.0);                         // below: 0 (subnormals do not matter here); a NaN:
-    const double k = rint(x);                     //   the caller's, who adds x to the sum
-    const double y = (x - k) * 0.693147180559945309417;
-    double r = fma(y, 1.0 / 39916800.0, 1.0 / 3628800.0);
-    r = fma(y, r, 1.0 / 362880.0);
-    r = fma(y, r, 1.0 / 40320.0);
-    r = fma(y, r, 1.0 / 5040.0);
-    r = fma(y, r, 1.0 / 720.0);
-    r = fma(y, r, 1.0 / 120.0);
-    r = fma(y, r, 1.0 / 24.0);
-    r = fma(y, r, 1.0 / 6.0);
-    r = fma(y, r, 0.5);
-    r = fma(y, r, 1.0);
-    r = fma(y, r, 1.0);
+    x = fmax(x, -1080.0);
+    const double k = rint(x), f = x - k;
+    double r = 1.0203121063391729e-07;
+    r = fma(r, f, 1.3255224878668817e-06);
+    r = fma(r, f, 1.525268684626772e-05);
+    r = fma(r, f, 0.00015403455852453838);
+    r = fma(r, f, 0.0013333558179043112);
+    r = fma(r, f, 0.009618129159402558);
+    r = fma(r, f, 0.055504108664760424);
+    r = fma(r, f, 0.2402265069581299);
+    r = fma(r, f, 0.6931471805599453);
+    r = fma(r, f, 1.0);
     return __builtin_ldexp(r, (int)k);
 }
+// e^((x - m) / T), m / T in units of ln 2 given.  (Its rounding is one factor for a whole row's weights.)
+__device__ __forceinline__ double exp_of(float x, double inv_t, double m_t) { return exp2_64(fma((double)x, inv_t, -m_t)); }
 
-__device__ __forceinline__ double shfl_xor(double x, int o) {
+// Sums over a wave's lanes in six DPP steps: within rows of 16, then the rows before.  (Each is a
+// few cycles where a permute through LDS is a round trip: the walk of 8 chains took 16.6 us with those.)
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double moved(double x) {
     const unsigned long long b = __double_as_longlong(x);
-    const unsigned lo = __shfl_xor((unsigned)b, o), hi = __shfl_xor((unsigned)(b >> 32), o);
+    const unsigned lo = __builtin_amdgcn_update_dpp(0, (int)b, CTRL, ROWS, 0xF, false);
+    const unsigned hi = __builtin_amdgcn_update_dpp(0, (int)(b >> 32), CTRL, ROWS, 0xF, false);
     return __longlong_as_double(((unsigned long long)hi << 32) | lo);
 }
-__device__ __forceinline__ double shfl_up(double x, int o) {
-    const unsigned long long b = __double_as_longlong(x);
-    const unsigned lo = __shfl_up((unsigned)b, o), hi = __shfl_up((unsigned)(b >> 32), o);
-    return __longlong_as_double(((unsigned long long)hi << 32) | lo);
-}
-
-__device__ __forceinline__ double wave_sum(double x) {
-    for (int o = 1; o < 64; o <<= 1) x += shfl_xor(x, o);
+__device__ __forceinline__ double running_sum(double x) {
+    x += moved<0x111, 0xF>(x);                    // row_shr 1, 2, 4, 8: zeros come in
+    x += moved<0x112, 0xF>(x);
+    x += moved<0x114, 0xF>(x);
+    x += moved<0x118, 0xF>(x);
+    x += moved<0x142, 0xA>(x);                    // row_bcast 15 into rows 1 and 3
+    x += moved<0x143, 0xC>(x);                    // row_bcast 31 into rows 2 and 3
     return x;
+}
+__device__ __forceinline__ double of_lane(double x, int i) {
+    const unsigned long long b = __double_as_longlong(x);
+    return __longlong_as_double(((unsigned long long)(unsigned)__builtin_amdgcn_readlane((int)(b >> 32), i) << 32) |
+                                (unsigned)__builtin_amdgcn_readlane((int)b, i));
+}
+__device__ __forceinline__ double wave_sum(double x) { return of_lane(running_sum(x), 63); }
+
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float max_moved(float x) {
+    return fmaxf(x, __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(x), __float_as_int(x), CTRL, ROWS, 0xF, false)));
+}
+__device__ __forceinline__ float wave_max(float x) {
+    x = max_moved<0x111, 0xF>(x);
+    x = max_moved<0x112, 0xF>(x);
+    x = max_moved<0x114, 0xF>(x);
+    x = max_moved<0x118, 0xF>(x);
+    x = max_moved<0x142, 0xA>(x);
+    x = max_moved<0x143, 0xC>(x);
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int min_moved(int x) {
+    return min(x, __builtin_amdgcn_update_dpp(x, x, CTRL, ROWS, 0xF, false));
+}
+__device__ __forceinline__ int wave_min(int x) {
+    x = min_moved<0x111, 0xF>(x);
+    x = min_moved<0x112, 0xF>(x);
+    x = min_moved<0x114, 0xF>(x);
+    x = min_moved<0x118, 0xF>(x);
+    x = min_moved<0x142, 0xA>(x);
+    x = min_moved<0x143, 0xC>(x);
+    return __builtin_amdgcn_readlane(x, 63);
 }
 
 constexpr int kNone = 0x7FFFFFFF;
@@ -92,18 +130,25 @@ __device__ __forceinline__ floatx4 load4(const float* x, int i, int end, float f
 
 // ---- the sums of every row ----
 
-// A workgroup's part: its maximum first, over the values it holds in registers, then the sum with one
-// exponential to a value.
+// A workgroup's part: its maximum first, over the values it holds in registers, then (greedy) that
+// maximum's first index, or the sum with one exponential to a value.
+template <bool GREEDY>
 __global__ void __launch_bounds__(kThreads)
 verify_sums_kernel(VerifyArgs a) {
     constexpr int kWaves = kThreads / 64, kQuads = 4;
     __shared__ float top_lds[2][kWaves];
-    __shared__ int at_lds[2][kWaves];
     __shared__ double sum_lds[kWaves];
+    __shared__ int at_lds[kWaves], bad_lds[kWaves];
     const int sp = blockIdx.x, row = blockIdx.y, b = blockIdx.z, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    if (row > nodes_of(a, b)) return;
+    const int nodes = nodes_of(a, b);
+    if (row > nodes) return;
     const float* x = row_of(a, b, row);
     const int i0 = sp * a.part_len, i1 = min(a.V, i0 + a.part_len);
+    int child = -1;                               // the token of a child of this row, a node to a lane of wave 0
+    if (!GREEDY && wave == 0 && lane < nodes) {
+        const int parent = a.parents[(size_t)b * a.N + lane], token = a.tokens[(size_t)b * a.N + lane];
+        if (parent + 1 == row && lane >= row) child = token;
+    }
     float m = -INFINITY;
     int at = kNone;
     double S = 0.0;                               // the thread's own values, against m
@@ -113,81 +158,88 @@ verify_sums_kernel(VerifyArgs a) {
 #pragma unroll
         for (int u = 0; u < kQuads; ++u) v[u] = load4(x, j + (u * kThreads + threadIdx.x) * 4, i1, -INFINITY);
         float top = -INFINITY;
-        int where = kNone;
 #pragma unroll
         for (int u = 0; u < kQuads; ++u)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 bad |= !(v[u][e] < INFINITY);
-                if (v[u][e] > top) {              // the first of equals
-                    top = v[u][e];
-                    where = j + (u * kThreads + (int)threadIdx.x) * 4 + e;
-                }
+                top = fmaxf(top, v[u][e]);
             }
-        for (int o = 1; o < 64; o <<= 1) {
-            const float y = __shfl_xor(top, o);
-            const int z = __shfl_xor(where, o);
-            where = y > top ? z : y == top ? min(where, z) : where;
-            top = fmaxf(top, y);
-        }
-        if (lane == 0) {
-            top_lds[turn & 1][wave] = top;
-            at_lds[turn & 1][wave] = where;
-        }
+        top = wave_max(top);
+        if (lane == 0) top_lds[turn & 1][wave] = top;
         __syncthreads();
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            const float y = top_lds[turn & 1][w];
-            const int z = at_lds[turn & 1][w];
-            where = y > top ? z : y == top ? min(where, z) : where;
-            top = fmaxf(top, y);
-        }
+        for (int w = 0; w < kWaves; ++w) top = fmaxf(top, top_lds[turn & 1][w]);
         if (top > m) {
-            S = m == -INFINITY ? 0.0 : S * exp2_64(((double)m - top) * a.inv_t);
+            if (!GREEDY && m > -INFINITY) S *= exp2_64(((double)m - top) * a.inv_t);
             m = top;
-            at = where;
+            at = kNone;
         }
-        if (a.inv_t != 0.0 && m > -INFINITY && m < INFINITY) {
+        if constexpr (GREEDY) {
 #pragma unroll
             for (int u = 0; u < kQuads; ++u)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) S += v[u][e] == -INFINITY ? 0.0 : exp2_64(((double)v[u][e] - m) * a.inv_t);
+                for (int e = 0; e < 4; ++e)
+                    if (v[u][e] == m && top == m) at = min(at, j + (u * kThreads + (int)threadIdx.x) * 4 + e);
+        } else if (m > -INFINITY && m < INFINITY) {
+            const double m_t = m * a.inv_t;
+#pragma unroll
+            for (int u = 0; u < kQuads; ++u)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) S += exp_of(v[u][e], a.inv_t, m_t);
         }
     }
-    S = wave_sum(S);
-    if (lane == 0) sum_lds[wave] = S;
-    const bool any_bad = __syncthreads_or(bad);
+    // what the walk looks up: the logit and the draft's probability of the children in this part
+    if (!GREEDY && child >= i0 && child < i1)
+        a.chance[(size_t)b * a.N + lane] = make_float2(x[child], a.probs ? draft_row(a, b, row)[child] : 1.f);
+    if constexpr (GREEDY) at = wave_min(at);
+    else S = wave_sum(S);
+    const bool wave_bad = __any(bad);
+    if (lane == 0) {
+        sum_lds[wave] = S;
+        at_lds[wave] = at;
+        bad_lds[wave] = wave_bad;
+    }
+    __syncthreads();
     if (threadIdx.x == 0) {
         S = 0.0;
-        for (int w = 0; w < kWaves; ++w) S += sum_lds[w];
+        int any_bad = 0;
+        for (int w = 0; w < kWaves; ++w) {
+            S += sum_lds[w];
+            at = min(at, at_lds[w]);
+            any_bad |= bad_lds[w];
+        }
         a.part[((size_t)b * (a.N + 1) + row) * a.split + sp] = VerifyPart{S, m, any_bad ? -1 : at};
     }
 }
 
 // ---- the walk and the draw ----
 
-// e^((x - m) / T) scale - c q of a token, not below 0
-__device__ __forceinline__ double weight_of(float x, float m, double inv_t, double scale, double c, double q) {
-    return fmax(x == -INFINITY ? -c * q : exp2_64(((double)x - m) * inv_t) * scale - c * q, 0.0);
-}
-
-// The weights behind a row, and what a workgroup does with a range of them.
+// The weights max(e^((x - m) / T) scale - c q, 0) behind a row, and what a workgroup does with a range of them.
 template <int THREADS>
 struct Weights {
     static constexpr int kWaves = THREADS / 64;
     const float* x;
     const float* q;               // null: c is 0
-    float m;
-    double inv_t, scale, c;
-    const int* gone;              // LDS: tokens without weight
-    int n_gone;
-    double* lds;                  // [kWaves + 1]
+    double inv_t, m_t, scale, c;
+    int n_gone, gone;             // tokens without weight, one to a lane
+    double* lds;                  // [kWaves]
     int* found;                   // LDS, [2]
 
-    __device__ __forceinline__ double of(int v, float xv, float qv) const {
-        double w = weight_of(xv, m, inv_t, scale, c, (double)qv);
-        for (int i = 0; i < n_gone; ++i) w = gone[i] == v ? 0.0 : w;
-        return w;
+    // of four tokens from v on
+    __device__ __forceinline__ void four(floatx4 xv, floatx4 qv, double (&w)[4]) const {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            w[e] = exp_of(xv[e], inv_t, m_t) * scale;
+            if (q) w[e] = fmax(w[e] - c * (double)qv[e], 0.0);
+        }
+    }
+    __device__ __forceinline__ void leave_out(int v, double (&w)[4]) const {
+        for (int i = 0; i < n_gone; ++i) {
+            const int g = __builtin_amdgcn_readlane(gone, i) - v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = g == e ? 0.0 : w[e];
+        }
     }
     __device__ __forceinline__ double block_sum(double s) const {
         s = wave_sum(s);
@@ -198,9 +250,9 @@ struct Weights {
         for (int w = 0; w < kWaves; ++w) s += lds[w];
         return s;
     }
-    // of [i0, i1), in every thread
+    // of [i0, i1), in every thread; kQuads quads of a thread in flight
+    template <int kQuads>
     __device__ __forceinline__ double sum(int i0, int i1) const {
-        constexpr int kQuads = 2;
         double s = 0.0;
         for (int j = i0; j < i1; j += THREADS * kQuads * 4) {
             floatx4 xv[kQuads], qv[kQuads];
@@ -211,11 +263,33 @@ struct Weights {
                 qv[u] = q ? load4(q, i, i1, 0.f) : floatx4{0.f, 0.f, 0.f, 0.f};
             }
 #pragma unroll
-            for (int u = 0; u < kQuads; ++u)
+            for (int u = 0; u < kQuads; ++u) {
+                double w[4];
+                four(xv[u], qv[u], w);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s += of(j + (u * THREADS + threadIdx.x) * 4 + e, xv[u][e], qv[u][e]);
+                for (int e = 0; e < 4; ++e) s += w[e];
+            }
         }
         return block_sum(s);
+    }
+    // ... in a wave alone, in its lanes
+    __device__ __forceinline__ double wave_sum_of(int i0, int i1) const {
+        constexpr int kQuads = 8;
+        double s = 0.0;
+        for (int j = i0; j < i1; j += 64 * kQuads * 4) {
+            floatx4 xv[kQuads];
+#pragma unroll
+            for (int u = 0; u < kQuads; ++u) xv[u] = load4(x, j + (u * 64 + (int)(threadIdx.x & 63)) * 4, i1, -INFINITY);
+#pragma unroll
+            for (int u = 0; u < kQuads; ++u) {
+                double w[4];
+                four(xv[u], floatx4{0.f, 0.f, 0.f, 0.f}, w);
+                leave_out(j + (u * 64 + (int)(threadIdx.x & 63)) * 4, w);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s += w[e];
+            }
+        }
+        return wave_sum(s);
     }
     // The first token of [i0, i1) whose running sum passes point; where rounding leaves none, the last
     // of any weight; -1 without weights.  In every thread.
@@ -230,8 +304,8 @@ struct Weights {
         const int v0 = min(i1, i0 + (int)threadIdx.x * per), v1 = min(i1, v0 + per);
         auto quad = [&](int v, double (&w)[4]) __attribute__((always_inline)) {
             const floatx4 xv = load4(x, v, v1, -INFINITY), qv = q ? load4(q, v, v1, 0.f) : floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = of(v + e, xv[e], qv[e]);
+            four(xv, qv, w);
+            leave_out(v, w);
         };
         double mine = 0.0, first4[4] = {0.0, 0.0, 0.0, 0.0};
         if (v0 < v1) quad(v0, first4);
@@ -243,11 +317,7 @@ struct Weights {
 #pragma unroll
             for (int e = 0; e < 4; ++e) mine += w[e];
         }
-        double run = mine;
-        for (int o = 1; o < 64; o <<= 1) {
-            const double y = shfl_up(run, o);
-            if (lane >= o) run += y;
-        }
+        double run = running_sum(mine);
         __syncthreads();
         if (lane == 63) lds[wave] = run;
         __syncthreads();
@@ -276,21 +346,11 @@ struct Weights {
 // passes it; beyond the end (a random number of 1 and more) the last of any weight; -1 without weights.
 // left: what is still to go within it.
 __device__ __forceinline__ int part_of_point(double s, double u, double& left) {
-    const int lane = threadIdx.x & 63;
-    double run = s;
-    for (int o = 1; o < 64; o <<= 1) {
-        const double y = shfl_up(run, o);
-        if (lane >= o) run += y;
-    }
-    double W = run;                               // the last lane's
-    for (int o = 1; o < 64; o <<= 1) W = fmax(W, shfl_xor(W, o));
-    const double point = u * W;
+    const double run = running_sum(s);
+    const double point = u * of_lane(run, 63);
     const uint64_t past = __ballot(run > point), some = __ballot(s > 0.0);
     const int at = past ? __builtin_ctzll(past) : some ? 63 - __builtin_clzll(some) : -1;
-    const double rest = point - (run - s);
-    const unsigned long long bits = __double_as_longlong(rest);
-    const int from = max(at, 0);
-    left = __longlong_as_double(((unsigned long long)(unsigned)__shfl((int)(bits >> 32), from) << 32) | (unsigned)__shfl((int)bits, from));
+    left = of_lane(point - (run - s), max(at, 0));
     return at;
 }
 
@@ -299,53 +359,57 @@ constexpr int kWalkThreads = 1024;
 __global__ void __launch_bounds__(kWalkThreads)
 verify_walk_kernel(VerifyArgs a) {
     __shared__ VerifyPart rows[kMaxDrafts + 1];
+    __shared__ double share[kMaxDrafts + 1][kVerifySplitMax];    // of a row's sum, by part
     __shared__ double sums[kWalkThreads / 64];
-    __shared__ int gone[kMaxDrafts], found[2];
+    __shared__ int gone_lds[kMaxDrafts], found[2];
     const int b = blockIdx.x, nodes = nodes_of(a, b);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const VerifyPart* parts = a.part + (size_t)b * (a.N + 1) * a.split;
     // a node to a lane, in every wave
     int parent = -2, token = -1;                  // -2: nobody's child; a token below 0 weighs nothing
-    float u = 0.f;
+    float u = 0.f, u_last = 0.f;
+    float2 chance = make_float2(-INFINITY, 1.f);  // its logit and the draft's probability
     if (lane < nodes) {
-        const int p = a.parents[(size_t)b * a.N + lane], x = a.tokens[(size_t)b * a.N + lane];
-        parent = p >= -1 && p < lane ? p : -2;
-        token = (uint32_t)x < (uint32_t)a.V ? x : -1;
-        if (a.inv_t != 0.0) u = a.u[(size_t)b * (a.N + 1) + lane];
+        parent = a.parents[(size_t)b * a.N + lane];
+        token = a.tokens[(size_t)b * a.N + lane];
     }
-    float logit = -INFINITY, q_own = 1.f;
-    if (parent >= -1 && token >= 0 && a.inv_t != 0.0) {
-        logit = row_of(a, b, parent + 1)[token];
-        if (a.probs) q_own = draft_row(a, b, parent + 1)[token];
-    }
-    for (int row = wave; row <= nodes; row += kWalkThreads / 64) {
-        VerifyPart p{0.0, -INFINITY, kNone};
-        if (lane < a.split) p = a.part[((size_t)b * (a.N + 1) + row) * a.split + lane];
-        float m = p.m;
-        int at = p.at;
-        for (int o = 1; o < 64; o <<= 1) {
-            const float y = __shfl_xor(m, o);
-            const int z = __shfl_xor(at, o);
-            // a part without distribution (-1) takes all
-            at = min(at, z) < 0 ? -1 : y > m ? z : y == m ? min(at, z) : at;
-            m = fmaxf(m, y);
+    VerifyPart mine{0.0, -INFINITY, kNone};       // (the first of the wave's rows, asked for before the tokens are here)
+    if (lane < a.split && wave <= nodes) mine = parts[wave * a.split + lane];
+    if (a.inv_t != 0.0) {
+        if (lane < nodes) {
+            u = a.u[(size_t)b * (a.N + 1) + lane];
+            chance = a.chance[(size_t)b * a.N + lane];
         }
-        double S = 0.0;
-        if (a.inv_t != 0.0) S = wave_sum(p.m == -INFINITY || at < 0 ? 0.0 : p.S * exp2_64(((double)p.m - m) * a.inv_t));
-        if (lane == 0) rows[row] = VerifyPart{S, m, m == -INFINITY ? -1 : at};
+        u_last = a.u[(size_t)b * (a.N + 1) + a.N];
+    }
+    parent = parent >= -1 && parent < lane ? parent : -2;
+    token = (uint32_t)token < (uint32_t)a.V ? token : -1;
+    for (int row = wave; row <= nodes; row += kWalkThreads / 64) {
+        VerifyPart p = mine;
+        if (row != wave) {
+            p = VerifyPart{0.0, -INFINITY, kNone};
+            if (lane < a.split) p = parts[row * a.split + lane];
+        }
+        const float m = wave_max(p.m);
+        const bool none = __any(p.at < 0) || m == -INFINITY;
+        if (a.inv_t == 0.0) {
+            const int at = wave_min(p.m == m ? p.at : kNone);
+            if (lane == 0) rows[row] = VerifyPart{0.0, m, none ? -1 : at};
+        } else {
+            const double s = p.m == -INFINITY || none ? 0.0 : p.S * exp2_64(((double)p.m - m) * a.inv_t);
+            const double S = wave_sum(s);
+            share[row][lane] = s / S;
+            if (lane == 0) rows[row] = VerifyPart{S, m, none ? -1 : 0};
+        }
     }
     __syncthreads();
     double mass = 0.0;                            // p(x) behind the parent
     if (parent >= -1 && token >= 0 && a.inv_t != 0.0) {
         const VerifyPart p = rows[parent + 1];
-        if (p.at >= 0) mass = weight_of(logit, p.m, a.inv_t, 1.0 / p.S, 0.0, 0.0);
+        if (p.at >= 0) mass = exp_of(chance.x, a.inv_t, p.m * a.inv_t) / p.S;
     }
-    const double q = q_own;
+    const double q = chance.y;
 
-    auto of_lane = [&](double x, int i) __attribute__((always_inline)) {
-        const unsigned long long bits = __double_as_longlong(x);
-        return __longlong_as_double(((unsigned long long)(unsigned)__builtin_amdgcn_readlane((int)(bits >> 32), i) << 32) |
-                                    (unsigned)__builtin_amdgcn_readlane((int)bits, i));
-    };
     int last = -1, n_path = 0;
     double W = 1.0, c = 0.0, c_before = -1.0;     // w = max(p - c q, 0), W its sum
     uint64_t rejected = 0;                        // since the last one kept
@@ -387,8 +451,8 @@ verify_walk_kernel(VerifyArgs a) {
                 c = c2;
                 break;
             }
-            const Weights<kWalkThreads> w{row_of(a, b, last + 1), draft_row(a, b, last + 1), p.m, a.inv_t, 1.0 / p.S, c2, gone, 0, sums, found};
-            const double sum = w.sum(0, a.V);
+            const Weights<kWalkThreads> w{row_of(a, b, last + 1), draft_row(a, b, last + 1), a.inv_t, p.m * a.inv_t, 1.0 / p.S, c2, 0, 0, sums, found};
+            const double sum = w.template sum<4>(0, a.V);
             if (sum > 0.0) {
                 c = c2;
                 W = sum;
@@ -406,39 +470,44 @@ verify_walk_kernel(VerifyArgs a) {
 
     // the draw from p without the rejected tokens
     const int n_gone = a.probs ? 0 : __popcll(rejected);
-    if (n_gone && wave == 0 && (rejected >> lane & 1)) gone[__popcll(rejected & ((1ull << lane) - 1ull))] = token;
-    __syncthreads();
-    const Weights<kWalkThreads> w{row_of(a, b, last + 1), nullptr, p.m, a.inv_t, 1.0 / p.S, 0.0, gone, n_gone, sums, found};
-    double s = 0.0;
-    if (lane < a.split) {
-        const VerifyPart mine = a.part[((size_t)b * (a.N + 1) + last + 1) * a.split + lane];
-        if (mine.m > -INFINITY) s = mine.S * exp2_64(((double)mine.m - p.m) * a.inv_t) * w.scale;
-    }
-    uint64_t again = 0;                           // parts that hold a rejected token: summed without it
-    for (int i = 0; i < n_gone; ++i) again |= 1ull << (gone[i] / a.part_len);
-    for (; again; again &= again - 1) {
-        const int sp = __builtin_ctzll(again);
-        const double sum = w.sum(sp * a.part_len, min(a.V, (sp + 1) * a.part_len));
-        if (lane == sp) s = sum;
+    if (n_gone && wave == 0 && (rejected >> lane & 1)) gone_lds[__popcll(rejected & ((1ull << lane) - 1ull))] = token;
+    if (n_gone) __syncthreads();
+    const int gone = lane < n_gone ? gone_lds[lane] : -1;
+    const Weights<kWalkThreads> w{row_of(a, b, last + 1), nullptr, a.inv_t, p.m * a.inv_t, 1.0 / p.S, 0.0, n_gone, gone, sums, found};
+    double s = share[last + 1][lane];
+    // parts that hold a rejected token are summed again without it, a wave to a part
+    uint64_t again = 0;
+    for (int i = 0; i < n_gone; ++i) again |= 1ull << (__builtin_amdgcn_readlane(gone, i) / a.part_len);
+    if (again) {
+        int turn = 0;
+        for (uint64_t left = again; left; left &= left - 1, ++turn) {
+            if (turn % (kWalkThreads / 64) != wave) continue;
+            const int sp = __builtin_ctzll(left);
+            const double sum = w.wave_sum_of(sp * a.part_len, min(a.V, (sp + 1) * a.part_len));
+            if (lane == 0) share[last + 1][sp] = sum;
+        }
+        __syncthreads();
+        s = share[last + 1][lane];
     }
     double left;
-    const int sp = part_of_point(s, (double)a.u[(size_t)b * (a.N + 1) + a.N], left);
+    const int sp = part_of_point(s, (double)u_last, left);
     const int tok = sp < 0 ? -1 : w.find(sp * a.part_len, min(a.V, (sp + 1) * a.part_len), left);
     if (threadIdx.x == 0) a.next[b] = tok;
 }
 
 // ---- the draw from what a rejection has left ----
 
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kWalkThreads)
 verify_rest_kernel(VerifyArgs a) {
-    __shared__ double lds[kThreads / 64];
+    __shared__ double lds[kWalkThreads / 64];
     __shared__ int last_arrival, found[2];
     const int sp = blockIdx.x, b = blockIdx.y, lane = threadIdx.x & 63;
     const VerifyEnd e = a.end[b];
+    const double u = a.u[(size_t)b * (a.N + 1) + a.N];
     if (e.row < 0) return;
-    Weights<kThreads> w{row_of(a, b, e.row), draft_row(a, b, e.row), e.m, a.inv_t, e.scale, e.c, nullptr, 0, lds, found};
+    Weights<kWalkThreads> w{row_of(a, b, e.row), draft_row(a, b, e.row), a.inv_t, e.m * a.inv_t, e.scale, e.c, 0, 0, lds, found};
     {
-        const double sum = w.sum(sp * a.part_len, min(a.V, (sp + 1) * a.part_len));
+        const double sum = w.template sum<1>(sp * a.part_len, min(a.V, (sp + 1) * a.part_len));
         if (threadIdx.x == 0) {
             __hip_atomic_store(a.sums + (size_t)b * a.split + sp, sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             // the store has completed before the ticket is taken
@@ -449,7 +518,6 @@ verify_rest_kernel(VerifyArgs a) {
         __syncthreads();
         if (!last_arrival) return;
     }
-    const double u = a.u[(size_t)b * (a.N + 1) + a.N];
     const double s = lane < a.split ? __hip_atomic_load(a.sums + (size_t)b * a.split + lane, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0.0;
     double left;
     const int part = part_of_point(s, u, left);
@@ -458,7 +526,7 @@ verify_rest_kernel(VerifyArgs a) {
         // nothing is left by the last rejection, which then changes nothing: the whole row with
         // the weights before it
         w.c = e.c_before;
-        left = u * w.sum(0, a.V);
+        left = u * w.template sum<2>(0, a.V);
         i0 = 0;
         i1 = a.V;
     }
@@ -479,13 +547,15 @@ hipError_t launch_verify(const VerifyArgs& args, hipStream_t s) {
     VerifyArgs a = args;
     a.part_len = verify_part_len(a.V);
     a.split = (a.V + a.part_len - 1) / a.part_len;
-    hipLaunchKernelGGL(verify_sums_kernel, dim3(a.split, a.N + 1, a.B), dim3(kThreads), 0, s, a);
+    const dim3 grid(a.split, a.N + 1, a.B);
+    if (a.inv_t == 0.0) hipLaunchKernelGGL(verify_sums_kernel<true>, grid, dim3(kThreads), 0, s, a);
+    else hipLaunchKernelGGL(verify_sums_kernel<false>, grid, dim3(kThreads), 0, s, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(verify_walk_kernel, dim3(a.B), dim3(kWalkThreads), 0, s, a);
     e = hipGetLastError();
     if (e != hipSuccess || !a.probs) return e;
-    hipLaunchKernelGGL(verify_rest_kernel, dim3(a.split, a.B), dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL(verify_rest_kernel, dim3(a.split, a.B), dim3(kWalkThreads), 0, s, a);
     return hipGetLastError();
 }
 
