@@ -321,7 +321,8 @@ struct Weights {
         __syncthreads();
         if (lane == 63) lds[wave] = run;
         __syncthreads();
-        for (int w = 0; w < wave; ++w) run += lds[w];
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) run += w < wave ? lds[w] : 0.0;
         double before = run - mine;
         int first = kNone, last = -1;
         for (int v = v0; v < v1; v += 4) {
@@ -335,8 +336,10 @@ struct Weights {
                 if (before > point && w[e] > 0.0 && first == kNone) first = v + e;
             }
         }
-        if (first != kNone) atomicMin(&found[0], first);
-        if (last >= 0) atomicMax(&found[1], last);
+        // a wave's first and last are its first and last lane's that have one
+        const uint64_t firsts = __ballot(first != kNone), lasts = __ballot(last >= 0);
+        if (firsts && lane == __builtin_ctzll(firsts)) atomicMin(&found[0], first);
+        if (lasts && lane == 63 - __builtin_clzll(lasts)) atomicMax(&found[1], last);
         __syncthreads();
         return found[0] != kNone ? found[0] : found[1];
     }
@@ -362,27 +365,28 @@ verify_walk_kernel(VerifyArgs a) {
     __shared__ double share[kMaxDrafts + 1][kVerifySplitMax];    // of a row's sum, by part
     __shared__ double sums[kWalkThreads / 64];
     __shared__ int gone_lds[kMaxDrafts], found[2];
-    const int b = blockIdx.x, nodes = nodes_of(a, b);
+    const int b = blockIdx.x;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const VerifyPart* parts = a.part + (size_t)b * (a.N + 1) * a.split;
     // a node to a lane, in every wave
     int parent = -2, token = -1;                  // -2: nobody's child; a token below 0 weighs nothing
     float u = 0.f, u_last = 0.f;
     float2 chance = make_float2(-INFINITY, 1.f);  // its logit and the draft's probability
-    if (lane < nodes) {
+    if (lane < a.N) {                             // (all of the first loads go out before the count is here)
         parent = a.parents[(size_t)b * a.N + lane];
         token = a.tokens[(size_t)b * a.N + lane];
     }
     VerifyPart mine{0.0, -INFINITY, kNone};       // (the first of the wave's rows, asked for before the tokens are here)
-    if (lane < a.split && wave <= nodes) mine = parts[wave * a.split + lane];
+    if (lane < a.split && wave <= a.N) mine = parts[wave * a.split + lane];
     if (a.inv_t != 0.0) {
-        if (lane < nodes) {
+        if (lane < a.N) {
             u = a.u[(size_t)b * (a.N + 1) + lane];
             chance = a.chance[(size_t)b * a.N + lane];
         }
         u_last = a.u[(size_t)b * (a.N + 1) + a.N];
     }
-    parent = parent >= -1 && parent < lane ? parent : -2;
+    const int nodes = nodes_of(a, b);
+    parent = parent >= -1 && parent < lane && lane < nodes ? parent : -2;
     token = (uint32_t)token < (uint32_t)a.V ? token : -1;
     for (int row = wave; row <= nodes; row += kWalkThreads / 64) {
         VerifyPart p = mine;
@@ -412,7 +416,7 @@ verify_walk_kernel(VerifyArgs a) {
 
     int last = -1, n_path = 0;
     double W = 1.0, c = 0.0, c_before = -1.0;     // w = max(p - c q, 0), W its sum
-    uint64_t rejected = 0;                        // since the last one kept
+    uint64_t rejected = 0, weighed = 0;           // since the last one kept; those of them that had a weight
     uint64_t todo = ~0ull;                        // nodes not looked at yet
     for (;;) {                                    // (the same in every wave)
         const uint64_t next = __ballot(parent == last) & todo;
@@ -431,7 +435,10 @@ verify_walk_kernel(VerifyArgs a) {
                 if (a.probs) w = fmax(w - c * qi, 0.0);
                 else if (__ballot(token == x) & rejected) w = 0.0;         // a rejected sibling's token
                 yes = (double)__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(u), i)) * qi * W < w;
-                if (!yes && !a.probs) W -= w;
+                if (!yes && !a.probs) {
+                    W -= w;
+                    weighed |= w > 0.0 ? 1ull << i : 0;
+                }
             }
         }
         if (yes) {
@@ -440,7 +447,7 @@ verify_walk_kernel(VerifyArgs a) {
             last = i;
             W = 1.0;
             c = 0.0;
-            rejected = 0;
+            rejected = weighed = 0;
             continue;
         }
         if (x >= 0) rejected |= 1ull << i;
@@ -469,15 +476,20 @@ verify_walk_kernel(VerifyArgs a) {
     if (a.inv_t == 0.0 || p.at < 0 || c != 0.0) return;
 
     // the draw from p without the rejected tokens
-    const int n_gone = a.probs ? 0 : __popcll(rejected);
-    if (n_gone && wave == 0 && (rejected >> lane & 1)) gone_lds[__popcll(rejected & ((1ull << lane) - 1ull))] = token;
+    const int n_gone = __popcll(weighed);
+    if (n_gone && wave == 0 && (weighed >> lane & 1)) gone_lds[__popcll(weighed & ((1ull << lane) - 1ull))] = token;
     if (n_gone) __syncthreads();
     const int gone = lane < n_gone ? gone_lds[lane] : -1;
     const Weights<kWalkThreads> w{row_of(a, b, last + 1), nullptr, a.inv_t, p.m * a.inv_t, 1.0 / p.S, 0.0, n_gone, gone, sums, found};
-    double s = share[last + 1][lane];
-    // parts that hold a rejected token are summed again without it, a wave to a part
-    uint64_t again = 0;
-    for (int i = 0; i < n_gone; ++i) again |= 1ull << (__builtin_amdgcn_readlane(gone, i) / a.part_len);
+    const double whole = share[last + 1][lane];
+    double s = whole;
+    for (uint64_t left = weighed; left; left &= left - 1) {
+        const int i = __builtin_ctzll(left), sp = __builtin_amdgcn_readlane(token, i) / a.part_len;
+        s -= lane == sp ? of_lane(mass, i) : 0.0;
+    }
+    // a part of which next to nothing is left is summed again without those tokens, a wave to a part (what
+    // the difference is off by, 2^-52 of the whole, stays below 2^-42 of what is left)
+    const uint64_t again = __ballot(s < whole * 0x1p-10);
     if (again) {
         int turn = 0;
         for (uint64_t left = again; left; left &= left - 1, ++turn) {
@@ -487,7 +499,7 @@ verify_walk_kernel(VerifyArgs a) {
             if (lane == 0) share[last + 1][sp] = sum;
         }
         __syncthreads();
-        s = share[last + 1][lane];
+        s = again >> lane & 1 ? share[last + 1][lane] : s;
     }
     double left;
     const int sp = part_of_point(s, (double)u_last, left);
