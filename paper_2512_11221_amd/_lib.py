@@ -148,8 +148,9 @@ def _ptr(x):
 
 def _stream(s):
     if s is None:
+        # the handle alone: a torch.cuda.Stream made for it takes 2.7 us, the handle 0.5
         import torch
-        return torch.cuda.current_stream().cuda_stream
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     if isinstance(s, int):
         return s
     return s.cuda_stream
@@ -304,20 +305,21 @@ def _rows(ctx, name, x, kv, n=None):
     """Rows [..., heads, dim] of the context's type, heads and head dim as its query (kv 0) or KV
     heads (1): their number and the elements from one to the next.  The dimensions before the heads
     have to be evenly spaced."""
-    stride, shape = x.stride(), x.shape
+    shape = x.shape
     layout = ctx.layout if type(ctx) is Context else None
     if layout is not None:
-        if x.dtype != layout[3]:
+        if x.dtype is not layout[3]:
             raise AsrkfError(EINVAL, f"{name} is {x.dtype}, the context {layout[3]}")
         if len(shape) < 3 or shape[-2] != layout[kv] or shape[-1] != layout[2]:
             raise AsrkfError(EINVAL, f"{name} must be [..., {layout[kv]}, {layout[2]}], not {tuple(shape)}")
     elif len(shape) < 3:
         raise AsrkfError(EINVAL, f"{name} must be [..., heads, dim]")
-    rows = math.prod(shape[:-2])
+    rows = x.numel() // (shape[-2] * shape[-1])
     if n is not None and rows != n:
         raise AsrkfError(EINVAL, f"{name} has {rows} rows, not {n}")
-    if rows == 0:
-        return rows, 0
+    if x.is_contiguous():
+        return rows, shape[-2] * shape[-1] if rows > 1 else 0
+    stride = x.stride()
     if stride[-1] != 1 or (shape[-2] > 1 and stride[-2] != shape[-1]):
         raise ValueError(f"{name}: the heads of a token must be dense rows")
     step, size = 0, 1                # of the last dimension that has more than one row; rows behind it
@@ -335,17 +337,16 @@ def _rows(ctx, name, x, kv, n=None):
 
 
 def _array(name, x, dtype, shape, optional=False):
-    """A dense tensor of that type and shape."""
+    """The address of a dense tensor of that type and shape (None for one that may be left out)."""
     if x is None and optional:
-        return
-    if not hasattr(x, "data_ptr"):
-        return
-    if x.dtype != dtype:
+        return None
+    if x.dtype is not dtype:
         raise AsrkfError(EINVAL, f"{name} is {x.dtype}, not {dtype}")
-    if tuple(x.shape) != tuple(shape):
-        raise AsrkfError(EINVAL, f"{name} is {tuple(x.shape)}, not {tuple(shape)}")
+    if x.shape != shape:
+        raise AsrkfError(EINVAL, f"{name} is {tuple(x.shape)}, not {shape}")
     if not x.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
+    return x.data_ptr()
 
 
 def asrkf_rotate(ctx, pos, q, q_out, k, k_out, rows_per_seq=0, inverse=False, stream=None):
@@ -364,8 +365,8 @@ def asrkf_rotate(ctx, pos, q, q_out, k, k_out, rows_per_seq=0, inverse=False, st
             strides.append(step)
     if n is None:
         raise ValueError("neither q nor k")
-    if pos is not None and hasattr(pos, "data_ptr"):
-        _array("pos", pos.reshape(-1) if pos.is_contiguous() else pos, torch.int32, (n,))
+    if pos is not None and (pos.dtype is not torch.int32 or pos.numel() != n or not pos.is_contiguous()):
+        raise AsrkfError(EINVAL, f"pos must be {n} contiguous int32, not {tuple(pos.shape)} {pos.dtype}")
     _check(load().asrkf_rotate(ctx, n, rows_per_seq, _ptr(pos), _ptr(q), strides[0], _ptr(q_out), strides[1], _ptr(k), strides[2],
                                _ptr(k_out), strides[3], 1 if inverse else 0, _stream(stream)))
 
@@ -403,9 +404,9 @@ def asrkf_attend_drafts(ctx, layer, sees, q, k, v, out, count=None, stream=None)
     _rows(ctx, "out", out, 0, B * N)
     if not out.is_contiguous():
         raise ValueError("out must be contiguous")
-    _array("sees", sees, torch.uint64 if sees.dtype == torch.uint64 else torch.int64, (B, N))
-    _array("count", count, torch.int32, (B,), optional=True)
-    _check(load().asrkf_attend_drafts(ctx, layer, N, _ptr(count), _ptr(sees), _ptr(q), sq, _ptr(k), sk, _ptr(v), sv, _ptr(out),
+    sees = _array("sees", sees, torch.uint64 if sees.dtype is torch.uint64 else torch.int64, (B, N))
+    count = _array("count", count, torch.int32, (B,), optional=True)
+    _check(load().asrkf_attend_drafts(ctx, layer, N, count, sees, _ptr(q), sq, _ptr(k), sk, _ptr(v), sv, _ptr(out),
                                       _stream(stream)))
 
 
@@ -417,14 +418,11 @@ def asrkf_verify_drafts(ctx, tokens, parents, root_logits, logits, u, path, n_pa
     B, N = _tree_sizes(ctx, "tokens", tokens, 1)
     V = ctx.sizes[2] if type(ctx) is Context else root_logits.shape[-1]
     i32, f32 = torch.int32, torch.float32
-    for name, x, t, shape, optional in (("tokens", tokens, i32, (B, N), False), ("parents", parents, i32, (B, N), False),
-                                        ("path", path, i32, (B, N), False), ("n_path", n_path, i32, (B,), False),
-                                        ("next", next, i32, (B,), False), ("count", count, i32, (B,), True),
-                                        ("root_logits", root_logits, f32, (B, V), False), ("logits", logits, f32, (B, N, V), False),
-                                        ("probs", probs, f32, (B, N, V), True), ("u", u, f32, (B, N + 1), True)):
-        _array(name, x, t, shape, optional)
-    _check(load().asrkf_verify_drafts(ctx, N, _ptr(count), _ptr(tokens), _ptr(parents), _ptr(root_logits), _ptr(logits), _ptr(probs),
-                                      temperature, _ptr(u), _ptr(path), _ptr(n_path), _ptr(next), _stream(stream)))
+    _check(load().asrkf_verify_drafts(
+        ctx, N, _array("count", count, i32, (B,), True), _array("tokens", tokens, i32, (B, N)), _array("parents", parents, i32, (B, N)),
+        _array("root_logits", root_logits, f32, (B, V)), _array("logits", logits, f32, (B, N, V)), _array("probs", probs, f32, (B, N, V), True),
+        temperature, _array("u", u, f32, (B, N + 1), True), _array("path", path, i32, (B, N)), _array("n_path", n_path, i32, (B,)),
+        _array("next", next, i32, (B,)), _stream(stream)))
 
 
 def asrkf_accept_drafts(ctx, path, n_path, k, v, stream=None):
@@ -433,8 +431,7 @@ def asrkf_accept_drafts(ctx, path, n_path, k, v, stream=None):
     import torch
     B, N = _tree_sizes(ctx, "path", path, 1)
     L = ctx.sizes[0] if type(ctx) is Context else (k.shape[0] if len(k.shape) > 4 else 1)
-    _array("path", path, torch.int32, (B, N))
-    _array("n_path", n_path, torch.int32, (B,))
+    path, n_path = _array("path", path, torch.int32, (B, N)), _array("n_path", n_path, torch.int32, (B,))
     strides = []
     for name, x in (("k", k), ("v", v)):
         if len(x.shape) == 4:
@@ -445,7 +442,7 @@ def asrkf_accept_drafts(ctx, path, n_path, k, v, stream=None):
         strides += [step, x.stride()[0] if L > 1 else 0]
         if L > 1 and strides[-1] < 1:
             raise ValueError(f"{name}: layers overlap")
-    _check(load().asrkf_accept_drafts(ctx, N, _ptr(path), _ptr(n_path), _ptr(k), strides[0], strides[1], _ptr(v), strides[2],
+    _check(load().asrkf_accept_drafts(ctx, N, path, n_path, _ptr(k), strides[0], strides[1], _ptr(v), strides[2],
                                       strides[3], _stream(stream)))
 
 
