@@ -14,8 +14,10 @@
 // the scores' registers and V's transposed LDS reads.
 //
 // The tiles of all pairs are dealt to a fixed number of workgroups from the counts on the
-// device (attention_split.h).  A pair that several workgroups share leaves one partial each, and
-// the one that arrives last folds them in order.
+// device (attention_split.h).  A pair that several workgroups share leaves one partial each, which a
+// second launch folds in order.  (Folded by the workgroup that arrives last, a megabyte of partials went
+// through one compute unit: 64 rows of one sequence of 8000 tokens, 8 KV heads, took 77 us.)
+#include <algorithm>
 #include <type_traits>
 
 #include "attention_split.h"
@@ -27,7 +29,6 @@ namespace asrkf {
 namespace {
 
 constexpr int kStreamPolicy = 2;              // non-temporal: rows that one workgroup reads
-constexpr int kAgentScope = 16;               // partials: past the XCD's own L2
 constexpr int kNowhere = (int)0x80000000;     // past every buffer's range: reads as zeros
 // What a piece costs a workgroup beside its rows, in tiles.
 constexpr int kDraftPieceCost = 2;
@@ -180,6 +181,26 @@ __device__ __forceinline__ float weight(float m, float M, float scale_log2) {
     return m == M ? 1.f : __builtin_amdgcn_exp2f((m - (M == -INFINITY ? 0.f : M)) * scale_log2);
 }
 
+// Where part k of a pair lies: a workgroup has a slot in the aligned form, and else two, one for the pair
+// that it ends (or holds the middle of) and one for the pair that it begins.
+__device__ __forceinline__ int draft_slot(int first, bool aligned, int k) { return aligned ? first + k : first + (k ? 2 * k : 1); }
+
+// Four dims of a query row of (sequence, KV head), from its sums: zeros where nothing was seen.
+template <bool BF16, int D>
+__device__ __forceinline__ void write_row(const DraftArgs& a, int b, int kvh, int row, int quad, floatx4 o, float sum) {
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] *= inv;
+    const int G = a.Hq / a.Hkv, shift = __ffs(G) - 1;
+    const size_t at = (((size_t)b * a.N + (row >> shift)) * a.Hq + kvh * G + (row & (G - 1))) * D + quad * 4;
+    if constexpr (BF16) {
+        typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+        *reinterpret_cast<bf16x4*>(reinterpret_cast<__bf16*>(a.out) + at) = __builtin_convertvector(o, bf16x4);
+    } else {
+        *reinterpret_cast<floatx4*>(reinterpret_cast<float*>(a.out) + at) = o;
+    }
+}
+
 template <int ROWS, int D, int RW, int KW>
 __global__ void __launch_bounds__((Tile<ROWS, D, RW, KW>::kThreads), (Tile<ROWS, D, RW, KW>::kPerSimd))
 draft_kernel(DraftArgs a) {
@@ -188,7 +209,7 @@ draft_kernel(DraftArgs a) {
     constexpr int KB = T::kKB, NQ = T::kQRegs, NL = T::kLoads, DB = D / 32;
     __shared__ __align__(16) char lds[T::kLds];
     __shared__ float ml_lds[T::kSplit ? T::kWaves * 2 * 32 : 1];
-    __shared__ int infinite_lds, last_arrival;
+    __shared__ int infinite_lds;
     extern __shared__ __align__(16) int32_t deal_lds[];           // more than 64 sequences
 
     const int wave = wave_uniform(threadIdx.x >> 6);
@@ -487,36 +508,21 @@ draft_kernel(DraftArgs a) {
             l = __uint_as_float(y[0]) + __uint_as_float(y[1]);
         }
         const int first_slot = deal.aligned ? wave_uniform(pc.slot) - part : 2 * (w - part);
-        auto slot_of = [&](int k) __attribute__((always_inline)) {
-            return deal.aligned ? first_slot + k : first_slot + (k ? 2 * k : 1);
-        };
-        float* my_acc = a.part_acc + (size_t)slot_of(part) * T::kRows * D;
-        float* my_ml = a.part_ml + (size_t)slot_of(part) * 2 * T::kRows;
-        // four dims of row r of the block, with the row's sum
-        auto write = [&](int r, int quad, floatx4 o, float sum) __attribute__((always_inline)) {
-            if (r >= live_rows) return;
-            const float inv = sum == 0.f ? 0.f : 1.f / sum;       // nothing seen: zeros
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] *= inv;
-            const int at = r0 + r;
-            char* to = a.out + (((size_t)b * a.N + (at >> group_shift)) * a.Hq + kvh * G + (at & (G - 1))) * T::kRow + quad * 4 * T::kElem;
-            if constexpr (BF16) {
-                typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-                *reinterpret_cast<bf16x4*>(to) = __builtin_convertvector(o, bf16x4);
-            } else {
-                *reinterpret_cast<floatx4*>(to) = o;
-            }
-        };
-        const auto ra = buffer(my_acc, T::kRows * D * 4), rm = buffer(my_ml, 2 * T::kRows * 4);
+        const int slot = draft_slot(first_slot, deal.aligned, part);
+        if (part == 0 && threadIdx.x == 0)
+            a.fold[(size_t)b * a.Hkv * a.row_blocks + gi] = make_int2(deal.aligned ? n_parts : -n_parts, first_slot);
+        float* my_acc = a.part_acc + (size_t)slot * T::kRows * D;
+        float* my_ml = a.part_ml + (size_t)slot * 2 * T::kRows;
         auto finish = [&](int r, int quad, floatx4 o, float mx, float sum) __attribute__((always_inline)) {
+            if (r >= live_rows) return;
             if (n_parts == 1) {
-                write(r, quad, o, sum);
+                write_row<BF16, D>(a, b, kvh, r0 + r, quad, o, sum);
                 return;
             }
-            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(uintx4, o), ra, (quad * T::kRows + r) * 16, 0, kAgentScope);
+            *reinterpret_cast<floatx4*>(my_acc + (quad * T::kRows + r) * 4) = o;
             if (quad == 0) {
-                __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(mx), rm, r * 4, 0, kAgentScope);
-                __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(sum), rm, (T::kRows + r) * 4, 0, kAgentScope);
+                my_ml[r] = mx;
+                my_ml[T::kRows + r] = sum;
             }
         };
         __syncthreads();                                  // every wave has read its tiles
@@ -582,61 +588,58 @@ draft_kernel(DraftArgs a) {
                                floatx4{acc[d][i * 4], acc[d][i * 4 + 1], acc[d][i * 4 + 2], acc[d][i * 4 + 3]}, m, l);
             }
         }
-        if (n_parts > 1) {
-            // the device-scope stores of every thread have completed before the ticket is
-            // taken, so no cache-wide write-back is needed
-            __builtin_amdgcn_s_waitcnt(0);
-            __syncthreads();
-            int* ticket = a.ticket + (size_t)b * a.Hkv * a.row_blocks + gi;
-            if (threadIdx.x == 0)
-                last_arrival = __hip_atomic_fetch_add(ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == n_parts - 1;
-            __syncthreads();
-            if (last_arrival) {
-                const int rows = min(T::kRows, live_rows);
-                for (int e = threadIdx.x; e < T::kRows * (D / 4); e += T::kThreads) {
-                    const int r = e % T::kRows, quad = e / T::kRows;
-                    if (r >= rows) continue;
-                    float M = -INFINITY, L = 0.f;
-                    floatx4 o = {0.f, 0.f, 0.f, 0.f};
-                    constexpr int kPass = 4;              // partials in flight
-                    for (int k0 = 0; k0 < n_parts; k0 += kPass) {
-                        float pm[kPass], pl[kPass];
-                        floatx4 po[kPass];
-#pragma unroll
-                        for (int u = 0; u < kPass; ++u) {
-                            const int slot = slot_of(min(k0 + u, n_parts - 1));
-                            const auto fa = buffer(a.part_acc + (size_t)slot * T::kRows * D, T::kRows * D * 4);
-                            const auto fm = buffer(a.part_ml + (size_t)slot * 2 * T::kRows, 2 * T::kRows * 4);
-                            pm[u] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(fm, r * 4, 0, kAgentScope));
-                            pl[u] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(fm, (T::kRows + r) * 4, 0, kAgentScope));
-                            po[u] = __builtin_bit_cast(floatx4, __builtin_amdgcn_raw_buffer_load_b128(fa, e * 16, 0, kAgentScope));
-                        }
-                        float Mn = M;
-#pragma unroll
-                        for (int u = 0; u < kPass; ++u)
-                            if (k0 + u < n_parts) Mn = fmaxf(Mn, pm[u]);
-                        const float f0 = weight(M, Mn, a.scale_log2);
-                        L *= f0;
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) o[i] *= f0;
-#pragma unroll
-                        for (int u = 0; u < kPass; ++u) {
-                            if (k0 + u >= n_parts) continue;
-                            const float f = weight(pm[u], Mn, a.scale_log2);
-                            L = fmaf(f, pl[u], L);
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) o[i] = fmaf(f, po[u][i], o[i]);
-                        }
-                        M = Mn;
-                    }
-                    write(r, quad, o, L);
-                }
-                if (threadIdx.x == 0) *ticket = 0;        // ready for the next launch
-            }
-        }
         __syncthreads();                                  // the states have been read: tiles may be rewritten
     }
     }
+}
+
+// The partials of a pair folded in their order, four dims of a row to a thread, several partials in
+// flight.
+constexpr int kFoldThreads = 256;
+template <bool BF16, int D>
+__global__ void __launch_bounds__(kFoldThreads)
+fold_kernel(DraftArgs a, int rows) {
+    constexpr int kQuads = D / 4, kRowsHere = kFoldThreads / kQuads, kPass = 8;
+    const int gi = blockIdx.y, b = blockIdx.z;
+    const int2 f = a.fold[(size_t)b * a.Hkv * a.row_blocks + gi];
+    const int kvh = gi / a.row_blocks, r0 = gi % a.row_blocks * rows;
+    const int r = blockIdx.x * kRowsHere + threadIdx.x % kRowsHere, quad = threadIdx.x / kRowsHere;
+    // (pairs without nodes were not dealt: what stands there is of an earlier launch)
+    if (r >= rows || r0 + r >= nodes_of(a, b) * (a.Hq / a.Hkv)) return;
+    const bool aligned = f.x > 0;
+    const int n_parts = aligned ? f.x : -f.x;
+    if (n_parts == 1) return;
+    float M = -INFINITY, L = 0.f;
+    floatx4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int k0 = 0; k0 < n_parts; k0 += kPass) {
+        float pm[kPass], pl[kPass];
+        floatx4 po[kPass];
+#pragma unroll
+        for (int u = 0; u < kPass; ++u) {
+            const size_t slot = draft_slot(f.y, aligned, min(k0 + u, n_parts - 1));
+            pm[u] = a.part_ml[slot * 2 * rows + r];
+            pl[u] = a.part_ml[(slot * 2 + 1) * rows + r];
+            po[u] = *reinterpret_cast<const floatx4*>(a.part_acc + (slot * kQuads + quad) * rows * 4 + r * 4);
+        }
+        float Mn = M;
+#pragma unroll
+        for (int u = 0; u < kPass; ++u)
+            if (k0 + u < n_parts) Mn = fmaxf(Mn, pm[u]);
+        const float f0 = weight(M, Mn, a.scale_log2);
+        L *= f0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] *= f0;
+#pragma unroll
+        for (int u = 0; u < kPass; ++u) {
+            if (k0 + u >= n_parts) continue;
+            const float fu = weight(pm[u], Mn, a.scale_log2);
+            L = fmaf(fu, pl[u], L);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[i] = fmaf(fu, po[u][i], o[i]);
+        }
+        M = Mn;
+    }
+    write_row<BF16, D>(a, b, kvh, r0 + r, quad, o, L);
 }
 
 struct DraftLaunch {
@@ -654,6 +657,11 @@ hipError_t launch_walk(const DraftArgs& args, const DraftLaunch& l) {
     a.row_blocks = (a.N * (a.Hq / a.Hkv) + T::kRows - 1) / T::kRows;
     const size_t lds = a.B > 64 ? (size_t)(2 * a.B + 1) * 4 : 0;
     hipLaunchKernelGGL(kernel, dim3(l.blocks), dim3(T::kThreads), lds, l.stream, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    const int rows = std::min(T::kRows, a.N * (a.Hq / a.Hkv)), per = kFoldThreads / (D / 4);
+    hipLaunchKernelGGL((fold_kernel<T::kBF16, D>), dim3((rows + per - 1) / per, a.Hkv * a.row_blocks, a.B), dim3(kFoldThreads), 0, l.stream, a,
+                       T::kRows);
     return hipGetLastError();
 }
 

@@ -276,7 +276,7 @@ struct DraftArgs {
     int32_t list_tail;        // entries at a list's end whose rows are not written: 0 or 1
     float* part_acc;          // [slots][D / 4][rows][4] of the pairs that several workgroups share
     float* part_ml;           // [slots][2][rows]
-    int32_t* ticket;          // [B][pairs of a sequence], zero between launches
+    int2* fold;               // [B][pairs of a sequence] their parts and where these lie (written)
     int32_t B, N, cap, Hq, Hkv, pool_rows;
     int32_t grid;             // workgroups the work is dealt to
     int32_t row_blocks;       // blocks of query rows of a (sequence, KV head) (set for the launch)

@@ -213,8 +213,8 @@ struct asrkf_ctx {
     int draft_grid[4] = {0, 0, 0, 0};   // attention workgroups resident at once, by 32, 64, 128, 256 rows
     int cus = 0;
     void* draft_space = nullptr;        // one allocation:
-    int32_t* draft_ticket = nullptr;    // [B][Hkv][2] (zero between launches)
-    int32_t* accept_ticket = nullptr;
+    int2* draft_fold = nullptr;         // [B][Hkv][2]
+    int32_t* accept_ticket = nullptr;   // zero between launches, as the next
     int32_t* verify_ticket = nullptr;   // [B]
     VerifyPart* verify_part = nullptr;  // [B][nodes + 1][kVerifySplitMax]
     VerifyEnd* verify_end = nullptr;    // [B]
@@ -1482,7 +1482,7 @@ asrkf_status asrkf_reserve_drafts(asrkf_ctx* ctx, int32_t max_nodes) {
     }
     const size_t B = (size_t)c.batch;
     void* parts[9] = {};
-    const size_t bytes[9] = {B * c.n_kv_heads * 2 * 4, 4, B * 4, B * (max_nodes + 1) * kVerifySplitMax * sizeof(VerifyPart),
+    const size_t bytes[9] = {B * c.n_kv_heads * 2 * sizeof(int2), 4, B * 4, B * (max_nodes + 1) * kVerifySplitMax * sizeof(VerifyPart),
                              B * sizeof(VerifyEnd), B * kVerifySplitMax * 8, acc, ml, B * max_nodes * sizeof(float2)};
     size_t total = 0;
     for (size_t x : bytes) total += (x + 255) / 256 * 256;
@@ -1507,7 +1507,7 @@ asrkf_status asrkf_reserve_drafts(asrkf_ctx* ctx, int32_t max_nodes) {
     }
     if (ctx->draft_space) (void)hipFree(ctx->draft_space);
     ctx->draft_space = space;
-    ctx->draft_ticket = static_cast<int32_t*>(parts[0]);
+    ctx->draft_fold = static_cast<int2*>(parts[0]);
     ctx->accept_ticket = static_cast<int32_t*>(parts[1]);
     ctx->verify_ticket = static_cast<int32_t*>(parts[2]);
     ctx->verify_part = static_cast<VerifyPart*>(parts[3]);
@@ -1612,7 +1612,7 @@ asrkf_status asrkf_attend_drafts(asrkf_ctx* ctx, int32_t layer, int32_t n_nodes,
     a.list_tail = ctx->next_layer > layer ? 0 : 1;     // the step's own token, once it is in the cache
     a.part_acc = ctx->draft_acc;
     a.part_ml = ctx->draft_ml;
-    a.ticket = ctx->draft_ticket;
+    a.fold = ctx->draft_fold;
     a.B = c.batch;
     a.N = n_nodes;
     a.cap = ctx->cap;
