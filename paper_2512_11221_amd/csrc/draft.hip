@@ -32,16 +32,20 @@ constexpr int kStreamPolicy = 2;              // non-temporal: rows that one wor
 constexpr int kNowhere = (int)0x80000000;     // past every buffer's range: reads as zeros
 // What a piece costs a workgroup beside its rows, in tiles.
 constexpr int kDraftPieceCost = 2;
+// Tiles of a part at least; up to which half of the workgroups do; and parts of a pair at most.
+constexpr int kDraftLeast = 2, kDraftShort = 8, kDraftParts = 16;
 // As for prompts: the rescaling of O waits until a row's maximum has grown by 2^kLazy.
 constexpr float kLazy = 8.f;
 
 __device__ __forceinline__ int wave_uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
-template <int ROWS, int D, int RW, int KW>
+// A workgroup's waves: RW take 32 query rows each, KW a share of a tile's keys, DW a share of the
+// outputs' dims (rows of 256 values: their sums would take half of the registers).
+template <int ROWS, int D, int RW, int KW, int DW>
 struct Tile {
     static constexpr bool kFour = ROWS == kRowsFour, kBF16 = ROWS != kRowsF32;
-    static constexpr bool kSplit = RW == 1;               // every wave has a tile of its own
-    static constexpr int kWaves = RW * KW, kThreads = kWaves * 64;
+    static constexpr bool kSplit = RW == 1 && DW == 1;    // every wave has a tile of its own
+    static constexpr int kWaves = RW * KW * DW, kThreads = kWaves * 64;
     static constexpr int kRows = 32 * RW;                 // query rows of a workgroup
     static constexpr int kElem = kBF16 ? 2 : 4;
     static constexpr int kRow = D * kElem;                // bytes of a row of one head, in LDS
@@ -49,13 +53,15 @@ struct Tile {
     static constexpr int kStep = KW * kKeys;              // ... of the workgroup's
     static constexpr int kTileKeys = kSplit ? kKeys : kStep;          // ... of a tile in LDS
     static constexpr int kKB = kKeys / 32;                // score blocks of 32 keys
+    static constexpr int kDims = D / DW, kDB = kDims / 32;            // of a wave's sums
     static constexpr int kLoaders = kSplit ? 64 : kThreads;
     // LDS row strides: 16 rows of a 16-byte piece (K), and 4 rows of 64 bytes (V, bf16) or
     // rows 4 apart of 128 bytes (V, fp32), meet no bank twice
     static constexpr int kKStride = kRow + 16;
     static constexpr int kVStride = kRow + (kBF16 ? 64 : 32);
     static constexpr int kKBuffer = kTileKeys * kKStride, kVBuffer = kTileKeys * kVStride;
-    static constexpr int kBuffers = kSplit ? 1 : 2;
+    // one buffer where two of them would leave a compute unit one workgroup of four waves
+    static constexpr int kBuffers = kSplit || (kWaves == 4 && 2 * (kKBuffer + kVBuffer) > 80 * 1024) ? 1 : 2;
     static constexpr int kTiles = kBuffers * (kKBuffer + kVBuffer);   // of the workgroup, or of a wave
     static constexpr int kLds = kTiles * (kSplit ? kWaves : 1);
     static constexpr int kPieces = kRow / 16;             // 16-byte pieces of a row in LDS
@@ -65,12 +71,16 @@ struct Tile {
     static constexpr int kPoolPieces = kPoolRow / 16;
     static constexpr int kPoolTotal = kTileKeys * kPoolPieces;
     static constexpr int kLoads = (kPoolTotal + kLoaders - 1) / kLoaders;
+    // Tiles of the list on their way in registers: a launch is bound by what is in flight, and a tile of 4-bit
+    // rows, or one that eight waves share, is small.
+    static constexpr int kStageRegs = kLoads * (kFour ? 10 : 8);
+    static constexpr int kStages = kStageRegs <= 10 ? 4 : kStageRegs <= 16 || DW == 4 ? 2 : 1;
     static constexpr int kQRegs = kBF16 ? D / 16 : D / 8; // 16-byte pieces of q per lane
     static constexpr int kState = D + 4;                  // floats of a row of a wave's state
-    static constexpr int kPerSimd = kRow <= 256 || kWaves == 8 ? 2 : 1;
+    static constexpr int kPerSimd = kRow <= 256 || kWaves == 8 || DW > 1 ? 2 : 1;
     static_assert(kNodeLoads * kLoaders == kTileKeys * kPieces, "whole pieces per thread");
     static_assert(kTileKeys <= 64, "a lane per key's list entry");
-    static_assert(kSplit || KW == 1 || RW * 64 * (D / 2 + 2) * 4 <= kLds, "the states of half the waves fit the tiles");
+    static_assert(kSplit || KW == 1 || RW * DW * 64 * (kDims / 2 + 2) * 4 <= kLds, "the states of half the waves fit the tiles");
     static_assert(!kSplit || 32 * kState * 4 <= kTiles, "a wave's state fits its tile");
 };
 
@@ -79,8 +89,31 @@ struct Tile {
 // tiles.
 struct Deal : Split {
     int tiles, units, off;          // of the lane's sequence (up to 64 sequences)
+    int n, nodes;                   // its list and its nodes
     const int32_t* lds;
     int B;
+
+    // As Split has it, with fewer tiles to a part: a tile costs a round trip to memory.  Half of the workgroups
+    // where that leaves short parts, all of them else.
+    __device__ __forceinline__ void choose(int total, int longest, int filled) {
+        const int average = (total * groups + limit - 1) / limit;
+        auto share_of = [&](int most) { return most > 0 ? (longest + most - 1) / most : 1 << 30; };      // most: parts to a pair
+        const int pairs = greater(1, filled * groups), half = share_of(limit / 2 / pairs);
+        const int all = share_of(limit / pairs);
+        share = greater(half <= kDraftShort ? half : all, (longest + kDraftParts - 1) / kDraftParts);
+        share = greater(share, kDraftLeast);
+        aligned = limit >= pairs && share <= greater(average + cost, kDraftShort);
+    }
+    __device__ __forceinline__ void ranges(int sum) {
+        if (aligned) {
+            live = sum;
+            return;
+        }
+        live = greater(1, lesser(limit, sum / (cost + 1)));
+        share = sum / live;
+        extra = sum - share * live;
+        if (sum == 0) live = 0;
+    }
 
     // the sequence that owns unit x
     __device__ __forceinline__ int find(int x) const {
@@ -113,10 +146,7 @@ __device__ __forceinline__ Deal make_deal(const DraftArgs& a, int32_t* lds) {
     p.B = a.B;
     p.lds = lds;
     const int lane = threadIdx.x & 63;
-    auto tiles = [&](int b) __attribute__((always_inline)) {
-        const int c = nodes_of(a, b), n = listed(a, b);
-        return c == 0 ? 0 : (n + STEP - 1) / STEP + (c + STEP - 1) / STEP;
-    };
+    auto tiles = [&](int n, int c) __attribute__((always_inline)) { return c == 0 ? 0 : (n + STEP - 1) / STEP + (c + STEP - 1) / STEP; };
     auto total_of = [&](int& sum, int& top, int& filled) __attribute__((always_inline)) {
         for (int o = 1; o < 64; o <<= 1) {
             sum += __shfl_xor(sum, o);
@@ -132,7 +162,9 @@ __device__ __forceinline__ Deal make_deal(const DraftArgs& a, int32_t* lds) {
         return x;
     };
     if (a.B <= 64) {
-        p.tiles = lane < a.B ? tiles(lane) : 0;
+        p.n = listed(a, min(lane, a.B - 1));
+        p.nodes = nodes_of(a, min(lane, a.B - 1));
+        p.tiles = lane < a.B ? tiles(p.n, p.nodes) : 0;
         int sum = p.tiles, top = p.tiles, filled = p.tiles > 0;
         total_of(sum, top, filled);
         p.choose(wave_uniform(sum), wave_uniform(top), wave_uniform(filled));
@@ -147,7 +179,7 @@ __device__ __forceinline__ Deal make_deal(const DraftArgs& a, int32_t* lds) {
         const int per = (a.B + 63) / 64, b0 = min(a.B, lane * per), b1 = min(a.B, b0 + per);
         int sum = 0, top = 0, filled = 0;
         for (int b = b0; b < b1; ++b) {
-            const int t = tiles(b);
+            const int t = tiles(listed(a, b), nodes_of(a, b));
             lds[a.B + 1 + b] = t;
             sum += t;
             top = max(top, t);
@@ -201,12 +233,12 @@ __device__ __forceinline__ void write_row(const DraftArgs& a, int b, int kvh, in
     }
 }
 
-template <int ROWS, int D, int RW, int KW>
-__global__ void __launch_bounds__((Tile<ROWS, D, RW, KW>::kThreads), (Tile<ROWS, D, RW, KW>::kPerSimd))
+template <int ROWS, int D, int RW, int KW, int DW>
+__global__ void __launch_bounds__((Tile<ROWS, D, RW, KW, DW>::kThreads), (Tile<ROWS, D, RW, KW, DW>::kPerSimd))
 draft_kernel(DraftArgs a) {
-    using T = Tile<ROWS, D, RW, KW>;
+    using T = Tile<ROWS, D, RW, KW, DW>;
     constexpr bool BF16 = T::kBF16, FOUR = T::kFour;
-    constexpr int KB = T::kKB, NQ = T::kQRegs, NL = T::kLoads, DB = D / 32;
+    constexpr int KB = T::kKB, NQ = T::kQRegs, NL = T::kLoads, DB = T::kDB;
     __shared__ __align__(16) char lds[T::kLds];
     __shared__ float ml_lds[T::kSplit ? T::kWaves * 2 * 32 : 1];
     __shared__ int infinite_lds;
@@ -216,7 +248,8 @@ draft_kernel(DraftArgs a) {
     const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
     const int loader = T::kSplit ? lane : threadIdx.x;    // among those that load a tile
     const int row_wave = wave % RW;
-    const int key0 = T::kSplit ? 0 : wave / RW * T::kKeys;        // the wave's keys within a tile in LDS
+    const int key0 = T::kSplit ? 0 : wave / RW % KW * T::kKeys;   // the wave's keys within a tile in LDS
+    const int dim0 = wave / (RW * KW) % DW * T::kDims;            // ... dims of the outputs
     char* tiles_lds = T::kSplit ? lds + wave * T::kTiles : lds;
     const int G = a.Hq / a.Hkv, group_shift = __ffs(G) - 1;
 
@@ -233,7 +266,8 @@ draft_kernel(DraftArgs a) {
         const int t0 = wave_uniform(pc.t0), t1 = wave_uniform(pc.t1);
         const int n_parts = wave_uniform(pc.n_parts), part = wave_uniform(pc.part);
         const int kvh = gi / a.row_blocks, r0 = gi % a.row_blocks * T::kRows;
-        const int n = wave_uniform(listed(a, b)), nodes = wave_uniform(nodes_of(a, b));
+        const int n = a.B <= 64 ? __builtin_amdgcn_readlane(deal.n, b) : wave_uniform(listed(a, b));
+        const int nodes = a.B <= 64 ? __builtin_amdgcn_readlane(deal.nodes, b) : wave_uniform(nodes_of(a, b));
         const int live_rows = (nodes << group_shift) - r0;        // of the block, at least
         if (live_rows <= 0) continue;             // (every workgroup of the pair does)
         const int node_tiles = (nodes + T::kStep - 1) / T::kStep;
@@ -252,42 +286,35 @@ draft_kernel(DraftArgs a) {
         const bool idle = row_wave * 32 >= live_rows;     // no row of the wave is written
         const int row = wr0 + col;                        // the lane's query row
         const int node = min(row >> group_shift, nodes - 1);      // rows past the end repeat the last node's
-        intx4 q[NQ];
-        {
-            const char* p = a.q + ((size_t)b * a.N + node) * a.q_stride + (kvh * G + (row & (G - 1))) * T::kRow;
-#pragma unroll
-            for (int i = 0; i < NQ; ++i)
-                q[i] = *reinterpret_cast<const intx4*>(p + (BF16 ? i * 32 + half * 16 : half * (T::kRow / 2) + i * 16));
-        }
-        const uint64_t sees = a.sees[(size_t)b * a.N + node] & (nodes >= 64 ? ~0ull : (1ull << nodes) - 1ull);
-
         // ---- the list's tiles: an entry per lane, then the rows ----
-        int entry = 0;
-        intx4 kx[NL], vx[NL];
-        uint32_t ks[FOUR ? NL : 1], vs[FOUR ? NL : 1];
+        constexpr int kStages = T::kStages;
+        intx4 kx[kStages][NL], vx[kStages][NL];
+        uint32_t ks[kStages][FOUR ? NL : 1], vs[kStages][FOUR ? NL : 1];
         // tile j of the wave (split) or of the workgroup
-        auto request_entries = [&](int j) __attribute__((always_inline)) {
+        auto entries = [&](int j) __attribute__((always_inline)) {
             const int at = j * T::kTileKeys + (lane & (T::kTileKeys - 1));
-            entry = __builtin_amdgcn_raw_buffer_load_b32(rl, at < n ? at * 4 : kNowhere, 0, 0);
-            entry = at < n ? entry : -1;
+            const int p = __builtin_amdgcn_raw_buffer_load_b32(rl, at < n ? at * 4 : kNowhere, 0, 0);
+            return at < n ? p : -1;
         };
-        auto request = [&]() __attribute__((always_inline)) {
+        auto request = [&](auto STAGE, int entry) __attribute__((always_inline)) {
+            constexpr int g = decltype(STAGE)::value;
 #pragma unroll
             for (int u = 0; u < NL; ++u) {
                 const int i = loader + u * T::kLoaders;
                 const int p = __shfl(entry, i / T::kPoolPieces & (T::kTileKeys - 1));
                 const bool in = p >= 0 && (T::kPoolTotal % T::kLoaders == 0 || i < T::kPoolTotal);
                 const int off = in ? p * T::kPoolRow + i % T::kPoolPieces * 16 : kNowhere;
-                kx[u] = __builtin_bit_cast(intx4, __builtin_amdgcn_raw_buffer_load_b128(rk, off, 0, kStreamPolicy));
-                vx[u] = __builtin_bit_cast(intx4, __builtin_amdgcn_raw_buffer_load_b128(rv, off, 0, kStreamPolicy));
+                kx[g][u] = __builtin_bit_cast(intx4, __builtin_amdgcn_raw_buffer_load_b128(rk, off, 0, kStreamPolicy));
+                vx[g][u] = __builtin_bit_cast(intx4, __builtin_amdgcn_raw_buffer_load_b128(rv, off, 0, kStreamPolicy));
                 if constexpr (FOUR) {
                     const int so = in ? p * (D / kScaleGroup) + i % T::kPoolPieces : kNowhere;
-                    ks[u] = __builtin_amdgcn_raw_buffer_load_b8(rks, so, 0, 0);
-                    vs[u] = __builtin_amdgcn_raw_buffer_load_b8(rvs, so, 0, 0);
+                    ks[g][u] = __builtin_amdgcn_raw_buffer_load_b8(rks, so, 0, 0);
+                    vs[g][u] = __builtin_amdgcn_raw_buffer_load_b8(rvs, so, 0, 0);
                 }
             }
         };
-        auto keep = [&](int buf) __attribute__((always_inline)) {
+        auto keep = [&](auto STAGE, int buf) __attribute__((always_inline)) {
+            constexpr int g = decltype(STAGE)::value;
             char* kt = tiles_lds + buf * T::kKBuffer;
             char* vt = tiles_lds + T::kBuffers * T::kKBuffer + buf * T::kVBuffer;
 #pragma unroll
@@ -296,23 +323,24 @@ draft_kernel(DraftArgs a) {
                 if (T::kPoolTotal % T::kLoaders != 0 && i >= T::kPoolTotal) continue;
                 const int key = i / T::kPoolPieces, piece = i % T::kPoolPieces;
                 if constexpr (FOUR) {
-                    const float kf = scale_value(ks[u]), vf = scale_value(vs[u]);
+                    const float kf = scale_value(ks[g][u]), vf = scale_value(vs[g][u]);
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
-                        const uint32_t kc = (uint32_t)kx[u][c], vc = (uint32_t)vx[u][c];
+                        const uint32_t kc = (uint32_t)kx[g][u][c], vc = (uint32_t)vx[g][u][c];
                         *reinterpret_cast<uintx4*>(kt + key * T::kKStride + piece * 64 + c * 16) =
                             uintx4{decode2<0>(kc, kf), decode2<1>(kc, kf), decode2<2>(kc, kf), decode2<3>(kc, kf)};
                         *reinterpret_cast<uintx4*>(vt + key * T::kVStride + piece * 64 + c * 16) =
                             uintx4{decode2<0>(vc, vf), decode2<1>(vc, vf), decode2<2>(vc, vf), decode2<3>(vc, vf)};
                     }
                 } else {
-                    *reinterpret_cast<intx4*>(kt + key * T::kKStride + piece * 16) = kx[u];
-                    *reinterpret_cast<intx4*>(vt + key * T::kVStride + piece * 16) = vx[u];
+                    *reinterpret_cast<intx4*>(kt + key * T::kKStride + piece * 16) = kx[g][u];
+                    *reinterpret_cast<intx4*>(vt + key * T::kVStride + piece * 16) = vx[g][u];
                 }
             }
         };
-        // nodes from .. of a tile into LDS, zeros past the last; whether some value of V was not
-        // finite (it is left out there: a weight of zero must not meet it)
+        // Nodes from .. of a tile into LDS, zeros past the last; whether some value of V was not finite (it is
+        // left out there: a weight of zero must not meet it).  Asked for behind the list's rows, they arrive
+        // with them; asked for before, their registers were spilled.
         auto keep_nodes = [&](int from) __attribute__((always_inline)) {
             bool bad = false;
 #pragma unroll 4
@@ -330,6 +358,28 @@ draft_kernel(DraftArgs a) {
             return bad;
         };
 
+        // List tiles [l0, l1) of the workgroup's steps; those of nodes come first.  Loads come back in the order
+        // in which they were asked for: a tile's entries are asked for before the rows of the tile before it, or
+        // waiting for them would wait for those rows.
+        const int l0 = max(t0, node_tiles) - node_tiles, l1 = t1 - node_tiles;
+        const auto tile_of = [&](int j) __attribute__((always_inline)) { return T::kSplit ? j * KW + wave : j; };
+        int soon, later;                                  // entries of the next tile to ask for, and of the one behind it
+        int first[kStages];
+#pragma unroll
+        for (int g = 0; g < kStages; ++g) first[g] = entries(tile_of(l0 + g));
+        soon = entries(tile_of(l0 + kStages));
+        later = entries(tile_of(l0 + kStages + 1));
+        intx4 q[NQ];
+        {
+            const char* p = a.q + ((size_t)b * a.N + node) * a.q_stride + (kvh * G + (row & (G - 1))) * T::kRow;
+#pragma unroll
+            for (int i = 0; i < NQ; ++i)
+                q[i] = *reinterpret_cast<const intx4*>(p + (BF16 ? i * 32 + half * 16 : half * (T::kRow / 2) + i * 16));
+        }
+        const uint64_t sees = a.sees[(size_t)b * a.N + node] & (nodes >= 64 ? ~0ull : (1ull << nodes) - 1ull);
+
+        unroll<kStages>([&](auto STAGE) __attribute__((always_inline)) { request(STAGE, first[decltype(STAGE)::value]); });
+
         float m = -INFINITY, l = 0.f;                     // of the lane's row (l: the lane's own keys)
         floatx16 acc[DB];
 #pragma unroll
@@ -340,7 +390,7 @@ draft_kernel(DraftArgs a) {
         // the wave's tile in buffer buf; visible: bit j where the lane's row sees key j
         auto tile = [&](int buf, bool masked, uint64_t visible) __attribute__((always_inline)) {
             const char* kt = tiles_lds + buf * T::kKBuffer + key0 * T::kKStride;
-            const char* vt = tiles_lds + T::kBuffers * T::kKBuffer + buf * T::kVBuffer + key0 * T::kVStride;
+            const char* vt = tiles_lds + T::kBuffers * T::kKBuffer + buf * T::kVBuffer + key0 * T::kVStride + dim0 * T::kElem;
             floatx16 s[KB];
 #pragma unroll
             for (int i = 0; i < NQ; ++i)
@@ -360,6 +410,7 @@ draft_kernel(DraftArgs a) {
                             s[kb] = __builtin_amdgcn_mfma_f32_32x32x2f32(__int_as_float(kr[e]), __int_as_float(q[i][e]), s[kb], 0, 0, 0);
                     }
                 }
+            __builtin_amdgcn_sched_barrier(0);
             // key of value i in block kb: 32 kb + 8 (i / 4) + 4 half + i % 4
             if (masked) {
                 const uint64_t mine = visible >> (half * 4);
@@ -439,7 +490,7 @@ draft_kernel(DraftArgs a) {
             if (infinite) {
                 // values that are not finite, from memory, to the rows that see their node
                 for (int key = from; key < min(nodes, from + T::kKeys); ++key) {
-                    const char* at = vn + (size_t)key * a.v_stride + half * 4 * T::kElem;
+                    const char* at = vn + (size_t)key * a.v_stride + (dim0 + half * 4) * T::kElem;
 #pragma unroll
                     for (int d = 0; d < DB; ++d)
 #pragma unroll
@@ -454,31 +505,21 @@ draft_kernel(DraftArgs a) {
             }
         };
 
-        // list tiles [l0, l1) of the workgroup's steps; those of nodes come first
-        const int l0 = max(t0, node_tiles) - node_tiles, l1 = t1 - node_tiles;
-        if constexpr (T::kSplit) {
-            request_entries(l0 * KW + wave);
-            request();
-            request_entries((l0 + 1) * KW + wave);
-            for (int j = t0; j < min(t1, node_tiles); ++j) {
+        // tile j out of its stage into LDS, and tile j + kStages on its way
+        auto turn = [&](auto STAGE, int j, int buf) __attribute__((always_inline)) {
+            keep(STAGE, buf);
+            const int entry = soon;
+            soon = later;
+            later = entries(tile_of(j + kStages + 2));
+            request(STAGE, entry);
+        };
+        for (int j = t0; j < min(t1, node_tiles); ++j) {
+            if constexpr (T::kSplit) {
                 const bool infinite = __any(keep_nodes(j * T::kStep + wave * T::kKeys));
                 __builtin_amdgcn_wave_barrier();
                 node_tile(j * T::kStep + wave * T::kKeys, infinite);
                 __builtin_amdgcn_wave_barrier();
-            }
-            for (int j = l0; j < l1; ++j) {
-                keep(0);
-                __builtin_amdgcn_wave_barrier();
-                request();
-                request_entries((j + 2) * KW + wave);
-                list_tile(0, (j * KW + wave) * T::kKeys);
-                __builtin_amdgcn_wave_barrier();
-            }
-        } else {
-            request_entries(l0);
-            request();
-            request_entries(l0 + 1);
-            for (int j = t0; j < min(t1, node_tiles); ++j) {
+            } else {
                 if (threadIdx.x == 0) infinite_lds = 0;
                 __syncthreads();
                 if (keep_nodes(j * T::kStep)) infinite_lds = 1;
@@ -486,20 +527,38 @@ draft_kernel(DraftArgs a) {
                 node_tile(j * T::kStep + key0, infinite_lds != 0);
                 __syncthreads();
             }
-            if (l0 < l1) {
-                keep(l0 & 1);
-                request();
-                request_entries(l0 + 2);
-            }
-            for (int j = l0; j < l1; ++j) {
-                __syncthreads();                          // tile j is in place, tile j - 1 has been read
-                if (j + 1 < l1) {
-                    keep((j + 1) & 1);
-                    request();
-                    request_entries(j + 3);
-                }
-                list_tile(j & 1, j * T::kStep + key0);
-            }
+        }
+        if constexpr (T::kSplit) {
+            for (int j0 = l0; j0 < l1; j0 += kStages)
+                unroll<kStages>([&](auto STAGE) __attribute__((always_inline)) {
+                    const int j = j0 + decltype(STAGE)::value;
+                    if (j >= l1) return;
+                    turn(STAGE, j, 0);
+                    __builtin_amdgcn_wave_barrier();
+                    list_tile(0, tile_of(j) * T::kKeys);
+                    __builtin_amdgcn_wave_barrier();
+                });
+        } else if constexpr (T::kBuffers == 1) {
+            for (int j0 = l0; j0 < l1; j0 += kStages)
+                unroll<kStages>([&](auto STAGE) __attribute__((always_inline)) {
+                    const int j = j0 + decltype(STAGE)::value;
+                    if (j >= l1) return;
+                    turn(STAGE, j, 0);
+                    __syncthreads();
+                    list_tile(0, j * T::kStep + key0);
+                    __syncthreads();
+                });
+        } else {
+            if (l0 < l1) turn(std::integral_constant<int, 0>{}, l0, 0);
+            for (int j0 = l0; j0 < l1; j0 += kStages)
+                unroll<kStages>([&](auto STAGE) __attribute__((always_inline)) {
+                    constexpr int g = decltype(STAGE)::value;
+                    const int j = j0 + g, buf = kStages % 2 == 0 ? g & 1 : (j - l0) & 1;
+                    if (j >= l1) return;
+                    __syncthreads();                      // tile j is in place, tile j - 1 has been read
+                    if (j + 1 < l1) turn(std::integral_constant<int, (g + 1) % kStages>{}, j + 1, buf ^ 1);
+                    list_tile(buf, j * T::kStep + key0);
+                });
         }
 
         // ---- the waves' states together, and the outputs or the partial ----
@@ -558,20 +617,21 @@ draft_kernel(DraftArgs a) {
         } else {
             if constexpr (KW == 2) {
                 // the second halves' states, value by value in the same lanes
-                float* state = reinterpret_cast<float*>(lds) + row_wave * 64 * (D / 2 + 2) + lane;
+                constexpr int kSums = T::kDims / 2;       // a lane's
+                float* state = reinterpret_cast<float*>(lds) + (row_wave + RW * (dim0 / T::kDims)) * 64 * (kSums + 2) + lane;
                 if (key0) {
 #pragma unroll
                     for (int d = 0; d < DB; ++d)
 #pragma unroll
                         for (int i = 0; i < 16; ++i) state[(d * 16 + i) * 64] = acc[d][i];
-                    state[D / 2 * 64] = m;
-                    state[(D / 2 + 1) * 64] = l;
+                    state[kSums * 64] = m;
+                    state[(kSums + 1) * 64] = l;
                 }
                 __syncthreads();
                 if (!key0) {
-                    const float m2 = state[D / 2 * 64], M = fmaxf(m, m2);
+                    const float m2 = state[kSums * 64], M = fmaxf(m, m2);
                     const float f = weight(m, M, a.scale_log2), f2 = weight(m2, M, a.scale_log2);
-                    l = l * f + state[(D / 2 + 1) * 64] * f2;
+                    l = l * f + state[(kSums + 1) * 64] * f2;
                     m = M;
 #pragma unroll
                     for (int d = 0; d < DB; ++d)
@@ -584,7 +644,7 @@ draft_kernel(DraftArgs a) {
                 for (int d = 0; d < DB; ++d)
 #pragma unroll
                     for (int i = 0; i < 4; ++i)           // dims 32 d + 8 i + 4 half ..
-                        finish(row_wave * 32 + col, d * 8 + i * 2 + half,
+                        finish(row_wave * 32 + col, dim0 / 4 + d * 8 + i * 2 + half,
                                floatx4{acc[d][i * 4], acc[d][i * 4 + 1], acc[d][i * 4 + 2], acc[d][i * 4 + 3]}, m, l);
             }
         }
@@ -648,10 +708,10 @@ struct DraftLaunch {
     int* occupancy;                 // non-null: report it instead
 };
 
-template <int ROWS, int D, int RW, int KW>
+template <int ROWS, int D, int RW, int KW, int DW>
 hipError_t launch_walk(const DraftArgs& args, const DraftLaunch& l) {
-    using T = Tile<ROWS, D, RW, KW>;
-    auto kernel = draft_kernel<ROWS, D, RW, KW>;
+    using T = Tile<ROWS, D, RW, KW, DW>;
+    auto kernel = draft_kernel<ROWS, D, RW, KW, DW>;
     if (l.occupancy) return hipOccupancyMaxActiveBlocksPerMultiprocessor(l.occupancy, kernel, T::kThreads, 0);
     DraftArgs a = args;
     a.row_blocks = (a.N * (a.Hq / a.Hkv) + T::kRows - 1) / T::kRows;
@@ -667,11 +727,19 @@ hipError_t launch_walk(const DraftArgs& args, const DraftLaunch& l) {
 
 template <int ROWS, int D>
 hipError_t launch_rows(const DraftArgs& a, int rows, const DraftLaunch& l) {
-    switch (rows) {
-        case 32: return launch_walk<ROWS, D, 1, 4>(a, l);
-        case 64: return launch_walk<ROWS, D, 2, 2>(a, l);
-        case 128: return launch_walk<ROWS, D, 4, 1>(a, l);
-        case 256: return launch_walk<ROWS, D, 8, 1>(a, l);
+    if constexpr (D == 256) {
+        switch (rows) {
+            case 32: return launch_walk<ROWS, D, 1, 2, 4>(a, l);
+            case 64: return launch_walk<ROWS, D, 2, 1, 2>(a, l);
+            case 128: return launch_walk<ROWS, D, 4, 1, 2>(a, l);
+        }
+    } else {
+        switch (rows) {
+            case 32: return launch_walk<ROWS, D, 1, 4, 1>(a, l);
+            case 64: return launch_walk<ROWS, D, 2, 2, 1>(a, l);
+            case 128: return launch_walk<ROWS, D, 4, 1, 1>(a, l);
+            case 256: return launch_walk<ROWS, D, 8, 1, 1>(a, l);
+        }
     }
     return hipErrorInvalidValue;
 }
@@ -772,9 +840,9 @@ accept_kernel(AcceptArgs a) {
 
 }  // namespace
 
-int draft_rows(int n, int group) {
+int draft_rows(int n, int group, int head_dim) {
     const int rows = n * group;
-    return rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
+    return rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 || head_dim == 256 ? 128 : 256;
 }
 
 hipError_t draft_occupancy(int rows_kind, int head_dim, int rows, int* blocks_per_cu) {
@@ -785,7 +853,7 @@ hipError_t launch_drafts(const DraftArgs& args, int rows_kind, int head_dim, int
     DraftArgs a = args;
     a.scale_log2 = (float)(1.4426950408889634 / __builtin_sqrt((double)head_dim));
     a.lazy = kLazy / a.scale_log2;
-    return dispatch(a, rows_kind, head_dim, draft_rows(a.N, a.Hq / a.Hkv), DraftLaunch{blocks, s, nullptr});
+    return dispatch(a, rows_kind, head_dim, draft_rows(a.N, a.Hq / a.Hkv, head_dim), DraftLaunch{blocks, s, nullptr});
 }
 
 hipError_t launch_accept(const AcceptArgs& a, hipStream_t s) {

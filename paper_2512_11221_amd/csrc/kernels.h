@@ -400,7 +400,9 @@ hipError_t launch_get_rows(const RowsArgs& a, bool four, hipStream_t s);
 hipError_t launch_rotate(const RotateArgs& a, int bf16, hipStream_t s);
 // Query rows of a workgroup that attends drafts of n nodes, and workgroups of that kind
 // that a CU holds.
-int draft_rows(int n, int group);
+int draft_rows(int n, int group, int head_dim);
+// Blocks of those rows, at most.
+constexpr int kDraftBlocks = kMaxDrafts * 8 / 128;
 hipError_t draft_occupancy(int rows_kind, int head_dim, int rows, int* blocks_per_cu);
 hipError_t launch_drafts(const DraftArgs& a, int rows_kind, int head_dim, int blocks, hipStream_t s);
 hipError_t launch_accept(const AcceptArgs& a, hipStream_t s);

@@ -213,7 +213,7 @@ struct asrkf_ctx {
     int draft_grid[4] = {0, 0, 0, 0};   // attention workgroups resident at once, by 32, 64, 128, 256 rows
     int cus = 0;
     void* draft_space = nullptr;        // one allocation:
-    int2* draft_fold = nullptr;         // [B][Hkv][2]
+    int2* draft_fold = nullptr;         // [B][Hkv][kDraftBlocks]
     int32_t* accept_ticket = nullptr;   // zero between launches, as the next
     int32_t* verify_ticket = nullptr;   // [B]
     VerifyPart* verify_part = nullptr;  // [B][nodes + 1][kVerifySplitMax]
@@ -1472,7 +1472,7 @@ asrkf_status asrkf_reserve_drafts(asrkf_ctx* ctx, int32_t max_nodes) {
     // partials: two slots of every attention workgroup, by the kind of workgroup
     size_t acc = 0, ml = 0;
     for (int i = 0, rows = 32; i < 4; ++i, rows *= 2) {
-        if (rows > draft_rows(max_nodes, ctx->group)) break;
+        if (rows > draft_rows(max_nodes, ctx->group, c.head_dim)) break;
         int per_cu = 0;
         HIP_OK(ctx, draft_occupancy(row_kind(ctx), c.head_dim, rows, &per_cu));
         if (per_cu < 1) return fail(ASRKF_EINVAL, "draft attention workgroup does not fit on a CU for this shape");
@@ -1482,7 +1482,7 @@ asrkf_status asrkf_reserve_drafts(asrkf_ctx* ctx, int32_t max_nodes) {
     }
     const size_t B = (size_t)c.batch;
     void* parts[9] = {};
-    const size_t bytes[9] = {B * c.n_kv_heads * 2 * sizeof(int2), 4, B * 4, B * (max_nodes + 1) * kVerifySplitMax * sizeof(VerifyPart),
+    const size_t bytes[9] = {B * c.n_kv_heads * kDraftBlocks * sizeof(int2), 4, B * 4, B * (max_nodes + 1) * kVerifySplitMax * sizeof(VerifyPart),
                              B * sizeof(VerifyEnd), B * kVerifySplitMax * 8, acc, ml, B * max_nodes * sizeof(float2)};
     size_t total = 0;
     for (size_t x : bytes) total += (x + 255) / 256 * 256;
@@ -1619,7 +1619,7 @@ asrkf_status asrkf_attend_drafts(asrkf_ctx* ctx, int32_t layer, int32_t n_nodes,
     a.Hq = c.n_q_heads;
     a.Hkv = c.n_kv_heads;
     a.pool_rows = ctx->pool_rows;
-    const int rows = draft_rows(n_nodes, ctx->group);
+    const int rows = draft_rows(n_nodes, ctx->group, c.head_dim);
     a.grid = ctx->draft_grid[rows == 32 ? 0 : rows == 64 ? 1 : rows == 128 ? 2 : 3];
     HIP_OK(ctx, launch_drafts(a, row_kind(ctx), c.head_dim, a.grid, s));
     return ASRKF_OK;
