@@ -33,6 +33,7 @@ constexpr int kNowhere = (int)0x80000000;     // past every buffer's range: read
 // What a piece costs a workgroup beside its rows, in tiles.
 constexpr int kDraftPieceCost = 2;
 // Tiles of a part at least; up to which half of the workgroups do; and parts of a pair at most.
+// (fp32 tiles, whose products take sixteen times as long, go one by one.)
 constexpr int kDraftLeast = 2, kDraftShort = 8, kDraftParts = 16;
 // As for prompts: the rescaling of O waits until a row's maximum has grown by 2^kLazy.
 constexpr float kLazy = 8.f;
@@ -90,6 +91,7 @@ struct Tile {
 struct Deal : Split {
     int tiles, units, off;          // of the lane's sequence (up to 64 sequences)
     int n, nodes;                   // its list and its nodes
+    int least;                      // tiles of a part
     const int32_t* lds;
     int B;
 
@@ -101,7 +103,7 @@ struct Deal : Split {
         const int pairs = greater(1, filled * groups), half = share_of(limit / 2 / pairs);
         const int all = share_of(limit / pairs);
         share = greater(half <= kDraftShort ? half : all, (longest + kDraftParts - 1) / kDraftParts);
-        share = greater(share, kDraftLeast);
+        share = greater(share, least);
         aligned = limit >= pairs && share <= greater(average + cost, kDraftShort);
     }
     __device__ __forceinline__ void ranges(int sum) {
@@ -138,28 +140,39 @@ __device__ __forceinline__ int nodes_of(const DraftArgs& a, int b) {
 }
 __device__ __forceinline__ int listed(const DraftArgs& a, int b) { return max(a.n_active[b] - a.list_tail, 0); }
 
-template <int STEP>
+// x of the lane that CTRL names, `old` where there is none (DPP)
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int moved_in(int old, int x) { return __builtin_amdgcn_update_dpp(old, x, CTRL, ROWS, 0xF, false); }
+
+template <int STEP, int LEAST>
 __device__ __forceinline__ Deal make_deal(const DraftArgs& a, int32_t* lds) {
     Deal p;
     p.init(1, a.Hkv * a.row_blocks, 1, a.grid);
     p.cost = kDraftPieceCost;
+    p.least = LEAST;
     p.B = a.B;
     p.lds = lds;
     const int lane = threadIdx.x & 63;
     auto tiles = [&](int n, int c) __attribute__((always_inline)) { return c == 0 ? 0 : (n + STEP - 1) / STEP + (c + STEP - 1) / STEP; };
-    auto total_of = [&](int& sum, int& top, int& filled) __attribute__((always_inline)) {
-        for (int o = 1; o < 64; o <<= 1) {
-            sum += __shfl_xor(sum, o);
-            top = max(top, __shfl_xor(top, o));
-            filled += __shfl_xor(filled, o);
-        }
-    };
     auto before = [&](int x) __attribute__((always_inline)) {     // inclusive sum over the lanes
-        for (int o = 1; o < 64; o <<= 1) {
-            const int y = __shfl_up(x, o);
-            if (lane >= o) x += y;
-        }
+        x += moved_in<0x111, 0xF>(0, x);                          // row_shr 1, 2, 4, 8
+        x += moved_in<0x112, 0xF>(0, x);
+        x += moved_in<0x114, 0xF>(0, x);
+        x += moved_in<0x118, 0xF>(0, x);
+        x += moved_in<0x142, 0xA>(0, x);                          // row_bcast 15 into rows 1 and 3
+        x += moved_in<0x143, 0xC>(0, x);                          // row_bcast 31 into rows 2 and 3
         return x;
+    };
+    auto total_of = [&](int& sum, int& top, int& filled) __attribute__((always_inline)) {
+        sum = __builtin_amdgcn_readlane(before(sum), 63);
+        filled = __builtin_amdgcn_readlane(before(filled), 63);
+        top = max(top, moved_in<0x111, 0xF>(top, top));
+        top = max(top, moved_in<0x112, 0xF>(top, top));
+        top = max(top, moved_in<0x114, 0xF>(top, top));
+        top = max(top, moved_in<0x118, 0xF>(top, top));
+        top = max(top, moved_in<0x142, 0xA>(top, top));
+        top = max(top, moved_in<0x143, 0xC>(top, top));
+        top = __builtin_amdgcn_readlane(top, 63);
     };
     if (a.B <= 64) {
         p.n = listed(a, min(lane, a.B - 1));
@@ -167,7 +180,7 @@ __device__ __forceinline__ Deal make_deal(const DraftArgs& a, int32_t* lds) {
         p.tiles = lane < a.B ? tiles(p.n, p.nodes) : 0;
         int sum = p.tiles, top = p.tiles, filled = p.tiles > 0;
         total_of(sum, top, filled);
-        p.choose(wave_uniform(sum), wave_uniform(top), wave_uniform(filled));
+        p.choose(sum, top, filled);
         p.units = p.units_of(p.tiles);
         const int incl = before(p.units);
         p.off = incl - p.units;
@@ -186,7 +199,7 @@ __device__ __forceinline__ Deal make_deal(const DraftArgs& a, int32_t* lds) {
             filled += t > 0;
         }
         total_of(sum, top, filled);
-        p.choose(wave_uniform(sum), wave_uniform(top), wave_uniform(filled));
+        p.choose(sum, top, filled);
         int mine = 0;
         for (int b = b0; b < b1; ++b) mine += p.units_of(lds[a.B + 1 + b]);
         const int incl = before(mine);
@@ -206,6 +219,12 @@ __device__ __forceinline__ Deal make_deal(const DraftArgs& a, int32_t* lds) {
     p.aligned = wave_uniform(summary[1]) != 0;
     p.ranges(wave_uniform(lds[a.B]));
     return p;
+}
+
+// x[from], x[from + 1], ... around, from 0 .. 3
+__device__ __forceinline__ intx4 quarters_from(intx4 x, int from) {
+    const intx4 y = from & 1 ? intx4{x[1], x[2], x[3], x[0]} : x;
+    return from & 2 ? intx4{y[2], y[3], y[0], y[1]} : y;
 }
 
 // The weight of a state whose reference is m, in one whose reference is M.
@@ -253,7 +272,7 @@ draft_kernel(DraftArgs a) {
     char* tiles_lds = T::kSplit ? lds + wave * T::kTiles : lds;
     const int G = a.Hq / a.Hkv, group_shift = __ffs(G) - 1;
 
-    const Deal deal = make_deal<T::kStep>(a, deal_lds);
+    const Deal deal = make_deal<T::kStep, BF16 ? kDraftLeast : 1>(a, deal_lds);
     for (int wi = blockIdx.x; wi < deal.live; wi += gridDim.x) {
     const int w = deal.range_of(wi);
     int x, x_end;
@@ -323,13 +342,18 @@ draft_kernel(DraftArgs a) {
                 if (T::kPoolTotal % T::kLoaders != 0 && i >= T::kPoolTotal) continue;
                 const int key = i / T::kPoolPieces, piece = i % T::kPoolPieces;
                 if constexpr (FOUR) {
+                    // neighbouring lanes stand 64 bytes apart: each writes its four quarters from another one on, so
+                    // that they meet no bank twice
                     const float kf = scale_value(ks[g][u]), vf = scale_value(vs[g][u]);
+                    const int turned = lane & 3;
+                    const intx4 kq = quarters_from(kx[g][u], turned), vq = quarters_from(vx[g][u], turned);
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
-                        const uint32_t kc = (uint32_t)kx[g][u][c], vc = (uint32_t)vx[g][u][c];
-                        *reinterpret_cast<uintx4*>(kt + key * T::kKStride + piece * 64 + c * 16) =
+                        const uint32_t kc = (uint32_t)kq[c], vc = (uint32_t)vq[c];
+                        const int at = piece * 64 + ((c + turned) & 3) * 16;
+                        *reinterpret_cast<uintx4*>(kt + key * T::kKStride + at) =
                             uintx4{decode2<0>(kc, kf), decode2<1>(kc, kf), decode2<2>(kc, kf), decode2<3>(kc, kf)};
-                        *reinterpret_cast<uintx4*>(vt + key * T::kVStride + piece * 64 + c * 16) =
+                        *reinterpret_cast<uintx4*>(vt + key * T::kVStride + at) =
                             uintx4{decode2<0>(vc, vf), decode2<1>(vc, vf), decode2<2>(vc, vf), decode2<3>(vc, vf)};
                     }
                 } else {
@@ -359,16 +383,16 @@ draft_kernel(DraftArgs a) {
         };
 
         // List tiles [l0, l1) of the workgroup's steps; those of nodes come first.  Loads come back in the order
-        // in which they were asked for: a tile's entries are asked for before the rows of the tile before it, or
-        // waiting for them would wait for those rows.
+        // in which they were asked for, so that waiting for a tile's entries means waiting for all rows asked
+        // for before them: they are asked for as many tiles earlier as rows are on their way.
         const int l0 = max(t0, node_tiles) - node_tiles, l1 = t1 - node_tiles;
         const auto tile_of = [&](int j) __attribute__((always_inline)) { return T::kSplit ? j * KW + wave : j; };
-        int soon, later;                                  // entries of the next tile to ask for, and of the one behind it
+        int ahead[kStages + 1];                           // entries of the next tiles to ask for
         int first[kStages];
 #pragma unroll
         for (int g = 0; g < kStages; ++g) first[g] = entries(tile_of(l0 + g));
-        soon = entries(tile_of(l0 + kStages));
-        later = entries(tile_of(l0 + kStages + 1));
+#pragma unroll
+        for (int g = 0; g <= kStages; ++g) ahead[g] = entries(tile_of(l0 + kStages + g));
         intx4 q[NQ];
         {
             const char* p = a.q + ((size_t)b * a.N + node) * a.q_stride + (kvh * G + (row & (G - 1))) * T::kRow;
@@ -508,9 +532,10 @@ draft_kernel(DraftArgs a) {
         // tile j out of its stage into LDS, and tile j + kStages on its way
         auto turn = [&](auto STAGE, int j, int buf) __attribute__((always_inline)) {
             keep(STAGE, buf);
-            const int entry = soon;
-            soon = later;
-            later = entries(tile_of(j + kStages + 2));
+            const int entry = ahead[0];
+#pragma unroll
+            for (int g = 0; g < kStages; ++g) ahead[g] = ahead[g + 1];
+            ahead[kStages] = entries(tile_of(j + 2 * kStages + 1));
             request(STAGE, entry);
         };
         for (int j = t0; j < min(t1, node_tiles); ++j) {
