@@ -326,7 +326,7 @@ asrkf_status asrkf_set_rotary(asrkf_ctx* ctx, const asrkf_rotary* r);
 
 /* Rows of queries and keys turned by their positions, for the calls that take
  * them: the library stores K and takes q as given.
- *   n_rows:       tokens, 0 .. 2^28
+ *   n_rows:       tokens, 0 .. 2^25
  *   rows_per_seq: 0: row i stands at position pos[i].  Else n_rows = batch *
  *                 rows_per_seq, and row i, of sequence i / rows_per_seq, stands
  *                 pos[i] positions behind the token that the present step

@@ -1350,7 +1350,7 @@ asrkf_status asrkf_rotate(asrkf_ctx* ctx, int32_t n_rows, int32_t rows_per_seq, 
     if (st != ASRKF_OK) return st;
     const asrkf_config& c = ctx->cfg;
     if (!ctx->rotary) return fail(ASRKF_ESTATE, "asrkf_set_rotary comes first");
-    if (n_rows < 0 || n_rows > (1 << 28)) return fail(ASRKF_EINVAL, "n_rows must be in 0..2^28");
+    if (n_rows < 0 || n_rows > kMaxRotateRows) return fail(ASRKF_EINVAL, "n_rows must be in 0..%d", kMaxRotateRows);
     if (rows_per_seq < 0 || (rows_per_seq > 0 && (int64_t)rows_per_seq * c.batch != n_rows))
         return fail(ASRKF_EINVAL, "n_rows must be rows_per_seq for every one of the %d sequences", c.batch);
     if (rows_per_seq == 0 && !pos && n_rows > 0) return fail(ASRKF_EINVAL, "null positions");

@@ -101,6 +101,24 @@ def test_in_place_on_slices_of_a_fused_projection(dtype, layout):
         A.asrkf_destroy(ctx)
 
 
+def test_the_most_rows():
+    """2^25 rows of 128 bytes: 4 GiB, turned in place."""
+    import torch
+    A, ctx = _init(2, 1, 1, 64)
+    try:
+        A.asrkf_set_rotary(ctx, 64)
+        freq = A.asrkf_rotary_table(64, 64)
+        n = 1 << 25
+        x = _rows(4096, 1, 64, "bf16").repeat(n // 4096, 1, 1)
+        some = torch.cat([torch.arange(i, i + 100) for i in (0, (1 << 24) - 50, n - 100)]).cuda()
+        before = x[some]
+        pos = torch.arange(n, device="cuda", dtype=torch.int32)
+        A.asrkf_rotate(ctx, pos, None, None, x, x)
+        R.check(x[some], *R.turned(before, some, freq, "halves"))
+    finally:
+        A.asrkf_destroy(ctx)
+
+
 def test_values_that_are_not_finite_stay_in_their_pair():
     import torch
     A, ctx = _init(2, 8, 2, 64, "f32")
@@ -243,7 +261,7 @@ def test_refusals():
             names = ["n", "per", "pos", "q", "qs", "qo", "qos", "k", "ks", "ko", "kos"]
             return [kw.get(n, v) for n, v in zip(names, good)]
         big = 1 << 30
-        for bad in (dict(n=-1), dict(n=(1 << 28) + 1), dict(per=-1), dict(per=3), dict(per=10), dict(pos=0), dict(q=0), dict(qo=0), dict(ko=0),
+        for bad in (dict(n=-1), dict(n=(1 << 25) + 1), dict(per=-1), dict(per=3), dict(per=10), dict(pos=0), dict(q=0), dict(qo=0), dict(ko=0),
                     dict(q=0, qo=0, k=0, ko=0), dict(qs=-512), dict(qs=8), dict(qs=514), dict(qos=big), dict(q=P(q) + 2), dict(ko=P(ko) + 8),
                     dict(pos=P(pos) + 2), dict(qo=P(q) + 1024), dict(ko=P(q)), dict(qo=P(k)), dict(ko=P(qo)), dict(qos=1024, qo=P(q)),
                     dict(n=1 << 20), dict(pos=P(qo)), dict(k=torch.zeros(4096).data_ptr())):
