@@ -503,7 +503,10 @@ verify_walk_kernel(VerifyArgs a) {
     }
     double left;
     const int sp = part_of_point(s, (double)u_last, left);
-    const int tok = sp < 0 ? -1 : w.find(sp * a.part_len, min(a.V, (sp + 1) * a.part_len), left);
+    // no weight is left only where W, a difference, was rounded upwards and the last token that had one was
+    // rejected for that: it is the next one
+    const int tok = sp < 0 ? __builtin_amdgcn_readlane(token, 63 - __builtin_clzll(weighed | 1))
+                           : w.find(sp * a.part_len, min(a.V, (sp + 1) * a.part_len), left);
     if (threadIdx.x == 0) a.next[b] = tok;
 }
 

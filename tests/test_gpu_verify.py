@@ -226,6 +226,28 @@ def test_the_ends_of_the_random_numbers(u):
         A.asrkf_destroy(ctx)
 
 
+def test_the_last_token_of_any_weight():
+    """Three tokens have all of the weight and the first two drafts of them are rejected: the third is kept, or, where
+    the rounded rest of 10^-7 says no, the next one."""
+    A, ctx = _init(1024, 20000, 3)
+    try:
+        for T in (0.7, 1.0, 1.9):
+            c = Case(1024, 3, 20000, False, int(T * 10), ragged=False)
+            c.parents[:] = -1
+            c.tokens[:] = [5000, 10, 15000]
+            c.root[:] = -np.inf
+            c.root[:, 5000] = c.rng.uniform(-9, 9, 1024)
+            c.root[:, 10] = c.root[:, 5000] + c.rng.uniform(-1, 1, 1024).astype(np.float32)
+            c.root[:, 15000] = c.root[:, 5000] + T * np.log(10.0 ** c.rng.uniform(-6.5, -5.5, 1024)).astype(np.float32)
+            c.u[:] = 1 - 2.0 ** -24
+            path, n, nxt = c.run(A, ctx, T)
+            kept = n == 1
+            assert kept.sum() + (n == 0).sum() == 1024
+            assert (path[kept, 0] == 2).all() and (nxt[kept] >= 0).all() and (nxt[~kept] == 15000).all()
+    finally:
+        A.asrkf_destroy(ctx)
+
+
 @pytest.mark.parametrize("probs", [False, True])
 def test_next_tokens_have_the_targets_distribution(probs):
     """The token behind the root, drafted or drawn, over 40 x 1024 sequences whose two siblings are drawn from q:
