@@ -46,6 +46,9 @@ template <int ROWS, int D, int RW, int KW, int DW>
 struct Tile {
     static constexpr bool kFour = ROWS == kRowsFour, kBF16 = ROWS != kRowsF32;
     static constexpr bool kSplit = RW == 1 && DW == 1;    // every wave has a tile of its own
+    // The list's K goes from memory into the matrix operands' registers, and not through LDS: 4-bit rows of which a lane
+    // takes half a row, that no other wave needs.
+    static constexpr bool kDirect = kFour && kSplit;
     static constexpr int kWaves = RW * KW * DW, kThreads = kWaves * 64;
     static constexpr int kRows = 32 * RW;                 // query rows of a workgroup
     static constexpr int kElem = kBF16 ? 2 : 4;
@@ -305,6 +308,11 @@ draft_kernel(DraftArgs a) {
         const bool idle = row_wave * 32 >= live_rows;     // no row of the wave is written
         const int row = wr0 + col;                        // the lane's query row
         const int node = min(row >> group_shift, nodes - 1);      // rows past the end repeat the last node's
+        // where the lane's i-th piece of K and q lies in a row: the two halves of a wave's lanes take eight dims each
+        // of a product of 16, or all of a half row's in turn
+        const auto piece_at = [&](int i) __attribute__((always_inline)) {
+            return BF16 && !T::kDirect ? i * 32 + half * 16 : half * (T::kRow / 2) + i * 16;
+        };
         // ---- the list's tiles: an entry per lane, then the rows ----
         constexpr int kStages = T::kStages;
         intx4 kx[kStages][NL], vx[kStages][NL];
@@ -323,11 +331,17 @@ draft_kernel(DraftArgs a) {
                 const int p = __shfl(entry, i / T::kPoolPieces & (T::kTileKeys - 1));
                 const bool in = p >= 0 && (T::kPoolTotal % T::kLoaders == 0 || i < T::kPoolTotal);
                 const int off = in ? p * T::kPoolRow + i % T::kPoolPieces * 16 : kNowhere;
-                kx[g][u] = __builtin_bit_cast(intx4, __builtin_amdgcn_raw_buffer_load_b128(rk, off, 0, kStreamPolicy));
+                const int so = in ? p * (D / kScaleGroup) + i % T::kPoolPieces : kNowhere;
+                int k_off = off, k_so = so;
+                if constexpr (T::kDirect) {               // the lane's key and half of its row
+                    const int kp = __shfl(entry, col), piece = half * NL + u;
+                    k_off = kp >= 0 ? kp * T::kPoolRow + piece * 16 : kNowhere;
+                    k_so = kp >= 0 ? kp * (D / kScaleGroup) + piece : kNowhere;
+                }
+                kx[g][u] = __builtin_bit_cast(intx4, __builtin_amdgcn_raw_buffer_load_b128(rk, k_off, 0, kStreamPolicy));
                 vx[g][u] = __builtin_bit_cast(intx4, __builtin_amdgcn_raw_buffer_load_b128(rv, off, 0, kStreamPolicy));
                 if constexpr (FOUR) {
-                    const int so = in ? p * (D / kScaleGroup) + i % T::kPoolPieces : kNowhere;
-                    ks[g][u] = __builtin_amdgcn_raw_buffer_load_b8(rks, so, 0, 0);
+                    ks[g][u] = __builtin_amdgcn_raw_buffer_load_b8(rks, k_so, 0, 0);
                     vs[g][u] = __builtin_amdgcn_raw_buffer_load_b8(rvs, so, 0, 0);
                 }
             }
@@ -351,8 +365,9 @@ draft_kernel(DraftArgs a) {
                     for (int c = 0; c < 4; ++c) {
                         const uint32_t kc = (uint32_t)kq[c], vc = (uint32_t)vq[c];
                         const int at = piece * 64 + ((c + turned) & 3) * 16;
-                        *reinterpret_cast<uintx4*>(kt + key * T::kKStride + at) =
-                            uintx4{decode2<0>(kc, kf), decode2<1>(kc, kf), decode2<2>(kc, kf), decode2<3>(kc, kf)};
+                        if constexpr (!T::kDirect)
+                            *reinterpret_cast<uintx4*>(kt + key * T::kKStride + at) =
+                                uintx4{decode2<0>(kc, kf), decode2<1>(kc, kf), decode2<2>(kc, kf), decode2<3>(kc, kf)};
                         *reinterpret_cast<uintx4*>(vt + key * T::kVStride + at) =
                             uintx4{decode2<0>(vc, vf), decode2<1>(vc, vf), decode2<2>(vc, vf), decode2<3>(vc, vf)};
                     }
@@ -397,8 +412,7 @@ draft_kernel(DraftArgs a) {
         {
             const char* p = a.q + ((size_t)b * a.N + node) * a.q_stride + (kvh * G + (row & (G - 1))) * T::kRow;
 #pragma unroll
-            for (int i = 0; i < NQ; ++i)
-                q[i] = *reinterpret_cast<const intx4*>(p + (BF16 ? i * 32 + half * 16 : half * (T::kRow / 2) + i * 16));
+            for (int i = 0; i < NQ; ++i) q[i] = *reinterpret_cast<const intx4*>(p + piece_at(i));
         }
         const uint64_t sees = a.sees[(size_t)b * a.N + node] & (nodes >= 64 ? ~0ull : (1ull << nodes) - 1ull);
 
@@ -411,17 +425,15 @@ draft_kernel(DraftArgs a) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[d][i] = 0.f;
 
-        // the wave's tile in buffer buf; visible: bit j where the lane's row sees key j
-        auto tile = [&](int buf, bool masked, uint64_t visible) __attribute__((always_inline)) {
-            const char* kt = tiles_lds + buf * T::kKBuffer + key0 * T::kKStride;
+        // the wave's tile in buffer buf; visible: bit j where the lane's row sees key j; piece_of: the i-th of K
+        auto tile = [&](int buf, bool masked, uint64_t visible, auto piece_of) __attribute__((always_inline)) {
             const char* vt = tiles_lds + T::kBuffers * T::kKBuffer + buf * T::kVBuffer + key0 * T::kVStride + dim0 * T::kElem;
             floatx16 s[KB];
 #pragma unroll
             for (int i = 0; i < NQ; ++i)
 #pragma unroll
                 for (int kb = 0; kb < KB; ++kb) {
-                    const intx4 kr = *reinterpret_cast<const intx4*>(
-                        kt + (kb * 32 + col) * T::kKStride + (BF16 ? i * 32 + half * 16 : half * (T::kRow / 2) + i * 16));
+                    const intx4 kr = piece_of(i, kb);
                     if (i == 0)
 #pragma unroll
                         for (int e = 0; e < 16; ++e) s[kb][e] = 0.f;
@@ -504,13 +516,19 @@ draft_kernel(DraftArgs a) {
                 }
             });
         };
-        auto list_tile = [&](int buf, int from) __attribute__((always_inline)) {
+        auto in_lds = [&](int buf) __attribute__((always_inline)) {
+            const char* kt = tiles_lds + buf * T::kKBuffer + (key0 + col) * T::kKStride;
+            return [=](int i, int kb) __attribute__((always_inline)) {
+                return *reinterpret_cast<const intx4*>(kt + kb * 32 * T::kKStride + piece_at(i));
+            };
+        };
+        auto list_tile = [&](int buf, int from, auto piece_of) __attribute__((always_inline)) {
             const int left = n - from;
-            if (left > 0 && !idle) tile(buf, left < T::kKeys, left >= 64 ? ~0ull : (1ull << left) - 1ull);
+            if (left > 0 && !idle) tile(buf, left < T::kKeys, left >= 64 ? ~0ull : (1ull << left) - 1ull, piece_of);
         };
         auto node_tile = [&](int from, bool infinite) __attribute__((always_inline)) {
             if (from >= nodes || idle) return;
-            tile(0, true, sees >> from);
+            tile(0, true, sees >> from, in_lds(0));
             if (infinite) {
                 // values that are not finite, from memory, to the rows that see their node
                 for (int key = from; key < min(nodes, from + T::kKeys); ++key) {
@@ -558,9 +576,27 @@ draft_kernel(DraftArgs a) {
                 unroll<kStages>([&](auto STAGE) __attribute__((always_inline)) {
                     const int j = j0 + decltype(STAGE)::value;
                     if (j >= l1) return;
-                    turn(STAGE, j, 0);
-                    __builtin_amdgcn_wave_barrier();
-                    list_tile(0, tile_of(j) * T::kKeys);
+                    if constexpr (T::kDirect) {
+                        constexpr int g = decltype(STAGE)::value;
+                        intx4 x[NL];
+                        float f[NL];
+#pragma unroll
+                        for (int u = 0; u < NL; ++u) {
+                            x[u] = kx[g][u];
+                            f[u] = scale_value(ks[g][u]);
+                        }
+                        turn(STAGE, j, 0);
+                        __builtin_amdgcn_wave_barrier();
+                        list_tile(0, tile_of(j) * T::kKeys, [&](int i, int) __attribute__((always_inline)) {
+                            const uint32_t c = (uint32_t)x[i / 4][i % 4];
+                            return __builtin_bit_cast(intx4, uintx4{decode2<0>(c, f[i / 4]), decode2<1>(c, f[i / 4]), decode2<2>(c, f[i / 4]),
+                                                                    decode2<3>(c, f[i / 4])});
+                        });
+                    } else {
+                        turn(STAGE, j, 0);
+                        __builtin_amdgcn_wave_barrier();
+                        list_tile(0, tile_of(j) * T::kKeys, in_lds(0));
+                    }
                     __builtin_amdgcn_wave_barrier();
                 });
         } else if constexpr (T::kBuffers == 1) {
@@ -570,7 +606,7 @@ draft_kernel(DraftArgs a) {
                     if (j >= l1) return;
                     turn(STAGE, j, 0);
                     __syncthreads();
-                    list_tile(0, j * T::kStep + key0);
+                    list_tile(0, j * T::kStep + key0, in_lds(0));
                     __syncthreads();
                 });
         } else {
@@ -582,7 +618,7 @@ draft_kernel(DraftArgs a) {
                     if (j >= l1) return;
                     __syncthreads();                      // tile j is in place, tile j - 1 has been read
                     if (j + 1 < l1) turn(std::integral_constant<int, (g + 1) % kStages>{}, j + 1, buf ^ 1);
-                    list_tile(buf, j * T::kStep + key0);
+                    list_tile(buf, j * T::kStep + key0, in_lds(buf));
                 });
         }
 
@@ -761,7 +797,9 @@ hipError_t launch_rows(const DraftArgs& a, int rows, const DraftLaunch& l) {
     } else {
         switch (rows) {
             case 32: return launch_walk<ROWS, D, 1, 4, 1>(a, l);
-            case 64: return launch_walk<ROWS, D, 2, 2, 1>(a, l);
+            case 64:
+                if constexpr (ROWS != kRowsFour) return launch_walk<ROWS, D, 2, 2, 1>(a, l);
+                break;
             case 128: return launch_walk<ROWS, D, 4, 1, 1>(a, l);
             case 256: return launch_walk<ROWS, D, 8, 1, 1>(a, l);
         }
@@ -865,9 +903,15 @@ accept_kernel(AcceptArgs a) {
 
 }  // namespace
 
-int draft_rows(int n, int group, int head_dim) {
+// Rows of a pair by the least workgroup that has room for all of them, so that the list is read once; but twice 32 for 64
+// rows over a cache in 4 bits, which waits for its products and not for memory, and needs no barrier there (64 rows, 8 KV
+// heads of 128 values: 32 sequences of 2000 tokens 44 us against 56, 8 of 32000 134 against 143, one of 8000 22 against 29;
+// 128 rows in fours 80, 221 and 26 against 79, 192 and 37).  In bf16: 64 rows of 8 sequences of 8000 tokens 99 us in two
+// blocks, 70 in one; 256 rows 191 by 32, 160 by 64, 122 by 128, 104 in one.
+int draft_rows(int rows_kind, int n, int group, int head_dim) {
     const int rows = n * group;
-    return rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 || head_dim == 256 ? 128 : 256;
+    if (rows <= 32 || (rows <= 64 && rows_kind == kRowsFour && head_dim <= 128)) return 32;
+    return rows <= 64 ? 64 : rows <= 128 || head_dim == 256 ? 128 : 256;
 }
 
 hipError_t draft_occupancy(int rows_kind, int head_dim, int rows, int* blocks_per_cu) {
@@ -878,7 +922,7 @@ hipError_t launch_drafts(const DraftArgs& args, int rows_kind, int head_dim, int
     DraftArgs a = args;
     a.scale_log2 = (float)(1.4426950408889634 / __builtin_sqrt((double)head_dim));
     a.lazy = kLazy / a.scale_log2;
-    return dispatch(a, rows_kind, head_dim, draft_rows(a.N, a.Hq / a.Hkv, head_dim), DraftLaunch{blocks, s, nullptr});
+    return dispatch(a, rows_kind, head_dim, draft_rows(rows_kind, a.N, a.Hq / a.Hkv, head_dim), DraftLaunch{blocks, s, nullptr});
 }
 
 hipError_t launch_accept(const AcceptArgs& a, hipStream_t s) {

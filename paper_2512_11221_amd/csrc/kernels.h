@@ -401,7 +401,7 @@ hipError_t launch_get_rows(const RowsArgs& a, bool four, hipStream_t s);
 hipError_t launch_rotate(const RotateArgs& a, int bf16, hipStream_t s);
 // Query rows of a workgroup that attends drafts of n nodes, and workgroups of that kind
 // that a CU holds.
-int draft_rows(int n, int group, int head_dim);
+int draft_rows(int rows_kind, int n, int group, int head_dim);
 // Blocks of those rows, at most.
 constexpr int kDraftBlocks = kMaxDrafts * 8 / 128;
 hipError_t draft_occupancy(int rows_kind, int head_dim, int rows, int* blocks_per_cu);

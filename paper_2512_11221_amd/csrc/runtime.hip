@@ -357,6 +357,7 @@ hipError_t follow_last_stream(asrkf_ctx* ctx, hipStream_t s) {
     return e;
 }
 
+int draft_kind(int rows) { return rows == 32 ? 0 : rows == 64 ? 1 : rows == 128 ? 2 : 3; }
 int row_kind(const asrkf_ctx* ctx) {
     return ctx->four ? kRowsFour : ctx->cfg.dtype == ASRKF_BF16 ? kRowsBF16 : kRowsF32;
 }
@@ -1471,14 +1472,16 @@ asrkf_status asrkf_reserve_drafts(asrkf_ctx* ctx, int32_t max_nodes) {
     if (st != ASRKF_OK) return st;
     // partials: two slots of every attention workgroup, by the kind of workgroup
     size_t acc = 0, ml = 0;
-    for (int i = 0, rows = 32; i < 4; ++i, rows *= 2) {
-        if (rows > draft_rows(max_nodes, ctx->group, c.head_dim)) break;
+    int grid[4] = {};
+    for (int n = 1; n <= max_nodes; ++n) {
+        const int rows = draft_rows(row_kind(ctx), n, ctx->group, c.head_dim), i = draft_kind(rows);
+        if (grid[i]) continue;
         int per_cu = 0;
         HIP_OK(ctx, draft_occupancy(row_kind(ctx), c.head_dim, rows, &per_cu));
         if (per_cu < 1) return fail(ASRKF_EINVAL, "draft attention workgroup does not fit on a CU for this shape");
-        ctx->draft_grid[i] = per_cu * ctx->cus;
-        acc = std::max(acc, (size_t)2 * ctx->draft_grid[i] * rows * c.head_dim * 4);
-        ml = std::max(ml, (size_t)2 * ctx->draft_grid[i] * rows * 2 * 4);
+        grid[i] = per_cu * ctx->cus;
+        acc = std::max(acc, (size_t)2 * grid[i] * rows * c.head_dim * 4);
+        ml = std::max(ml, (size_t)2 * grid[i] * rows * 2 * 4);
     }
     const size_t B = (size_t)c.batch;
     void* parts[9] = {};
@@ -1516,6 +1519,7 @@ asrkf_status asrkf_reserve_drafts(asrkf_ctx* ctx, int32_t max_nodes) {
     ctx->draft_acc = static_cast<float*>(parts[6]);
     ctx->draft_ml = static_cast<float*>(parts[7]);
     ctx->verify_chance = static_cast<float2*>(parts[8]);
+    for (int i = 0; i < 4; ++i) ctx->draft_grid[i] = grid[i];
     ctx->draft_nodes = max_nodes;
     return ASRKF_OK;
 }
@@ -1619,8 +1623,7 @@ asrkf_status asrkf_attend_drafts(asrkf_ctx* ctx, int32_t layer, int32_t n_nodes,
     a.Hq = c.n_q_heads;
     a.Hkv = c.n_kv_heads;
     a.pool_rows = ctx->pool_rows;
-    const int rows = draft_rows(n_nodes, ctx->group, c.head_dim);
-    a.grid = ctx->draft_grid[rows == 32 ? 0 : rows == 64 ? 1 : rows == 128 ? 2 : 3];
+    a.grid = ctx->draft_grid[draft_kind(draft_rows(row_kind(ctx), n_nodes, ctx->group, c.head_dim))];
     HIP_OK(ctx, launch_drafts(a, row_kind(ctx), c.head_dim, a.grid, s));
     return ASRKF_OK;
 }
