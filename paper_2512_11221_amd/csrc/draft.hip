@@ -30,11 +30,15 @@ namespace {
 
 constexpr int kStreamPolicy = 2;              // non-temporal: rows that one workgroup reads
 constexpr int kNowhere = (int)0x80000000;     // past every buffer's range: reads as zeros
-// What a piece costs a workgroup beside its rows, in tiles.
-constexpr int kDraftPieceCost = 2;
-// Tiles of a part at least; up to which half of the workgroups do; and parts of a pair at most.
-// (fp32 tiles, whose products take sixteen times as long, go one by one.)
-constexpr int kDraftLeast = 2, kDraftShort = 8, kDraftParts = 16;
+// What a piece costs a workgroup beside its rows, in tiles: about 5.5 us against 1.7 a tile of 128 keys in 4 bits (32
+// sequences of 350 to 2800 tokens, 8 KV heads, 64 rows each: 62.7 us, with 2 64.6, with 5 63.0).
+constexpr int kDraftPieceCost = 3;
+// The tiles of a part up to which half of the workgroups do (32 rows of 8 sequences of 2000 tokens, 8 KV heads: 28.6 us, with
+// 4 32.8), and the parts of a pair at most (one sequence of 8000: 25.2 us with 16 parts, 28.2 with 32; 64 rows 29.2, with 8 32.5).
+constexpr int kDraftShort = 8, kDraftParts = 16;
+// Tiles of a part at least: a tile of nodes and one of the list stay together (100 tokens: 12.2 us, apart 13.6), but for fp32,
+// whose products take sixteen times as long.
+constexpr int kDraftLeast = 2;
 // As for prompts: the rescaling of O waits until a row's maximum has grown by 2^kLazy.
 constexpr float kLazy = 8.f;
 
@@ -309,9 +313,10 @@ draft_kernel(DraftArgs a) {
         const int row = wr0 + col;                        // the lane's query row
         const int node = min(row >> group_shift, nodes - 1);      // rows past the end repeat the last node's
         // where the lane's i-th piece of K and q lies in a row: the two halves of a wave's lanes take eight dims each
-        // of a product of 16, or all of a half row's in turn
+        // of a product of 16, or 32 in turn, or a half row
         const auto piece_at = [&](int i) __attribute__((always_inline)) {
-            return BF16 && !T::kDirect ? i * 32 + half * 16 : half * (T::kRow / 2) + i * 16;
+            if constexpr (T::kDirect) return (i / 4 * 2 + half) * 64 + i % 4 * 16;
+            else return BF16 ? i * 32 + half * 16 : half * (T::kRow / 2) + i * 16;
         };
         // ---- the list's tiles: an entry per lane, then the rows ----
         constexpr int kStages = T::kStages;
@@ -332,16 +337,19 @@ draft_kernel(DraftArgs a) {
                 const bool in = p >= 0 && (T::kPoolTotal % T::kLoaders == 0 || i < T::kPoolTotal);
                 const int off = in ? p * T::kPoolRow + i % T::kPoolPieces * 16 : kNowhere;
                 const int so = in ? p * (D / kScaleGroup) + i % T::kPoolPieces : kNowhere;
-                int k_off = off, k_so = so;
-                if constexpr (T::kDirect) {               // the lane's key and half of its row
-                    const int kp = __shfl(entry, col), piece = half * NL + u;
-                    k_off = kp >= 0 ? kp * T::kPoolRow + piece * 16 : kNowhere;
-                    k_so = kp >= 0 ? kp * (D / kScaleGroup) + piece : kNowhere;
+                int k_off = off;
+                if constexpr (T::kDirect) {               // the lane's key, every other piece of its row
+                    const int kp = __shfl(entry, col);
+                    k_off = kp >= 0 ? kp * T::kPoolRow + (2 * u + half) * 16 : kNowhere;
+                    if (u == 0) {                         // all scales of the row
+                        const int k_so = kp >= 0 ? kp * (D / kScaleGroup) : kNowhere;
+                        ks[g][0] = NL == 2 ? __builtin_amdgcn_raw_buffer_load_b32(rks, k_so, 0, 0) : __builtin_amdgcn_raw_buffer_load_b16(rks, k_so, 0, 0);
+                    }
                 }
                 kx[g][u] = __builtin_bit_cast(intx4, __builtin_amdgcn_raw_buffer_load_b128(rk, k_off, 0, kStreamPolicy));
                 vx[g][u] = __builtin_bit_cast(intx4, __builtin_amdgcn_raw_buffer_load_b128(rv, off, 0, kStreamPolicy));
                 if constexpr (FOUR) {
-                    ks[g][u] = __builtin_amdgcn_raw_buffer_load_b8(rks, k_so, 0, 0);
+                    if constexpr (!T::kDirect) ks[g][u] = __builtin_amdgcn_raw_buffer_load_b8(rks, so, 0, 0);
                     vs[g][u] = __builtin_amdgcn_raw_buffer_load_b8(rvs, so, 0, 0);
                 }
             }
@@ -358,7 +366,7 @@ draft_kernel(DraftArgs a) {
                 if constexpr (FOUR) {
                     // neighbouring lanes stand 64 bytes apart: each writes its four quarters from another one on, so
                     // that they meet no bank twice
-                    const float kf = scale_value(ks[g][u]), vf = scale_value(vs[g][u]);
+                    const float kf = T::kDirect ? 0.f : scale_value(ks[g][u]), vf = scale_value(vs[g][u]);
                     const int turned = lane & 3;
                     const intx4 kq = quarters_from(kx[g][u], turned), vq = quarters_from(vx[g][u], turned);
 #pragma unroll
@@ -583,7 +591,7 @@ draft_kernel(DraftArgs a) {
 #pragma unroll
                         for (int u = 0; u < NL; ++u) {
                             x[u] = kx[g][u];
-                            f[u] = scale_value(ks[g][u]);
+                            f[u] = scale_value(ks[g][0] >> (2 * u + half) * 8 & 0xFF);
                         }
                         turn(STAGE, j, 0);
                         __builtin_amdgcn_wave_barrier();
