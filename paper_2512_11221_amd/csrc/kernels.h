@@ -240,7 +240,7 @@ struct RowsArgs {
 
 // Rotary positions (rotate.hip): rows of queries and keys turned by their positions.
 constexpr int kMaxPairs = 128;
-constexpr int kMaxRotateRows = 1 << 25;       // a grid of 2^31 threads, four rows to a workgroup of 256
+constexpr int kMaxRotateRows = 1 << 25;
 struct RotateArgs {
     const char* x[2];         // [n][heads][D], rows x_stride bytes apart (16-byte aligned, as the strides)
     char* y[2];               // the same, y_stride apart; may be x

@@ -101,22 +101,24 @@ def test_in_place_on_slices_of_a_fused_projection(dtype, layout):
         A.asrkf_destroy(ctx)
 
 
-def test_the_most_rows():
-    """2^25 rows of 128 bytes: 4 GiB, turned in place."""
+@pytest.mark.parametrize("heads,dim,n", [(1, 64, 1 << 25), (32, 128, (1 << 23) + 4096)])
+def test_the_most_rows(heads, dim, n):
+    """2^25 rows of 128 bytes, and more rows of 8 KiB than a grid has workgroups for (64 GiB): turned in place."""
     import torch
-    A, ctx = _init(2, 1, 1, 64)
+    A, ctx = _init(2, heads, heads, dim)
     try:
-        A.asrkf_set_rotary(ctx, 64)
-        freq = A.asrkf_rotary_table(64, 64)
-        n = 1 << 25
-        x = _rows(4096, 1, 64, "bf16").repeat(n // 4096, 1, 1)
-        some = torch.cat([torch.arange(i, i + 100) for i in (0, (1 << 24) - 50, n - 100)]).cuda()
+        A.asrkf_set_rotary(ctx, dim)
+        freq = A.asrkf_rotary_table(dim, dim)
+        x = _rows(4096, heads, dim, "bf16").repeat(n // 4096, 1, 1)
+        some = torch.cat([torch.arange(i, i + 100) for i in (0, (1 << 22) - 50, n - 100)]).cuda()
         before = x[some]
         pos = torch.arange(n, device="cuda", dtype=torch.int32)
         A.asrkf_rotate(ctx, pos, None, None, x, x)
         R.check(x[some], *R.turned(before, some, freq, "halves"))
     finally:
         A.asrkf_destroy(ctx)
+        del x
+        torch.cuda.empty_cache()
 
 
 def test_values_that_are_not_finite_stay_in_their_pair():
