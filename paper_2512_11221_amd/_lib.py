@@ -306,21 +306,23 @@ def _rows(ctx, name, x, kv, n=None):
     heads (1): their number and the elements from one to the next.  The dimensions before the heads
     have to be evenly spaced."""
     shape = x.shape
-    layout = ctx.layout if type(ctx) is Context else None
-    if layout is not None:
+    if len(shape) < 3:
+        raise AsrkfError(EINVAL, f"{name} must be [..., heads, dim]")
+    heads, dim = shape[-2], shape[-1]
+    if type(ctx) is Context:
+        layout = ctx.layout
         if x.dtype is not layout[3]:
             raise AsrkfError(EINVAL, f"{name} is {x.dtype}, the context {layout[3]}")
-        if len(shape) < 3 or shape[-2] != layout[kv] or shape[-1] != layout[2]:
+        if heads != layout[kv] or dim != layout[2]:
             raise AsrkfError(EINVAL, f"{name} must be [..., {layout[kv]}, {layout[2]}], not {tuple(shape)}")
-    elif len(shape) < 3:
-        raise AsrkfError(EINVAL, f"{name} must be [..., heads, dim]")
-    rows = x.numel() // (shape[-2] * shape[-1])
+    token = heads * dim
+    rows = x.numel() // token
     if n is not None and rows != n:
         raise AsrkfError(EINVAL, f"{name} has {rows} rows, not {n}")
     if x.is_contiguous():
-        return rows, shape[-2] * shape[-1] if rows > 1 else 0
+        return rows, token if rows > 1 else 0
     stride = x.stride()
-    if stride[-1] != 1 or (shape[-2] > 1 and stride[-2] != shape[-1]):
+    if stride[-1] != 1 or (heads > 1 and stride[-2] != dim):
         raise ValueError(f"{name}: the heads of a token must be dense rows")
     step, size = 0, 1                # of the last dimension that has more than one row; rows behind it
     for d in range(len(shape) - 3, -1, -1):
@@ -328,7 +330,7 @@ def _rows(ctx, name, x, kv, n=None):
             continue
         if step == 0:
             step = stride[d]
-            if step < shape[-2] * shape[-1]:
+            if step < token:
                 raise ValueError(f"{name}: tokens overlap")
         elif stride[d] != step * size:
             raise ValueError(f"{name}: tokens must be evenly spaced")
@@ -340,35 +342,39 @@ def _array(name, x, dtype, shape, optional=False):
     """The address of a dense tensor of that type and shape (None for one that may be left out)."""
     if x is None and optional:
         return None
+    if x.dtype is dtype and x.shape == shape and x.is_contiguous():
+        return x.data_ptr()
     if x.dtype is not dtype:
         raise AsrkfError(EINVAL, f"{name} is {x.dtype}, not {dtype}")
     if x.shape != shape:
         raise AsrkfError(EINVAL, f"{name} is {tuple(x.shape)}, not {shape}")
-    if not x.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
-    return x.data_ptr()
+    raise ValueError(f"{name} must be contiguous")
 
 
 def asrkf_rotate(ctx, pos, q, q_out, k, k_out, rows_per_seq=0, inverse=False, stream=None):
     """q, q_out [..., q heads, dim], k, k_out [..., KV heads, dim]: as many rows each, evenly spaced; pos:
     an int32 tensor of as many entries (or None with rows_per_seq)."""
     import torch
-    n, strides = None, []
-    for name, x, y, kv in (("q", q, q_out, 0), ("k", k, k_out, 1)):
-        if (x is None) != (y is None):
-            raise ValueError(f"{name} and its output go together")
-        for what, t in ((name, x), (f"{name}_out", y)):
-            if t is None:
-                strides.append(0)
-                continue
-            n, step = _rows(ctx, what, t, kv, n)
-            strides.append(step)
+    if (q is None) != (q_out is None) or (k is None) != (k_out is None):
+        raise ValueError("q and k each go with their output")
+    n, qp, qs, yp, ys, kp, ks, zp, zs = None, None, 0, None, 0, None, 0, None, 0
+    if q is not None:
+        n, qs = _rows(ctx, "q", q, 0)
+        _, ys = _rows(ctx, "q_out", q_out, 0, n)
+        qp, yp = q.data_ptr(), q_out.data_ptr()
+    if k is not None:
+        n, ks = _rows(ctx, "k", k, 1, n)
+        _, zs = _rows(ctx, "k_out", k_out, 1, n)
+        kp, zp = k.data_ptr(), k_out.data_ptr()
     if n is None:
         raise ValueError("neither q nor k")
-    if pos is not None and (pos.dtype is not torch.int32 or pos.numel() != n or not pos.is_contiguous()):
-        raise AsrkfError(EINVAL, f"pos must be {n} contiguous int32, not {tuple(pos.shape)} {pos.dtype}")
-    _check(load().asrkf_rotate(ctx, n, rows_per_seq, _ptr(pos), _ptr(q), strides[0], _ptr(q_out), strides[1], _ptr(k), strides[2],
-                               _ptr(k_out), strides[3], 1 if inverse else 0, _stream(stream)))
+    if pos is not None:
+        if pos.dtype is not torch.int32 or pos.numel() != n or not pos.is_contiguous():
+            raise AsrkfError(EINVAL, f"pos must be {n} contiguous int32, not {tuple(pos.shape)} {pos.dtype}")
+        pos = pos.data_ptr()
+    code = load().asrkf_rotate(ctx, n, rows_per_seq, pos, qp, qs, yp, ys, kp, ks, zp, zs, 1 if inverse else 0, _stream(stream))
+    if code:
+        _check(code)
 
 
 def asrkf_reserve_drafts(ctx, max_nodes):
@@ -406,7 +412,7 @@ def asrkf_attend_drafts(ctx, layer, sees, q, k, v, out, count=None, stream=None)
         raise ValueError("out must be contiguous")
     sees = _array("sees", sees, torch.uint64 if sees.dtype is torch.uint64 else torch.int64, (B, N))
     count = _array("count", count, torch.int32, (B,), optional=True)
-    _check(load().asrkf_attend_drafts(ctx, layer, N, count, sees, _ptr(q), sq, _ptr(k), sk, _ptr(v), sv, _ptr(out),
+    _check(load().asrkf_attend_drafts(ctx, layer, N, count, sees, q.data_ptr(), sq, k.data_ptr(), sk, v.data_ptr(), sv, out.data_ptr(),
                                       _stream(stream)))
 
 

@@ -18,7 +18,7 @@
 // Launches: the sums of every row of logits, in parts of at most 64 to a row, and the walk, a workgroup to a
 // sequence, which also draws the next token: the parts' sums say which part holds the drawn point, and
 // only that one is read again.  The sums of 17 rows of 50257 logits of 32 sequences take 21.6 us (3.7 TB/s; the 64-bit
-// exponentials about 10 of it), of 6 rows of 128256 of 8 8.6; the walk, bound by round trips, 8 to 10.  Where the walk ends behind a rejection with draft probabilities the
+// operations alone are 11 at the vector units' rate), of 6 rows of 128256 of 8 8.6; the walk, bound by round trips, 8 to 10.  Where the walk ends behind a rejection with draft probabilities the
 // weights are other ones, whose sums a third launch forms.
 #include "kernels.h"
 #include "tiles.h"
