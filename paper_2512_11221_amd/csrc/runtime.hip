@@ -394,11 +394,24 @@ hipError_t clear_state(asrkf_ctx* ctx, hipStream_t s) {
     return launch_clear(a, s);
 }
 
+// Allocations that a call has looked up, where arrays of its often lie in one.
+struct Allocations {
+    int n = 0;
+    struct { const char* base; size_t size; } of[4];
+};
+
 // Whether a kernel on the context's device may read p[0 .. bytes): memory of that
 // device (inside says whether the range lies in p's allocation).  Host memory,
 // another device's, and pointers that the runtime does not know are left to the
 // runtime's own copies, which take or refuse them.
-bool kernel_readable(const asrkf_ctx* ctx, const void* p, size_t bytes, bool* inside) {
+bool kernel_readable(const asrkf_ctx* ctx, const void* p, size_t bytes, bool* inside, Allocations* seen = nullptr) {
+    const char* at = static_cast<const char*>(p);
+    for (int i = 0; seen && i < seen->n; ++i) {
+        const auto& a = seen->of[i];
+        if (at < a.base || at >= a.base + a.size) continue;
+        *inside = bytes <= (size_t)(a.base + a.size - at);
+        return true;
+    }
     *inside = true;
     hipPointerAttribute_t attr{};
     hipDeviceptr_t base = nullptr;
@@ -409,7 +422,11 @@ bool kernel_readable(const asrkf_ctx* ctx, const void* p, size_t bytes, bool* in
         (void)hipGetLastError();
         return false;
     }
-    *inside = static_cast<const char*>(p) + bytes <= static_cast<const char*>(base) + size;
+    *inside = at + bytes <= static_cast<const char*>(base) + size;
+    if (seen && seen->n < 4) {
+        seen->of[seen->n].base = static_cast<const char*>(base);
+        seen->of[seen->n++].size = size;
+    }
     return true;
 }
 
@@ -1364,6 +1381,7 @@ asrkf_status asrkf_rotate(asrkf_ctx* ctx, int32_t n_rows, int32_t rows_per_seq, 
         {"q", q, q_stride, q_out, q_out_stride, c.n_q_heads}, {"k", k, k_stride, k_out, k_out_stride, c.n_kv_heads}};
     struct Span { const void* p; size_t bytes; };
     Span from[2] = {}, to[2] = {};
+    Allocations seen;
     for (int i = 0; i < 2; ++i) {
         const auto& r = both[i];
         if (!r.x) continue;
@@ -1380,7 +1398,7 @@ asrkf_status asrkf_rotate(asrkf_ctx* ctx, int32_t n_rows, int32_t rows_per_seq, 
             if (!aligned16(p)) return fail(ASRKF_EINVAL, "%s and its output must be 16-byte aligned", r.name);
             const size_t size = (size_t)(n_rows - 1) * bytes[o] + row;
             bool inside;
-            if (!kernel_readable(ctx, p, size, &inside))
+            if (!kernel_readable(ctx, p, size, &inside, &seen))
                 return fail(ASRKF_EINVAL, "%s and its output must be in memory of the context's device", r.name);
             if (!inside) return fail(ASRKF_EINVAL, "%s or its output is smaller than %d rows", r.name, n_rows);
             (o ? to : from)[i] = Span{p, size};
@@ -1416,7 +1434,7 @@ asrkf_status asrkf_rotate(asrkf_ctx* ctx, int32_t n_rows, int32_t rows_per_seq, 
     bool inside;
     if (pos) {
         if (reinterpret_cast<uintptr_t>(pos) & 3) return fail(ASRKF_EINVAL, "positions must be 4-byte aligned");
-        if (!kernel_readable(ctx, pos, (size_t)n_rows * 4, &inside) || !inside)
+        if (!kernel_readable(ctx, pos, (size_t)n_rows * 4, &inside, &seen) || !inside)
             return fail(ASRKF_EINVAL, "positions must be %d int32 in memory of the context's device", n_rows);
         for (const Span& x : to)
             if (x.p && overlap(x.p, x.bytes, pos, (size_t)n_rows * 4)) return fail(ASRKF_EINVAL, "an output overlaps the positions");
@@ -1537,11 +1555,11 @@ asrkf_status check_drafts(const asrkf_ctx* ctx, int n_nodes) {
 
 // An array of the caller's that a kernel reads or writes: aligned to its elements, and inside
 // its allocation.
-asrkf_status check_array(const asrkf_ctx* ctx, const char* name, const void* p, size_t bytes, size_t align) {
+asrkf_status check_array(const asrkf_ctx* ctx, Allocations& seen, const char* name, const void* p, size_t bytes, size_t align) {
     if (!p) return fail(ASRKF_EINVAL, "null %s", name);
     if (reinterpret_cast<uintptr_t>(p) % align) return fail(ASRKF_EINVAL, "%s must be %zu-byte aligned", name, align);
     bool inside;
-    if (!kernel_readable(ctx, p, bytes, &inside)) return fail(ASRKF_EINVAL, "%s must be in memory of the context's device", name);
+    if (!kernel_readable(ctx, p, bytes, &inside, &seen)) return fail(ASRKF_EINVAL, "%s must be in memory of the context's device", name);
     if (!inside) return fail(ASRKF_EINVAL, "%s is smaller than %zu bytes", name, bytes);
     return ASRKF_OK;
 }
@@ -1573,6 +1591,7 @@ asrkf_status asrkf_attend_drafts(asrkf_ctx* ctx, int32_t layer, int32_t n_nodes,
     asrkf_status st = check_ctx(ctx);
     if (st != ASRKF_OK) return st;
     const asrkf_config& c = ctx->cfg;
+    Allocations seen;
     CHECK(check_drafts(ctx, n_nodes));
     if (layer < 0 || layer >= c.n_layers) return fail(ASRKF_EINVAL, "layer out of range");
     if (!ctx->lists_ready) return fail(ASRKF_ESTATE, "drafts attend from the first decode step on");
@@ -1589,10 +1608,10 @@ asrkf_status asrkf_attend_drafts(asrkf_ctx* ctx, int32_t layer, int32_t n_nodes,
         {"v", v, (tokens - 1) * a.v_stride + c.n_kv_heads * head, 16},
         {"sees", sees, tokens * 8, 8},
         {"count", count, (size_t)c.batch * 4, 4}};
-    CHECK(check_array(ctx, "out", out, out_bytes, 16));
+    CHECK(check_array(ctx, seen, "out", out, out_bytes, 16));
     for (const auto& x : arrays) {
         if (x.p == count && !count) continue;     // optional
-        CHECK(check_array(ctx, x.name, x.p, x.bytes, x.align));
+        CHECK(check_array(ctx, seen, x.name, x.p, x.bytes, x.align));
         if (overlap(x.p, x.bytes, out, out_bytes)) return fail(ASRKF_EINVAL, "out overlaps %s", x.name);
     }
     hipStream_t s = static_cast<hipStream_t>(stream);
@@ -1636,6 +1655,7 @@ asrkf_status asrkf_verify_drafts(asrkf_ctx* ctx, int32_t n_nodes, const int32_t*
     asrkf_status st = check_ctx(ctx);
     if (st != ASRKF_OK) return st;
     const asrkf_config& c = ctx->cfg;
+    Allocations seen;
     CHECK(check_drafts(ctx, n_nodes));
     if (!(temperature >= 0.f) || isinf(temperature) || (temperature > 0.f && temperature < 1e-6f))
         return fail(ASRKF_EINVAL, "temperature must be 0 or finite and at least 1e-6");
@@ -1655,7 +1675,7 @@ asrkf_status asrkf_verify_drafts(asrkf_ctx* ctx, int32_t n_nodes, const int32_t*
         {"u", u, (nodes + B) * 4, false, temperature == 0.f}};
     for (const auto& x : arrays) {
         if (!x.p && x.optional) continue;
-        CHECK(check_array(ctx, x.name, x.p, x.bytes, 4));
+        CHECK(check_array(ctx, seen, x.name, x.p, x.bytes, 4));
         for (const auto& y : arrays)
             if (&x != &y && y.written && y.p && overlap(x.p, x.bytes, y.p, y.bytes))
                 return fail(ASRKF_EINVAL, "%s overlaps %s", y.name, x.name);
@@ -1694,6 +1714,7 @@ asrkf_status asrkf_accept_drafts(asrkf_ctx* ctx, int32_t n_nodes, const int32_t*
     asrkf_status st = check_ctx(ctx);
     if (st != ASRKF_OK) return st;
     const asrkf_config& c = ctx->cfg;
+    Allocations seen;
     CHECK(check_drafts(ctx, n_nodes));
     if (!ctx->lists_ready || ctx->next_layer != 0)
         return fail(ASRKF_ESTATE, "drafts are accepted between two steps: after asrkf_restore, before the next decode_step");
@@ -1710,10 +1731,10 @@ asrkf_status asrkf_accept_drafts(asrkf_ctx* ctx, int32_t n_nodes, const int32_t*
         if (x.layer < 0 || x.layer > ((int64_t)1 << 40)) return fail(ASRKF_EINVAL, "%s: layer stride out of range", x.name);
         *x.out = x.layer ? x.layer * (int64_t)ctx->esz : dense;
         if (*x.out % 16) return fail(ASRKF_EINVAL, "%s: the layer stride must be a multiple of 16 bytes", x.name);
-        CHECK(check_array(ctx, x.name, x.p, (size_t)(c.n_layers - 1) * *x.out + one, 16));
+        CHECK(check_array(ctx, seen, x.name, x.p, (size_t)(c.n_layers - 1) * *x.out + one, 16));
     }
-    CHECK(check_array(ctx, "path", path, tokens * 4, 4));
-    CHECK(check_array(ctx, "n_path", n_path, (size_t)c.batch * 4, 4));
+    CHECK(check_array(ctx, seen, "path", path, tokens * 4, 4));
+    CHECK(check_array(ctx, seen, "n_path", n_path, (size_t)c.batch * 4, 4));
     hipStream_t s = static_cast<hipStream_t>(stream);
     const bool capture = capturing(s);
     for (int b = 0; b < c.batch; ++b) {
