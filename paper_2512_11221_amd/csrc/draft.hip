@@ -249,6 +249,11 @@ __device__ __forceinline__ float weight(float m, float M, float scale_log2) {
 // that it ends (or holds the middle of) and one for the pair that it begins.
 __device__ __forceinline__ int draft_slot(int first, bool aligned, int k) { return aligned ? first + k : first + (k ? 2 * k : 1); }
 
+// Where four dims of a row stand in a partial, as the walk's threads write them: rows one after the other, or a
+// row to a lane.
+template <bool SPLIT, int D>
+__device__ __forceinline__ int partial_at(int rows, int row, int quad) { return SPLIT ? row * D + quad * 4 : (quad * rows + row) * 4; }
+
 // Four dims of a query row of (sequence, KV head), from its sums: zeros where nothing was seen.
 template <bool BF16, int D>
 __device__ __forceinline__ void write_row(const DraftArgs& a, int b, int kvh, int row, int quad, floatx4 o, float sum) {
@@ -360,8 +365,9 @@ draft_kernel(DraftArgs a) {
                 }
             }
         };
-        auto keep = [&](auto STAGE, int buf) __attribute__((always_inline)) {
+        auto keep = [&](auto STAGE, int from, int buf) __attribute__((always_inline)) {
             constexpr int g = decltype(STAGE)::value;
+            if (T::kSplit && from >= n) return;           // (nothing of it is the wave's)
             char* kt = tiles_lds + buf * T::kKBuffer;
             char* vt = tiles_lds + T::kBuffers * T::kKBuffer + buf * T::kVBuffer;
 #pragma unroll
@@ -396,6 +402,7 @@ draft_kernel(DraftArgs a) {
         // with them; asked for before, their registers were spilled.
         auto keep_nodes = [&](int from) __attribute__((always_inline)) {
             bool bad = false;
+            if (T::kSplit && from >= nodes) return bad;
 #pragma unroll 4
             for (int u = 0; u < T::kNodeLoads; ++u) {
                 const int i = loader + u * T::kLoaders, key = i / T::kPieces, piece = i % T::kPieces;
@@ -563,7 +570,7 @@ draft_kernel(DraftArgs a) {
 
         // tile j out of its stage into LDS, and tile j + kStages on its way
         auto turn = [&](auto STAGE, int j, int buf) __attribute__((always_inline)) {
-            keep(STAGE, buf);
+            keep(STAGE, tile_of(j) * T::kTileKeys, buf);
             const int entry = ahead[0];
 #pragma unroll
             for (int g = 0; g < kStages; ++g) ahead[g] = ahead[g + 1];
@@ -653,7 +660,7 @@ draft_kernel(DraftArgs a) {
                 write_row<BF16, D>(a, b, kvh, r0 + r, quad, o, sum);
                 return;
             }
-            *reinterpret_cast<floatx4*>(my_acc + (quad * T::kRows + r) * 4) = o;
+            *reinterpret_cast<floatx4*>(my_acc + partial_at<T::kSplit, D>(T::kRows, r, quad)) = o;
             if (quad == 0) {
                 my_ml[r] = mx;
                 my_ml[T::kRows + r] = sum;
@@ -673,8 +680,11 @@ draft_kernel(DraftArgs a) {
                 ml_lds[wave * 64 + 32 + col] = l;
             }
             __syncthreads();
-            for (int e = threadIdx.x; e < 32 * (D / 4); e += T::kThreads) {
-                const int r = e & 31, quad = e >> 5;
+            // rows one after the other, so that only those that are written take time (12 rows of 8 sequences of 8000
+            // tokens: 65 us, a row to a lane of all 32 71; 32 rows in 4 bits 43 and 42)
+#pragma unroll 2
+            for (int e = threadIdx.x; e < min(live_rows, 32) * (D / 4); e += T::kThreads) {
+                const int r = e / (D / 4), quad = e % (D / 4);
                 float M = -INFINITY, L = 0.f;
 #pragma unroll
                 for (int k = 0; k < KW; ++k) M = fmaxf(M, ml_lds[k * 64 + r]);
@@ -731,14 +741,15 @@ draft_kernel(DraftArgs a) {
 // The partials of a pair folded in their order, four dims of a row to a thread, several partials in
 // flight: 4 to 8 us, its launch and two round trips.
 constexpr int kFoldThreads = 256;
-template <bool BF16, int D>
+template <bool BF16, int D, bool SPLIT>
 __global__ void __launch_bounds__(kFoldThreads)
 fold_kernel(DraftArgs a, int rows) {
     constexpr int kQuads = D / 4, kRowsHere = kFoldThreads / kQuads, kPass = 8;
     const int gi = blockIdx.y, b = blockIdx.z;
     const int2 f = a.fold[(size_t)b * a.Hkv * a.row_blocks + gi];
     const int kvh = gi / a.row_blocks, r0 = gi % a.row_blocks * rows;
-    const int r = blockIdx.x * kRowsHere + threadIdx.x % kRowsHere, quad = threadIdx.x / kRowsHere;
+    const int r = blockIdx.x * kRowsHere + (SPLIT ? threadIdx.x / kQuads : threadIdx.x % kRowsHere);
+    const int quad = SPLIT ? threadIdx.x % kQuads : threadIdx.x / kRowsHere;
     // (pairs without nodes were not dealt: what stands there is of an earlier launch)
     if (r >= rows || r0 + r >= nodes_of(a, b) * (a.Hq / a.Hkv)) return;
     const bool aligned = f.x > 0;
@@ -754,7 +765,7 @@ fold_kernel(DraftArgs a, int rows) {
             const size_t slot = draft_slot(f.y, aligned, min(k0 + u, n_parts - 1));
             pm[u] = a.part_ml[slot * 2 * rows + r];
             pl[u] = a.part_ml[(slot * 2 + 1) * rows + r];
-            po[u] = *reinterpret_cast<const floatx4*>(a.part_acc + (slot * kQuads + quad) * rows * 4 + r * 4);
+            po[u] = *reinterpret_cast<const floatx4*>(a.part_acc + slot * rows * D + partial_at<SPLIT, D>(rows, r, quad));
         }
         float Mn = M;
 #pragma unroll
@@ -795,7 +806,7 @@ hipError_t launch_walk(const DraftArgs& args, const DraftLaunch& l) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const int rows = std::min(T::kRows, a.N * (a.Hq / a.Hkv)), per = kFoldThreads / (D / 4);
-    hipLaunchKernelGGL((fold_kernel<T::kBF16, D>), dim3((rows + per - 1) / per, a.Hkv * a.row_blocks, a.B), dim3(kFoldThreads), 0, l.stream, a,
+    hipLaunchKernelGGL((fold_kernel<T::kBF16, D, T::kSplit>), dim3((rows + per - 1) / per, a.Hkv * a.row_blocks, a.B), dim3(kFoldThreads), 0, l.stream, a,
                        T::kRows);
     return hipGetLastError();
 }

@@ -275,7 +275,7 @@ struct DraftArgs {
     const int32_t* list;      // layer base, [B][cap]
     const int32_t* n_active;  // layer base, [B]
     int32_t list_tail;        // entries at a list's end whose rows are not written: 0 or 1
-    float* part_acc;          // [slots][D / 4][rows][4] of the pairs that several workgroups share
+    float* part_acc;          // [slots][rows * D] of the pairs that several workgroups share
     float* part_ml;           // [slots][2][rows]
     int2* fold;               // [B][pairs of a sequence] their parts and where these lie (written)
     int32_t B, N, cap, Hq, Hkv, pool_rows;
