@@ -255,7 +255,8 @@ def test_large_values_and_scores(t):
 @pytest.mark.parametrize("Hq,Hkv,D,t,N,lens", [
     (32, 8, 128, "bf16", 5, [9000]), (32, 8, 128, "bf16", 60, [5000, 33]), (8, 1, 128, "four", 16, [20000, 700]), (16, 2, 64, "bf16", 64, [12000]),
     (16, 8, 256, "bf16", 12, [3000, 17]), (8, 2, 64, "f32", 30, [6000]), (32, 32, 128, "four", 3, [2000] * 3), (8, 2, 64, "bf16", 2, [30, 5000] * 5),
-    (4, 4, 128, "f32", 9, [100, 900, 2500])])
+    (4, 4, 128, "f32", 9, [100, 900, 2500]), (32, 8, 128, "four", 16, [20000, 700]), (16, 2, 64, "four", 7, [12000, 60]),
+    (8, 2, 128, "four", 13, [40] * 300)])
 def test_long_lists_are_shared(Hq, Hkv, D, t, N, lens):
     """Pairs cut over many workgroups, in equal parts and across the pairs; the same bits again."""
     import torch
@@ -281,6 +282,26 @@ def test_large_batches(B, N, t):
     rng = np.random.default_rng(B)
     lens = [int(x) for x in rng.integers(0, 200, B)]
     s = Setting(lens, 4, 2, 64, **_kind(t))
+    try:
+        sees, count = _masks(rng, B, N, "tree"), [int(x) for x in rng.integers(0, N + 1, B)]
+        q, k, v = s.nodes(N)
+        out = torch.full_like(q, 7.0)
+        s.A.asrkf_attend_drafts(s.ctx, 0, _sees(sees), q, k, v, out, count=torch.tensor(count, device="cuda", dtype=torch.int32))
+        for b in list(range(0, B, max(1, B // 40))) + [B - 1]:
+            ref, tol = s.reference(0, b, q, k, v, sees, count)
+            R.check(out[b, :count[b]], ref[:count[b]], tol[:count[b]])
+        for b in range(B):
+            assert (out[b, count[b]:] == 7.0).all()
+    finally:
+        s.close()
+
+
+@pytest.mark.parametrize("B,D,t,N", [(1024, 256, "bf16", 3), (1024, 128, "f32", 2), (1024, 128, "bf16", 5), (100, 256, "four", 24)])
+def test_large_batches_of_wide_rows(B, D, t, N):
+    """The plan of more than 64 sequences beside the largest tiles that a workgroup has."""
+    import torch
+    rng = np.random.default_rng(D + B)
+    s = Setting([int(x) for x in rng.integers(0, 40, B)], 4, 1, D, **_kind(t))
     try:
         sees, count = _masks(rng, B, N, "tree"), [int(x) for x in rng.integers(0, N + 1, B)]
         q, k, v = s.nodes(N)
