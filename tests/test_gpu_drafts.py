@@ -316,6 +316,26 @@ def test_large_batches_of_wide_rows(B, D, t, N):
         s.close()
 
 
+@pytest.mark.parametrize("Hq,Hkv,D,t", [(32, 8, 128, "bf16"), (16, 4, 128, "four"), (8, 2, 64, "f32"), (16, 4, 256, "bf16")])
+def test_room_that_grows(Hq, Hkv, D, t):
+    """Room for more nodes on the same context, then few and many nodes over lists that many workgroups share."""
+    s = Setting([6000, 300, 45], Hq, Hkv, D, nodes=1, **_kind(t))
+    try:
+        import torch
+        for room, ns in ((1, [1]), (9, [9, 2]), (64, [64, 1, 16, 31, 9])):
+            s.A.asrkf_reserve_drafts(s.ctx, room)
+            for N in ns:
+                sees, count = _masks(np.random.default_rng(N), s.B, N, "tree"), [N] * s.B
+                q, k, v = s.nodes(N)
+                out = torch.empty_like(q)
+                s.A.asrkf_attend_drafts(s.ctx, 0, _sees(sees), q, k, v, out)
+                for b in range(s.B):
+                    ref, tol = s.reference(0, b, q, k, v, sees, count)
+                    R.check(out[b], ref, tol)
+    finally:
+        s.close()
+
+
 def test_rows_past_two_gigabytes_of_a_pool():
     """The longest context: 2 GiB of K a sequence, the second sequence's rows beyond 32-bit offsets."""
     import torch
