@@ -152,10 +152,22 @@ ASRKF_HD bool next_piece(const Split& split, const Lists& lists, int w, int& x, 
     return false;
 }
 
-// How a step's attention is laid out when sequence b lists up to plen[b] + t
-// positions: KV heads a workgroup takes together, and how many workgroups to
-// launch (at least those with work, at most grid: idle ones delay the others).
-// Tiles of `tile` tokens; a wave has `room` bytes for relevance values.
+// How many workgroups to launch when sequence b lists up to plen[b] + t positions: at
+// least those with work, at most grid (idle ones delay the others).
+inline int attention_launch(const int32_t* plen, int batch, int t, int n_kv_heads, int tile, int grid, int heads_per_group) {
+    const int hw = heads_per_group;
+    const int64_t groups = n_kv_heads / hw;
+    const int cost = kPieceCost / hw > 1 ? kPieceCost / hw : 1;
+    const int least = kMinTiles / (hw < kMinTiles ? hw : kMinTiles);
+    int64_t live = 0;
+    for (int b = 0; b < batch && live < grid; ++b)
+        live += groups * (((plen[b] + t + tile - 1) / tile + cost + least - 1) / least);
+    return live < grid ? (live > 1 ? (int)live : 1) : grid;
+}
+
+// How a step's attention is laid out behind prompts of plen[b] tokens, t steps later: KV
+// heads a workgroup takes together, and the workgroups to launch.  Tiles of `tile`
+// tokens; a wave has `room` bytes for relevance values.
 inline void attention_layout(const int32_t* plen, int batch, int t, int n_kv_heads, int tile, int room, int grid,
                              int* heads_per_group, int* launch) {
     int64_t tiles = 0;
@@ -173,21 +185,16 @@ inline void attention_layout(const int32_t* plen, int batch, int t, int n_kv_hea
     // with eight).  The softmax reading keeps one value per query head either way and
     // its room holds fewer tiles; the same rule serves it (64 x 2k to 32k tokens: 831
     // us with one head, 808 with eight; 8 x 65k tokens of eight query heads, just on
-    // this side of the line: 417 and 455).  The choice rests on the prompts alone, so
-    // a step replayed from a graph is dealt like the same step run eagerly; lists that
-    // grow long from short prompts stay with the heads chosen for those (64 sequences
-    // grown from nothing to 18k tokens: 712 us a launch).
+    // this side of the line: 417 and 455).  The choice rests on the prompts alone, and not on
+    // what steps and accepted drafts have added, so that a step replayed from a graph is
+    // dealt like the same step run eagerly, and steps behind drafts alike whatever the host
+    // knows of their number; lists that grow long from short prompts stay with the heads
+    // chosen for those (64 sequences grown from nothing to 18k tokens: 712 us a launch).
     int hw = 1;
     if (tiles * n_kv_heads > (int64_t)room_tiles(tile, room) * grid) hw = n_kv_heads < 8 ? n_kv_heads : 8;
     while (hw < 8 && hw < n_kv_heads && (int64_t)batch * n_kv_heads / hw > grid) hw *= 2;
-    const int64_t groups = n_kv_heads / hw;
-    const int cost = kPieceCost / hw > 1 ? kPieceCost / hw : 1;
-    const int least = kMinTiles / (hw < kMinTiles ? hw : kMinTiles);
-    int64_t live = 0;
-    for (int b = 0; b < batch && live < grid; ++b)
-        live += groups * (((plen[b] + t + tile - 1) / tile + cost + least - 1) / least);
     *heads_per_group = hw;
-    *launch = live < grid ? (live > 1 ? (int)live : 1) : grid;
+    *launch = attention_launch(plen, batch, t, n_kv_heads, tile, grid, hw);
 }
 // ... of rows of 16 or 32 bits
 inline void attention_layout(const int32_t* plen, int batch, int t, int n_kv_heads, int row_bytes, int grid,

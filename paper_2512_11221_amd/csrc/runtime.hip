@@ -225,6 +225,7 @@ struct asrkf_ctx {
     bool accepted = false;              // asrkf_accept_drafts was called: the lengths grow on the device,
     bool accept_captured = false;       // by a graph's replays too
     std::vector<int32_t> plen_most;     // ... and are at most these (plen_host: as last read back)
+    std::vector<int32_t> prompt_len;    // the prompts', which the layout of a step rests on
 };
 
 namespace {
@@ -499,6 +500,7 @@ asrkf_status asrkf_init(const asrkf_config* cfg, asrkf_ctx** out) {
     ctx->scale_bytes = ctx->four ? (size_t)c.n_kv_heads * c.head_dim / kScaleGroup : 0;
     ctx->plen_host.assign(c.batch, 0);
     ctx->plen_most.assign(c.batch, 0);
+    ctx->prompt_len.assign(c.batch, 0);
     ctx->prefilled.assign(c.batch, 0);
 
     hipError_t e = hipGetDevice(&ctx->device);
@@ -725,7 +727,7 @@ asrkf_status asrkf_prefill(asrkf_ctx* ctx, int32_t layer, int32_t seq, const voi
         one.seq[0] = seq;
         HIP_OK(ctx, launch_prompt_store(p, one, s));
         ctx->prefilled[seq] = 1;
-        ctx->plen_host[seq] = ctx->plen_most[seq] = n_tokens;
+        ctx->plen_host[seq] = ctx->plen_most[seq] = ctx->prompt_len[seq] = n_tokens;
         mark_queued(ctx, s, capturing(s));
         return ASRKF_OK;
     }
@@ -755,7 +757,7 @@ asrkf_status asrkf_prefill(asrkf_ctx* ctx, int32_t layer, int32_t seq, const voi
     }
     HIP_OK(ctx, launch_prefill(p, s));
     ctx->prefilled[seq] = 1;
-    ctx->plen_host[seq] = ctx->plen_most[seq] = n_tokens;
+    ctx->plen_host[seq] = ctx->plen_most[seq] = ctx->prompt_len[seq] = n_tokens;
     mark_queued(ctx, s, capturing(s));
     return ASRKF_OK;
 }
@@ -848,7 +850,7 @@ asrkf_status asrkf_prefill_packed(asrkf_ctx* ctx, int32_t layer, int32_t n_seqs,
     }
     for (int i = 0; i < n_seqs; ++i) {
         ctx->prefilled[seqs[i]] = 1;
-        ctx->plen_host[seqs[i]] = ctx->plen_most[seqs[i]] = n_tokens[i];
+        ctx->plen_host[seqs[i]] = ctx->plen_most[seqs[i]] = ctx->prompt_len[seqs[i]] = n_tokens[i];
     }
     mark_queued(ctx, s, capturing(s));
     return ASRKF_OK;
@@ -1139,12 +1141,14 @@ asrkf_status decode_step_impl(asrkf_ctx* ctx, int32_t layer, const void* q, cons
     HIP_OK(ctx, follow_last_stream(ctx, s));
     mark_queued(ctx, s, capture);
     if (layer == 0) {
+        const int row = (int)(c.head_dim * ctx->esz), tile = ctx->four ? four_tile(c.head_dim) : tile_tokens(row);
         if (ctx->four)
-            attention_layout(ctx->plen_most.data(), c.batch, t, c.n_kv_heads, four_tile(c.head_dim), four_room(c.head_dim), ctx->grid,
+            attention_layout(ctx->prompt_len.data(), c.batch, t, c.n_kv_heads, tile, four_room(c.head_dim), ctx->grid,
                              &ctx->heads_per_group, &ctx->launch);
         else
-            attention_layout(ctx->plen_most.data(), c.batch, t, c.n_kv_heads, (int)(c.head_dim * ctx->esz), ctx->grid,
-                             &ctx->heads_per_group, &ctx->launch);
+            attention_layout(ctx->prompt_len.data(), c.batch, t, c.n_kv_heads, row, ctx->grid, &ctx->heads_per_group, &ctx->launch);
+        // accepted drafts: as many as there may be
+        if (ctx->accepted) ctx->launch = attention_launch(ctx->plen_most.data(), c.batch, t, c.n_kv_heads, tile, ctx->grid, ctx->heads_per_group);
         if (capture) ctx->launch = ctx->grid;    // replayed at later, longer steps
     }
     if (!ctx->lists_ready) {
@@ -1975,6 +1979,7 @@ asrkf_status asrkf_reset(asrkf_ctx* ctx) {
     if (ctx->flags_host) ctx->flags_host[0] = ctx->flags_host[1] = 0;
     ctx->plen_host.assign(c.batch, 0);
     ctx->plen_most.assign(c.batch, 0);
+    ctx->prompt_len.assign(c.batch, 0);
     ctx->accepted = ctx->accept_captured;
     ctx->prefilled.assign(c.batch, 0);
     ctx->t = 0;
