@@ -451,7 +451,8 @@ asrkf_status asrkf_verify_drafts(asrkf_ctx* ctx, int32_t n_nodes, const int32_t*
  *                 layer to the next, 0 for dense ones
  * The host learns how many were accepted at its next waiting call (as of replayed
  * steps); until then it counts every node, and a call that would then find no room
- * waits and looks.  ECAPACITY where a sequence has no room for n_nodes; a replayed
+ * waits and looks (one that is being captured goes by the lengths of the last waiting
+ * call).  ECAPACITY where a sequence has no room for n_nodes; a replayed
  * call without room appends nothing to that sequence, and the next waiting call
  * returns ECAPACITY.  ESTATE before the first decode step and within a step.
  * Asynchronous. */

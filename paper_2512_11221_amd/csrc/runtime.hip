@@ -1073,6 +1073,13 @@ asrkf_status learn_lengths(asrkf_ctx* ctx) {
     return st == ASRKF_OK ? check_overflow(ctx, true) : st;
 }
 
+// Room for n more positions of a sequence, by the most that it may hold.  A call that is being captured
+// cannot wait and look: it goes by the lengths that are known to be reached, and a replay that finds no
+// room is refused on the device.
+bool has_room(const asrkf_ctx* ctx, int b, int n, bool capture) {
+    return (capture ? ctx->plen_host[b] : ctx->plen_most[b]) + ctx->t + n <= ctx->cfg.max_ctx;
+}
+
 // The verdicts of the layers before layer_end whose planes are kept, and with e
 // the entropy monitors.
 hipError_t launch_verdicts(const asrkf_ctx* ctx, int layer_end, const EntropyArgs* e, hipStream_t s) {
@@ -1125,11 +1132,11 @@ asrkf_status decode_step_impl(asrkf_ctx* ctx, int32_t layer, const void* q, cons
     hipStream_t s = static_cast<hipStream_t>(stream);
     const bool capture = capturing(s);
     for (int b = 0; b < c.batch; ++b) {
-        if (ctx->plen_most[b] + ctx->t + 1 > c.max_ctx && layer == 0 && !capture) {
+        if (!has_room(ctx, b, 1, capture) && layer == 0 && !capture) {
             st = learn_lengths(ctx);      // accepted drafts may have been fewer
             if (st != ASRKF_OK) return st;
         }
-        if (ctx->plen_most[b] + ctx->t + 1 > c.max_ctx)
+        if (!has_room(ctx, b, 1, capture))
             return fail(ASRKF_ECAPACITY, "sequence %d would exceed max_ctx=%d", b, c.max_ctx);
     }
     const int t = ctx->t + 1;
@@ -1742,8 +1749,8 @@ asrkf_status asrkf_accept_drafts(asrkf_ctx* ctx, int32_t n_nodes, const int32_t*
     hipStream_t s = static_cast<hipStream_t>(stream);
     const bool capture = capturing(s);
     for (int b = 0; b < c.batch; ++b) {
-        if (ctx->plen_most[b] + ctx->t + n_nodes > c.max_ctx && !capture) CHECK(learn_lengths(ctx));
-        if (ctx->plen_most[b] + ctx->t + n_nodes > c.max_ctx)
+        if (!has_room(ctx, b, n_nodes, capture) && !capture) CHECK(learn_lengths(ctx));
+        if (!has_room(ctx, b, n_nodes, capture))
             return fail(ASRKF_ECAPACITY, "sequence %d has no room for %d nodes (max_ctx=%d)", b, n_nodes, c.max_ctx);
     }
     HIP_OK(ctx, follow_last_stream(ctx, s));

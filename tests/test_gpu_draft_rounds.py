@@ -37,3 +37,52 @@ def test_the_layout_of_a_step_does_not_hang_on_what_the_host_knows(kw, lens):
     finally:
         a.close()
         b.close()
+
+
+def test_a_round_is_captured_behind_drafts_that_were_counted_as_accepted():
+    """Ten rounds of rejected drafts: by the host's count the sequences are full, and a capture cannot look.  The
+    captured round runs until the room is really used up."""
+    import torch
+    r = Run([10, 3], N=4, max_ctx=40, L=2)
+    try:
+        A = r.A
+        k, v = r.nodes()
+        path, n_path = _i32([[0, 1, 2, 3]] * 2), _i32([0, 0])
+        q0 = [r.randn(2, h, 64) for h in (8, 2, 2)]
+        out = torch.empty((2, 2, 8, 64), device="cuda")
+
+        def calls():
+            for layer in range(2):
+                A.asrkf_decode_step(r.ctx, layer, *q0, out[layer])
+            A.asrkf_restore(r.ctx, None, A.NONE)
+            A.asrkf_accept_drafts(r.ctx, path, n_path, k, v)
+        calls()
+        assert r.state(0, 0)["n"] == 11
+        for _ in range(7):                           # 11 + 28 of 40
+            A.asrkf_accept_drafts(r.ctx, path, n_path, k, v)
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=torch.cuda.Stream()):
+            calls()
+        n_path.copy_(_i32([4, 1]))
+        torch.cuda.synchronize()
+        for t in range(1, 6):
+            g.replay()
+            torch.cuda.synchronize()
+            assert [r.state(1, b)["n"] for b in range(2)] == [11 + 5 * t, 4 + 2 * t]
+            torch.zeros(5000, device="cuda").sum().item()
+        # 36 of 40 are known now: a capture refuses what can never be replayed
+        torch.cuda.synchronize()
+        A.asrkf_accept_drafts(r.ctx, path, _i32([4, 0]), k, v)
+        assert r.state(0, 0)["n"] == 40
+        refused = []
+        g2 = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g2, stream=torch.cuda.Stream()):
+            torch.zeros(1, device="cuda")
+            for call in (lambda: A.asrkf_decode_step(r.ctx, 0, *q0, out[0]), lambda: A.asrkf_accept_drafts(r.ctx, path, n_path, k, v)):
+                with pytest.raises(A.AsrkfError) as e:
+                    call()
+                refused.append(e.value.code)
+        assert refused == [A._lib.ECAPACITY] * 2
+    finally:
+        r.close()
