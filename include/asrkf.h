@@ -454,7 +454,8 @@ asrkf_status asrkf_verify_drafts(asrkf_ctx* ctx, int32_t n_nodes, const int32_t*
  * waits and looks (one that is being captured goes by the lengths of the last waiting
  * call).  ECAPACITY where a sequence has no room for n_nodes; a replayed
  * call without room appends nothing to that sequence, and the next waiting call
- * returns ECAPACITY.  ESTATE before the first decode step and within a step.
+ * returns ECAPACITY, once: what the context holds stays good.  ESTATE before the first
+ * decode step and within a step.
  * Asynchronous. */
 asrkf_status asrkf_accept_drafts(asrkf_ctx* ctx, int32_t n_nodes, const int32_t* path, const int32_t* n_path,
                                  const void* k, int64_t k_stride, int64_t k_layer_stride, const void* v,

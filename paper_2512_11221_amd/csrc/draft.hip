@@ -911,7 +911,7 @@ accept_kernel(AcceptArgs a) {
     unsigned long long more = 0;
     for (int i = threadIdx.x; i < a.states * a.B; i += kAcceptThreads) {
         const int seq = i % a.B, len = a.plen[seq] + t, grow = taken(seq, len);
-        if (grow < 0) a.flags[1] = 1;
+        if (grow < 0) *a.no_room = 1;
         if (grow <= 0) continue;
         const int na = a.n_active[i];             // the last entry is the next token's position, len
         for (int j = 1; j <= grow; ++j) a.list[(size_t)i * a.cap + na - 1 + j] = len + j;

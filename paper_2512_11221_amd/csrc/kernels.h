@@ -299,7 +299,7 @@ struct AcceptArgs {
     int32_t* list;            // [states][B][cap] extended
     int32_t* n_active;
     unsigned long long* listed_total;
-    int32_t* flags;           // [1]: a sequence would pass max_ctx
+    int32_t* no_room;         // set where a sequence would pass max_ctx
     int32_t* ticket;          // zero between launches
     int32_t L, B, N, Hkv, pool_rows, head_bytes, four, cap, states, max_ctx;
 };

@@ -53,7 +53,7 @@ struct Status {
     unsigned long long counters[kCounters];
     int32_t flags[2];
     int32_t t;                  // steps started
-    int32_t pad;
+    int32_t no_room;            // accepted drafts of a replay were left out
 };
 
 asrkf_status fail(asrkf_status st, const char* fmt, ...) {
@@ -1034,6 +1034,21 @@ asrkf_status check_overflow(asrkf_ctx* ctx, bool synced) {
     return ASRKF_OK;
 }
 
+// Nodes that a replayed acceptance had no room for: said once by the next waiting call.  Their sequences
+// are as they were before it, and everything else is as it should be.
+asrkf_status report_no_room(asrkf_ctx* ctx) {
+    if (!ctx->status_host.no_room) return ASRKF_OK;
+    ClearArgs z{};
+    z.n = 1;
+    z.p[0] = &ctx->status->no_room;
+    z.words[0] = 1;
+    HIP_OK(ctx, launch_clear(z, nullptr));
+    HIP_OK(ctx, hipStreamSynchronize(nullptr));
+    ctx->status_host.no_room = 0;
+    return fail(ASRKF_ECAPACITY, "replayed drafts that were accepted had no room (max_ctx = %d) and were not "
+                "appended to their sequences", ctx->cfg.max_ctx);
+}
+
 }  // namespace
 
 namespace {
@@ -1769,7 +1784,7 @@ asrkf_status asrkf_accept_drafts(asrkf_ctx* ctx, int32_t n_nodes, const int32_t*
     a.list = ctx->list;
     a.n_active = ctx->n_active;
     a.listed_total = ctx->counters;
-    a.flags = ctx->flags;
+    a.no_room = &ctx->status->no_room;
     a.ticket = ctx->accept_ticket;
     a.L = c.n_layers;
     a.B = c.batch;
@@ -1801,6 +1816,7 @@ asrkf_status asrkf_stats(asrkf_ctx* ctx, asrkf_stats_t* out) {
     st = collect_timing(ctx);
     if (st != ASRKF_OK) return st;
     st = check_overflow(ctx, true);
+    if (st == ASRKF_OK) st = report_no_room(ctx);
     if (st != ASRKF_OK) return st;
     const asrkf_config& c = ctx->cfg;
     const size_t inst = (size_t)ctx->state_layers * c.batch;
@@ -1899,6 +1915,7 @@ asrkf_status asrkf_get_state(asrkf_ctx* ctx, int32_t layer, int32_t seq, int32_t
     st = sync_ctx(ctx);
     if (st != ASRKF_OK) return st;
     st = check_overflow(ctx, true);
+    if (st == ASRKF_OK) st = report_no_room(ctx);
     if (st != ASRKF_OK) return st;
     const int n = ctx->plen_host[seq] + ctx->t;
     const size_t sidx = (size_t)(ctx->token_scope ? 0 : layer) * c.batch + seq;
@@ -1937,6 +1954,7 @@ asrkf_status asrkf_get_residency(asrkf_ctx* ctx, int32_t layer, int32_t seq, int
     st = sync_ctx(ctx);
     if (st != ASRKF_OK) return st;
     st = check_overflow(ctx, true);
+    if (st == ASRKF_OK) st = report_no_room(ctx);
     if (st != ASRKF_OK) return st;
     const int n = ctx->plen_host[seq] + ctx->t;
     if (n_positions) *n_positions = n;

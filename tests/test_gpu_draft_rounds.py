@@ -86,3 +86,52 @@ def test_a_round_is_captured_behind_drafts_that_were_counted_as_accepted():
         assert refused == [A._lib.ECAPACITY] * 2
     finally:
         r.close()
+
+
+def test_replayed_acceptance_without_room_leaves_the_rest_as_it_is():
+    """Replays whose drafts have no room in one of two sequences: the next waiting call says so, once, and the context
+    goes on with the bits of one in which that sequence accepted nothing."""
+    import torch
+    a, b = (Run([22, 4], N=4, max_ctx=30, L=2, seed=4, tau=6.0) for _ in range(2))
+    try:
+        A = a.A
+        k, v = a.nodes()
+        rows = [[tuple(a.randn(2, h, 64) for h in (8, 2, 2)) for _ in range(2)] for _ in range(3)]
+        path, takes, graphs = _i32([[0, 1, 2, 3], [3, 1, 0, 2]]), [_i32([0, 0]) for _ in range(2)], []
+        for r, n_path in zip((a, b), takes):
+            r.step(rows[0])
+            torch.cuda.synchronize()
+            graphs.append(torch.cuda.CUDAGraph())
+            with torch.cuda.graph(graphs[-1], stream=torch.cuda.Stream()):
+                A.asrkf_accept_drafts(r.ctx, path, n_path, k, v)
+
+        def replay(*most):
+            for g, n_path, n in zip(graphs, takes, most):
+                n_path.copy_(_i32(n))
+                torch.cuda.synchronize()
+                g.replay()
+            torch.cuda.synchronize()
+        for t in range(1, 4):
+            replay([2, 3], [2, 3])
+            assert [a.state(1, i)["n"] for i in range(2)] == [23 + 2 * t, 5 + 3 * t]
+        for _ in range(2):                           # no room for two behind 29 of 30, room in the other sequence
+            replay([2, 3], [0, 3])
+            with pytest.raises(A.AsrkfError, match="room") as e:
+                A.asrkf_stats(a.ctx)
+            assert e.value.code == A._lib.ECAPACITY
+            x, y = A.asrkf_stats(a.ctx), A.asrkf_stats(b.ctx)
+            assert x["total_positions"] == y["total_positions"] == 2 * sum(b.state(0, i)["n"] for i in range(2))
+        replay([1, 0], [1, 0])                       # one fits
+        assert [a.state(0, i)["n"] for i in range(2)] == [30, 20]
+        for layer in range(2):
+            for i in range(2):
+                x, y = a.state(layer, i), b.state(layer, i)
+                assert all(np.array_equal(x[key], y[key]) for key in x)
+                assert all(torch.equal(p, q) for p, q in zip(a.rows(layer, i, 0, x["n"]), b.rows(layer, i, 0, x["n"])))
+        for r in (a, b):                             # a full sequence takes no further step
+            with pytest.raises(A.AsrkfError) as e:
+                r.step(rows[1])
+            assert e.value.code == A._lib.ECAPACITY
+    finally:
+        a.close()
+        b.close()
