@@ -492,6 +492,7 @@ verify_walk_kernel(VerifyArgs a) {
     // the difference is off by, 2^-52 of the whole, stays below 2^-42 of what is left)
     const uint64_t again = __ballot(s < whole * 0x1p-10);
     if (again) {
+        __syncthreads();                          // every wave has read the shares that are replaced
         int turn = 0;
         for (uint64_t left = again; left; left &= left - 1, ++turn) {
             if (turn % (kWalkThreads / 64) != wave) continue;
