@@ -46,8 +46,9 @@ __device__ __forceinline__ double exp2_64(double x) {
     r = fma(r, f, 1.0);
     return __builtin_ldexp(r, (int)k);
 }
-// e^((x - m) / T), m / T in units of ln 2 given.  (Its rounding is one factor for a whole row's weights.)
-__device__ __forceinline__ double exp_of(float x, double inv_t, double m_t) { return exp2_64(fma((double)x, inv_t, -m_t)); }
+// e^((x - m) / T), inv_t = log2(e) / T.  The difference first: of products that are rounded each, what is left would be
+// off by 2^-53 of m / T, which is 10^-9 of logits near 30 at T = 10^-6, and another factor in every part with a maximum of its own.
+__device__ __forceinline__ double exp_of(float x, double inv_t, double m) { return exp2_64(((double)x - m) * inv_t); }
 
 // Sums over a wave's lanes in six DPP steps: within rows of 16, then the rows before.  (Each is a
 // few cycles where a permute through LDS is a round trip: the walk of 8 chains took 16.6 us with those.)
@@ -183,11 +184,10 @@ verify_sums_kernel(VerifyArgs a) {
                 for (int e = 0; e < 4; ++e)
                     if (v[u][e] == m && top == m) at = min(at, j + (u * kThreads + (int)threadIdx.x) * 4 + e);
         } else if (m > -INFINITY && m < INFINITY) {
-            const double m_t = m * a.inv_t;
 #pragma unroll
             for (int u = 0; u < kQuads; ++u)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) S += exp_of(v[u][e], a.inv_t, m_t);
+                for (int e = 0; e < 4; ++e) S += exp_of(v[u][e], a.inv_t, m);
         }
     }
     // what the walk looks up: the logit and the draft's probability of the children in this part
@@ -222,7 +222,7 @@ struct Weights {
     static constexpr int kWaves = THREADS / 64;
     const float* x;
     const float* q;               // null: c is 0
-    double inv_t, m_t, scale, c;
+    double inv_t, m, scale, c;
     int n_gone, gone;             // tokens without weight, one to a lane
     double* lds;                  // [kWaves]
     int* found;                   // LDS, [2]
@@ -231,7 +231,7 @@ struct Weights {
     __device__ __forceinline__ void four(floatx4 xv, floatx4 qv, double (&w)[4]) const {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            w[e] = exp_of(xv[e], inv_t, m_t) * scale;
+            w[e] = exp_of(xv[e], inv_t, m) * scale;
             if (q) w[e] = fmax(w[e] - c * (double)qv[e], 0.0);
         }
     }
@@ -411,7 +411,7 @@ verify_walk_kernel(VerifyArgs a) {
     double mass = 0.0;                            // p(x) behind the parent
     if (parent >= -1 && token >= 0 && a.inv_t != 0.0) {
         const VerifyPart p = rows[parent + 1];
-        if (p.at >= 0) mass = exp_of(chance.x, a.inv_t, p.m * a.inv_t) / p.S;
+        if (p.at >= 0) mass = exp_of(chance.x, a.inv_t, p.m) / p.S;
     }
     const double q = chance.y;
 
@@ -459,7 +459,7 @@ verify_walk_kernel(VerifyArgs a) {
                 c = c2;
                 break;
             }
-            const Weights<kWalkThreads> w{row_of(a, b, last + 1), draft_row(a, b, last + 1), a.inv_t, p.m * a.inv_t, 1.0 / p.S, c2, 0, 0, sums, found};
+            const Weights<kWalkThreads> w{row_of(a, b, last + 1), draft_row(a, b, last + 1), a.inv_t, p.m, 1.0 / p.S, c2, 0, 0, sums, found};
             const double sum = w.template sum<4>(0, a.V);
             if (sum > 0.0) {
                 c = c2;
@@ -481,7 +481,7 @@ verify_walk_kernel(VerifyArgs a) {
     if (n_gone && wave == 0 && (weighed >> lane & 1)) gone_lds[__popcll(weighed & ((1ull << lane) - 1ull))] = token;
     if (n_gone) __syncthreads();
     const int gone = lane < n_gone ? gone_lds[lane] : -1;
-    const Weights<kWalkThreads> w{row_of(a, b, last + 1), nullptr, a.inv_t, p.m * a.inv_t, 1.0 / p.S, 0.0, n_gone, gone, sums, found};
+    const Weights<kWalkThreads> w{row_of(a, b, last + 1), nullptr, a.inv_t, p.m, 1.0 / p.S, 0.0, n_gone, gone, sums, found};
     const double whole = share[last + 1][lane];
     double s = whole;
     for (uint64_t left = weighed; left; left &= left - 1) {
@@ -522,7 +522,7 @@ verify_rest_kernel(VerifyArgs a) {
     const VerifyEnd e = a.end[b];
     const double u = a.u[(size_t)b * (a.N + 1) + a.N];
     if (e.row < 0) return;
-    Weights<kWalkThreads> w{row_of(a, b, e.row), draft_row(a, b, e.row), a.inv_t, e.m * a.inv_t, e.scale, e.c, 0, 0, lds, found};
+    Weights<kWalkThreads> w{row_of(a, b, e.row), draft_row(a, b, e.row), a.inv_t, e.m, e.scale, e.c, 0, 0, lds, found};
     {
         const double sum = w.template sum<1>(sp * a.part_len, min(a.V, (sp + 1) * a.part_len));
         if (threadIdx.x == 0) {

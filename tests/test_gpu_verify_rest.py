@@ -29,3 +29,67 @@ def test_parts_of_which_next_to_nothing_is_left(V, T):
             assert (n == 0).all() and not (nxt[:, None] == c.tokens).any()
     finally:
         A.asrkf_destroy(ctx)
+
+
+def _beside(about, octave, which):
+    """A temperature near `about` at which two logits, neighbours among the fp32 numbers from `octave` to twice that, have
+    a probability (of the larger or the smaller one) just beside an fp32 number: 10^-12 to 5 * 10^-10 of it."""
+    rng = np.random.default_rng(1)
+    T = (about * rng.uniform(0.9, 1.1, 100000)).astype(np.float32).astype(np.float64)
+    z = np.exp(-octave * 2.0 ** -23 / T)
+    p = (1 / (1 + z), z / (1 + z))[which]
+    u = p.astype(np.float32)
+    off = np.abs(u - p) / p
+    at = int(np.nonzero((off > 1e-12) & (off < 5e-10))[0][0])
+    return float(T[at]), u[at]
+
+
+@pytest.mark.parametrize("about,octave", [(1.2e-6, 16.0), (2.4e-6, 32.0), (2e-5, 256.0), (2e-3, 32768.0)])
+@pytest.mark.parametrize("V", [5000, 262144 + 9000])
+@pytest.mark.parametrize("first", [0, 1])
+def test_cold_rows_over_several_parts(about, octave, V, first):
+    """Temperatures at which a step of fp32 logits weighs e and more: two tokens in different parts of the row have all
+    of the weight, and the random numbers lie 10^-12 to 5 * 10^-10 beside the drafted token's probability, or beside
+    where the draw passes from the first of them in the vocabulary to the other."""
+    B = 512 if V < 10000 else 24
+    A, ctx = _init(B, V, 1)
+    try:
+        at = (V - 700, 12) if first else (12, V - 700)       # of the larger one and the smaller one
+        for draw in (False, True):
+            which = first if draw else 1
+            T, u = _beside(about, octave, which)
+            c = Case(B, 1, V, False, 0, ragged=False)
+            x = (octave * c.rng.uniform(1.001, 1.999, B)).astype(np.float32)
+            c.parents[:] = -1
+            c.root[:] = -np.inf
+            c.root[:, at[0]], c.root[:, at[1]] = x, np.nextafter(x, np.float32(0))
+            c.tokens[:] = -1 if draw else at[1]              # (one outside the vocabulary leaves the row as it is)
+            c.u[:, 0], c.u[:, 1] = (0.5, u) if draw else (u, 0.5)
+            c.check(c.run(A, ctx, T, count=False), T)
+    finally:
+        A.asrkf_destroy(ctx)
+
+
+@pytest.mark.parametrize("scale,T", [(1e12, 1e-6), (3e38, 1.0), (3e38, 1e-6), (1e30, 0.7)])
+@pytest.mark.parametrize("probs", [False, True])
+def test_the_largest_logits(scale, T, probs):
+    """Logits whose quotient by the temperature is known to more than a factor no longer: equal ones share the weight."""
+    T = float(np.float32(T))
+    B, V = 40, 9000
+    A, ctx = _init(B, V, 3)
+    try:
+        c = Case(B, 3, V, probs, 5, ragged=False)
+        rows = np.concatenate([c.root[:, None], c.logits], 1)
+        rows *= np.float32(scale / 100)
+        for b in range(B):
+            for i in range(4):
+                rows[b, i, c.rng.integers(0, V, 3)] = np.float32(scale) * np.float32(c.rng.uniform(0.5, 1))
+                if i < 3:
+                    c.tokens[b, i] = rows[b, i].argmax()
+        c.parents[:] = [-1, 0, 1]
+        c.root, c.logits = rows[:, 0].copy(), rows[:, 1:].copy()
+        got = c.run(A, ctx, T, count=False)
+        c.check(got, T)
+        assert got[1].any() and (got[2] >= 0).all()
+    finally:
+        A.asrkf_destroy(ctx)
