@@ -267,6 +267,7 @@ struct Weights {
             for (int u = 0; u < kQuads; ++u) {
                 double w[4];
                 four(xv[u], qv[u], w);
+                leave_out(j + (u * THREADS + (int)threadIdx.x) * 4, w);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) s += w[e];
             }
@@ -415,8 +416,16 @@ verify_walk_kernel(VerifyArgs a) {
     }
     const double q = chance.y;
 
+    // the tokens of those nodes, one to a lane
+    auto left_out = [&](uint64_t which) __attribute__((always_inline)) {
+        if (wave == 0 && (which >> lane & 1)) gone_lds[__popcll(which & ((1ull << lane) - 1ull))] = token;
+        __syncthreads();
+        return lane < __popcll(which) ? gone_lds[lane] : -1;
+    };
+
     int last = -1, n_path = 0;
     double W = 1.0, c = 0.0, c_before = -1.0;     // w = max(p - c q, 0), W its sum
+    double W_summed = 1.0;                        // the sum that W was last formed as, before differences
     uint64_t rejected = 0, weighed = 0;           // since the last one kept; those of them that had a weight
     uint64_t todo = ~0ull;                        // nodes not looked at yet
     for (;;) {                                    // (the same in every wave)
@@ -439,6 +448,13 @@ verify_walk_kernel(VerifyArgs a) {
                 if (!yes && !a.probs) {
                     W -= w;
                     weighed |= w > 0.0 ? 1ull << i : 0;
+                    // The difference is off by 10^-13 of the sum, as the exponentials are.  Where next to nothing
+                    // is left and another sibling asks, it is summed again, so that the last token of any weight is kept.
+                    if (W < W_summed * 0x1p-10 && (__ballot(parent == last) & todo)) {
+                        const Weights<kWalkThreads> rest{row_of(a, b, last + 1), nullptr, a.inv_t, p.m, 1.0 / p.S, 0.0, (int)__popcll(weighed),
+                                                         left_out(weighed), sums, found};
+                        W = W_summed = rest.template sum<4>(0, a.V);
+                    }
                 }
             }
         }
@@ -446,7 +462,7 @@ verify_walk_kernel(VerifyArgs a) {
             if (threadIdx.x == 0) a.path[(size_t)b * a.N + n_path] = i;
             ++n_path;
             last = i;
-            W = 1.0;
+            W = W_summed = 1.0;
             c = 0.0;
             rejected = weighed = 0;
             continue;
@@ -477,10 +493,7 @@ verify_walk_kernel(VerifyArgs a) {
     if (a.inv_t == 0.0 || p.at < 0 || c != 0.0) return;
 
     // the draw from p without the rejected tokens
-    const int n_gone = __popcll(weighed);
-    if (n_gone && wave == 0 && (weighed >> lane & 1)) gone_lds[__popcll(weighed & ((1ull << lane) - 1ull))] = token;
-    if (n_gone) __syncthreads();
-    const int gone = lane < n_gone ? gone_lds[lane] : -1;
+    const int n_gone = __popcll(weighed), gone = n_gone ? left_out(weighed) : -1;
     const Weights<kWalkThreads> w{row_of(a, b, last + 1), nullptr, a.inv_t, p.m, 1.0 / p.S, 0.0, n_gone, gone, sums, found};
     const double whole = share[last + 1][lane];
     double s = whole;
@@ -489,7 +502,7 @@ verify_walk_kernel(VerifyArgs a) {
         s -= lane == sp ? of_lane(mass, i) : 0.0;
     }
     // a part of which next to nothing is left is summed again without those tokens, a wave to a part (what
-    // the difference is off by, 2^-52 of the whole, stays below 2^-42 of what is left)
+    // the difference is off by, 10^-13 of the whole, stays below 10^-10 of what is left)
     const uint64_t again = __ballot(s < whole * 0x1p-10);
     if (again) {
         __syncthreads();                          // every wave has read the shares that are replaced
@@ -505,8 +518,8 @@ verify_walk_kernel(VerifyArgs a) {
     }
     double left;
     const int sp = part_of_point(s, (double)u_last, left);
-    // no weight is left only where W, a difference, was rounded upwards and the last token that had one was
-    // rejected for that: it is the next one
+    // no weight is left only where a random number of 1 and more rejected the last token that had one: it is
+    // the next one
     const int tok = sp < 0 ? __builtin_amdgcn_readlane(token, 63 - __builtin_clzll(weighed | 1))
                            : w.find(sp * a.part_len, min(a.V, (sp + 1) * a.part_len), left);
     if (threadIdx.x == 0) a.next[b] = tok;

@@ -93,3 +93,54 @@ def test_the_largest_logits(scale, T, probs):
         assert got[1].any() and (got[2] >= 0).all()
     finally:
         A.asrkf_destroy(ctx)
+
+
+@pytest.mark.parametrize("T", [0.7, 1.0, 1.9])
+@pytest.mark.parametrize("V", [20000, 300000])
+def test_the_last_token_of_any_weight_is_kept(V, T):
+    """Three tokens have all of the weight and the first two drafts of them are rejected: W is the third's weight, which
+    u < 1 keeps, however little it is."""
+    B = 1024 if V < 100000 else 64
+    T = float(np.float32(T))
+    A, ctx = _init(B, V, 4)
+    try:
+        c = Case(B, 4, V, False, int(T * 10), ragged=False)
+        c.parents[:] = [-1, -1, -1, 2]
+        c.tokens[:] = [5000, 10, 15000, 77]
+        c.root[:] = -np.inf
+        c.root[:, 5000] = c.rng.uniform(-9, 9, B)
+        c.root[:, 10] = c.root[:, 5000] + c.rng.uniform(-1, 1, B).astype(np.float32)
+        c.root[:, 15000] = c.root[:, 5000] + T * np.log(10.0 ** c.rng.uniform(-6.5, -5.5, B)).astype(np.float32)
+        c.u[:, :3] = 1 - 2.0 ** -24
+        got = c.run(A, ctx, T, count=False)
+        c.check(got, T)
+        assert (got[1] >= 1).all() and (got[0][:, 0] == 2).all()
+    finally:
+        A.asrkf_destroy(ctx)
+
+
+def test_siblings_that_weigh_less_and_less():
+    """Up to five siblings, each with all but 10^-1 to 10^-6.5 of what the ones before it have left, over a floor of
+    further tokens or none, and random numbers near 1: many rejections in a row, W down to 10^-30."""
+    B, N, V = 1024, 5, 9000
+    A, ctx = _init(B, V, N)
+    try:
+        deep = 0
+        for seed in range(4):
+            c = Case(B, N, V, False, seed, ragged=False)
+            c.parents[:] = -1
+            c.root[:] = -np.inf
+            c.root[B // 2:, 6000:] = -80.0
+            left = np.zeros(B)
+            for i in range(N):
+                c.tokens[:, i] = c.rng.permutation(V)[:B] % 6000
+                share = 10.0 ** c.rng.uniform(-6.5, -1, B)
+                c.root[np.arange(B), c.tokens[:, i]] = (left + np.log1p(-share)).astype(np.float32)
+                left += np.log(share)
+            c.u[:, :N] = 1 - c.rng.choice([2.0 ** -24, 2.0 ** -22, 2.0 ** -18], (B, N))
+            path, n, nxt = got = c.run(A, ctx, 1.0, count=False)
+            c.check(got, 1.0)
+            deep += ((n == 0) | (path[:, 0] >= 2)).sum()
+        assert deep > 1000
+    finally:
+        A.asrkf_destroy(ctx)
