@@ -1399,7 +1399,7 @@ asrkf_status asrkf_rotate(asrkf_ctx* ctx, int32_t n_rows, int32_t rows_per_seq, 
         return fail(ASRKF_EINVAL, "n_rows must be rows_per_seq for every one of the %d sequences", c.batch);
     if (rows_per_seq == 0 && !pos && n_rows > 0) return fail(ASRKF_EINVAL, "null positions");
     if (!q != !q_out || !k != !k_out) return fail(ASRKF_EINVAL, "rows and their outputs go together");
-    if (!q && !k) return fail(ASRKF_EINVAL, "neither q nor k");
+    if (!q && !k && n_rows > 0) return fail(ASRKF_EINVAL, "neither q nor k");      // (no rows may have no address)
     st = on_device(ctx);
     if (st != ASRKF_OK) return st;
     RotateArgs a = ctx->rotate;
