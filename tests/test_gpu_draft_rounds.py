@@ -135,3 +135,86 @@ def test_replayed_acceptance_without_room_leaves_the_rest_as_it_is():
     finally:
         a.close()
         b.close()
+
+
+@pytest.mark.parametrize("kw,tau", [(dict(), 8.0), (dict(dtype="f32"), 8.0), (dict(kv_bits=4, D=128), 11.0), (dict(scope="token"), 8.0),
+                                    (dict(history_W=3), 8.0), (dict(relevance="softmax"), 0.02)], ids=str)
+def test_counts_behind_an_acceptance(kw, tau):
+    """Steps behind an acceptance against those of a context whose prompt held the tokens, with a tau that the tokens
+    outside the window fall below in every variant: outputs, counts, lists."""
+    import torch
+    N = 5
+    a = Run([60, 58], N=N, seed=3, tau=tau, window_K=61, **kw)
+    try:
+        k, v = a.nodes()
+        rows = [[tuple(a.randn(2, h, a.D) for h in (8, a.Hkv, a.Hkv)) for _ in range(a.L)] for _ in range(6)]
+        a.step(rows[0])
+        a.A.asrkf_accept_drafts(a.ctx, _i32([[0, 1, 2, 3, 4]] * 2), _i32([N, 3]), k, v)
+        got = [a.step(x) for x in rows[1:]]
+        b = Run([60 + 1 + N, 58 + 1 + 3], N=N, seed=3, tau=tau, window_K=61, **kw)
+        try:
+            for layer in range(a.L):
+                K, V = [], []
+                for i, (p, take) in enumerate(zip((0, 60), (N, 3))):
+                    for out, x, j, d in ((K, a.prompts[layer][0], 1, k), (V, a.prompts[layer][1], 2, v)):
+                        out += [x[p:p + a.lens[i]], rows[0][layer][j][i:i + 1], d[layer, i, :take]]
+                b.A.asrkf_prefill_packed(b.ctx, layer, range(2), b.lens, None, torch.cat(K), torch.cat(V), None)
+            for x, y in zip(got, [b.step(x) for x in rows[1:]]):
+                # fp32 sums of up to 71 terms of |v| < 5 either way
+                assert (x - y).abs().max() <= 200 * 2.0 ** -24 * 5
+            for layer in range(a.L):
+                for i in range(2):
+                    x, y = a.state(layer, i), b.state(layer, i)
+                    assert x["n"] == y["n"] and list(x["count"]) == list(y["count"]) and list(x["active"]) == list(y["active"])
+                    assert x["count"].any() and x["frozen"].any()
+        finally:
+            b.close()
+    finally:
+        a.close()
+
+
+@pytest.mark.parametrize("kw", [dict(dtype="f32"), dict(), dict(kv_bits=4, D=128), dict(scope="token"), dict(D=256, Hkv=4)], ids=str)
+def test_replayed_rounds_have_the_bits_of_eager_ones(kw):
+    """A captured round, step, drafts and acceptance, against a context that runs the same calls: every replay's outputs
+    bit by bit, with lists that freeze and grow."""
+    import torch
+    a, b = (Run([40, 300], N=6, max_ctx=400, L=2, seed=9, tau=6.0, **kw) for _ in range(2))
+    try:
+        A, N, D, Hkv = a.A, 6, a.D, a.Hkv
+        q, q0 = a.randn(2, N, 8, D), [[a.randn(2, h, D) for h in (8, Hkv, Hkv)] for _ in range(2)]
+        k, v = a.nodes()
+        sees = torch.tensor([[1, 3, 5, 9, 17, 33], [1, 3, 7, 15, 31, 63]], device="cuda")
+        path, n_path = _i32([[0, 1, -1, 0, 0, 0], [2, 3, 5, 0, 0, 0]]), _i32([2, 1])
+        outs = {}
+
+        def calls(r):
+            o0, o = outs.setdefault(r, (torch.empty((2, 2, 8, D), device="cuda"), torch.empty((2,) + q.shape, dtype=q.dtype, device="cuda")))
+            for layer in range(2):
+                A.asrkf_decode_step(r.ctx, layer, *q0[layer], o0[layer])
+                A.asrkf_attend_drafts(r.ctx, layer, sees, q, k[layer], v[layer], o[layer])
+            A.asrkf_restore(r.ctx, None, A.NONE)
+            A.asrkf_accept_drafts(r.ctx, path, n_path, k, v)
+        for r in (a, b):
+            calls(r)
+            torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=torch.cuda.Stream()):
+            calls(a)
+        for t in range(6):
+            n_path.copy_(_i32([t % 3, 3 - t % 4]))
+            q.copy_(b.randn(*q.shape))
+            torch.cuda.synchronize()
+            g.replay()
+            torch.cuda.synchronize()
+            calls(b)
+            torch.cuda.synchronize()
+            assert all(torch.equal(x, y) for x, y in zip(outs[a], outs[b]))
+            for layer in range(2):
+                for i in range(2):
+                    x, y = a.state(layer, i), b.state(layer, i)
+                    assert all(np.array_equal(x[key], y[key]) for key in x)
+            torch.zeros(5000, device="cuda").sum().item()
+        assert any(a.state(layer, 1)["frozen"].any() for layer in range(2))
+    finally:
+        a.close()
+        b.close()
