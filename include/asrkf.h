@@ -433,7 +433,7 @@ asrkf_status asrkf_attend_drafts(asrkf_ctx* ctx, int32_t layer, int32_t n_nodes,
  *   next:        device, [batch] (written): the next token.  -1 where the logits
  *                behind the last node kept hold a NaN, +inf, or nothing above -inf: no child
  *                of such a row is kept.
- * Exponentials and sums are 64-bit.  EINVAL where an array reaches past the end of an
+ * Exponentials, to 4e-14 of themselves, and sums are 64-bit.  EINVAL where an array reaches past the end of an
  * allocation or an output overlaps another array.  Asynchronous. */
 asrkf_status asrkf_verify_drafts(asrkf_ctx* ctx, int32_t n_nodes, const int32_t* count, const int32_t* tokens,
                                  const int32_t* parents, const float* root_logits, const float* logits,

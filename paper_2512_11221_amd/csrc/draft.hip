@@ -18,9 +18,9 @@
 // second launch folds in order.
 //
 // Bound, by the query rows that a list's bytes meet: to 32 rows by the stream of K and V (8 sequences of 32768 tokens, a
-// third of them active, 8 KV heads of 128 in bf16, 20 query rows: 73 us, 5.2 TB/s of rows, their lines read in part); with 256 by
-// matrix cores, LDS and exponentials, a third each (4 of 12000 to 16384: 86 us, 0.6 PFLOP/s; the slope of long lists is
-// 0.96); short lists by five round trips, one after the other: 10 us for 512 tokens.  (Folded by the workgroup that
+// third of them active, 8 KV heads of 128 in bf16, 20 query rows: 73 us, 5.2 TB/s of rows; 5% more is fetched, of tiles
+// behind a part's end, which are asked for ahead); with 256 by matrix cores, LDS and exponentials, a third each (4 of
+// 12000 to 16384: 86 us, 0.6 PFLOP/s; the slope of long lists is 0.96); short lists by five round trips, one after the other: 10 us for 512 tokens.  (Folded by the workgroup that
 // arrives last, a megabyte of partials went through one compute unit: 64 rows of one sequence of 8000 tokens, 8 KV
 // heads, took 77 us, with a launch of its own 40.)
 #include <algorithm>

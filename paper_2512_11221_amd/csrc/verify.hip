@@ -13,13 +13,15 @@
 // Greedy (T = 0): a node is accepted where its token has the largest logit, the lowest index among
 // equals, and the next token is the one with the largest.
 // Accepted or not, and which token: decisions on sums over a vocabulary whose neighbours lie 10^-6
-// apart.  Exponentials and sums are 64-bit, so that they do not hang on the order of summation.
+// apart.  Exponentials (to 4e-14 of themselves) and sums are 64-bit, so that they do not hang on the order of summation.
 //
 // Launches: the sums of every row of logits, in parts of at most 64 to a row, and the walk, a workgroup to a
 // sequence, which also draws the next token: the parts' sums say which part holds the drawn point, and
-// only that one is read again.  The sums of 17 rows of 50257 logits of 32 sequences take 21.6 us (3.7 TB/s; the 64-bit
-// operations alone are 11 at the vector units' rate), of 6 rows of 128256 of 8 8.6; the walk, bound by round trips, 8 to 10.  Where the walk ends behind a rejection with draft probabilities the
-// weights are other ones, whose sums a third launch forms.
+// only that one is read again.  The sums of 399 rows of 50257 logits (32 sequences of 9 to 17) take 22.1 us (3.6 TB/s; the
+// 64-bit operations alone are 12 at the vector units' rate), of 48 rows of 128256 9.0; the walk, bound by round trips, 9 to
+// 10.  Where the walk ends behind a rejection with draft probabilities the weights are other ones, whose sums a third
+// launch forms; where such a rejection has a sibling to look at, the walk's workgroup forms them alone, 24 us a
+// rejection over 128256 tokens.
 #include "kernels.h"
 #include "tiles.h"
 
